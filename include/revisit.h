@@ -22,6 +22,14 @@
  *                                values into the cache, keys re-rotated to
  *                                the packed positions (Sec. 4.2)
  *
+ * The operators around that cache:
+ *
+ *   rotary_embed              -- rotary position embedding of queries and keys
+ *                                over time, row and column
+ *   attention_key_weight      -- the weight of every cached key in the attention
+ *   select_kept               -- which units of the cache to keep, by weight
+ *   compact_kv                -- move of the kept units into a smaller cache
+ *
  * and a streaming driver (rc_stream_*) that runs the paper's cache layout
  * chunk by chunk on the device.
  *
@@ -423,6 +431,159 @@ int reproject_rotation(const float* tgt_c2w, const float* tgt_K, const float* sr
  */
 int pool_token_depth(const float* depth, int32_t n_frames, int32_t h, int32_t w, int32_t p,
                      float* out, hipStream_t stream);
+
+/*
+ * rotary_embed -- rotary position embedding of queries and keys over three axes.
+ *
+ * A head's D elements are pairs (x_{2i}, x_{2i+1}). The first pairs_t pairs are
+ * the temporal band, the next pairs_y the grid row's, the next pairs_x the grid
+ * column's; pairs behind them are copied. Pair j of a band of n pairs is read
+ * as x_{2i} + i x_{2i+1} and multiplied by exp(i P theta^(-j / n)), P the token's
+ * position on that axis: the embedding whose temporal band pack_retrieved_kv
+ * and compact_kv turn. With inverse = 1 the angles are negated; as a
+ * rotation's transpose is its inverse, that is also the way from the gradients
+ * of the outputs to the gradients of q and k.
+ *
+ *   dtype        REVISIT_BF16, REVISIT_F32 (outputs in the same type), or
+ *                REVISIT_FP8_QK: q and k in bf16, outputs in fp8 e4m3, the
+ *                embedded value times q_scale / k_scale rounded to nearest even,
+ *                values beyond +-448 taken as +-448 (NaN stays NaN). The scales are
+ *                read for REVISIT_FP8_QK only.
+ *   q, k         [n_tokens] rows of [Hq][D] / [Hk][D] elements, row r starting q_row /
+ *                k_row elements after row r - 1 (so both may be views into the rows of
+ *                one projection); k nullable (q alone)
+ *   q_out, k_out the same with q_out_row / k_out_row. An output may be its own
+ *                input (same pointer, type and row stride); else it must not overlap
+ *                any input or output row.
+ *   D            a multiple of 8 in [8, 512]; pairs_t + pairs_y + pairs_x <= D / 2
+ *   pos          [n_tokens][3] int32: time, row and column of each token, any values;
+ *                or NULL: token r stands at (t0 + r / (h w), r / w mod h, r mod w)
+ *   theta > 0
+ *
+ * Angles are evaluated in double, their cos and sin to a few 1e-8, products
+ * and sums in fp32, and the result is rounded once to the output's type.
+ * Rows must start on 16 bytes (fp8 outputs on 8): pointers and row strides,
+ * REVISIT_ERR_SHAPE otherwise. n_tokens == 0 is valid (nothing to do).
+ */
+int rotary_embed(const void* q, int64_t q_row, const void* k, int64_t k_row,
+                 void* q_out, int64_t q_out_row, void* k_out, int64_t k_out_row,
+                 int32_t dtype, int32_t n_tokens, int32_t Hq, int32_t Hk, int32_t D,
+                 const int32_t* pos, int32_t t0, int32_t h, int32_t w,
+                 int32_t pairs_t, int32_t pairs_y, int32_t pairs_x, float theta,
+                 int32_t inverse, float q_scale, float k_scale, hipStream_t stream);
+
+/*
+ * attention_key_weight -- the weight of every cached key in the attention, the
+ * measure an eviction goes by:
+ *     out[h][k] = decay * prev[h][k] + sum_p exp(A_pk - LSE_p[h])
+ * with the logits A of biased_chunk_attention (bias included) and the LSE that
+ * call returned for the same q, k, bias and scale, or for a larger set of keys
+ * of which k is a part. A summand is a probability: one above 1, which such an LSE
+ * gives by rounding only, counts as 1. A query whose LSE is not finite (no key had
+ * weight, or NaN) adds nothing.
+ *
+ *   q, k, dtype, Lq, Lk, H, D, h, w, kv_frame_slot, corr_uv, corr_idx, S,
+ *   softmax_scale, lambda, sigma  as for biased_chunk_attention, with its limits
+ *   lse          [H][Lq] fp32
+ *   prev         nullable [H][Lk] fp32 (NULL: nothing is added; may be out itself)
+ *   decay        finite
+ *   out          [H][Lk] fp32
+ *
+ * Lq == 0 is valid (out = decay * prev, or 0). Exponentials and sums are fp32;
+ * the result does not change between calls (no atomics).
+ *
+ *   query_parts  0 = chosen from the shape and the compute units of the current
+ *                device, or a fixed number in [1, 64] (clamped to the number of
+ *                32-query tiles) of parts into which the queries are cut; the parts'
+ *                sums are added in their order by a second kernel
+ *   workspace, workspace_bytes  device scratch of at least the size
+ *                rc_key_weight_workspace_size() returns on the same device
+ *                (parts * H * Lk * 4 bytes when parts > 1, else 0), 16-byte aligned;
+ *                may be NULL / 0 when that size is 0. Too small:
+ *                REVISIT_ERR_SHAPE; NULL while needed: REVISIT_ERR_NULL. S is 0 in
+ *                the size query where the call has lambda = 0.
+ */
+int attention_key_weight(const void* q, const void* k, const float* lse, int32_t dtype,
+                         int32_t Lq, int32_t Lk, int32_t H, int32_t D, int32_t h, int32_t w,
+                         const int32_t* kv_frame_slot,
+                         const float* corr_uv, const int32_t* corr_idx, int32_t S,
+                         float softmax_scale, float lambda, float sigma,
+                         const float* prev, float decay, float* out,
+                         int32_t query_parts, void* workspace, size_t workspace_bytes,
+                         hipStream_t stream);
+
+int rc_key_weight_workspace_size(int32_t dtype, int32_t Lq, int32_t Lk, int32_t H, int32_t D,
+                                 int32_t h, int32_t w, int32_t S, int32_t query_parts, size_t* bytes);
+
+/*
+ * select_kept -- which units of a cache stay, by accumulated weight.
+ *
+ * The cache is n_units units of `unit` tokens each (1: by token; h w: by frame).
+ * For every set (a layer, or a layer's head)
+ *     score[u] = the sum of weight over the set's heads and the unit's tokens,
+ * taken in double and rounded once to fp32; the first `first` units (the
+ * anchor) and the last `last` (the recent window) stay in any case, and of
+ * the others those of largest score, so that `keep` units stay. Equal scores
+ * go to the smaller unit; NaN counts as smaller than any number, -0 as 0.
+ *
+ *   weight       [sets][heads][n_units * unit] fp32 (attention_key_weight)
+ *   out_idx      [sets][keep] int32: the units that stay, ascending
+ *   out_score    nullable [sets][keep] fp32: their scores
+ *   first, last >= 0, first + last <= keep <= n_units (REVISIT_ERR_PARAM otherwise)
+ *   sets <= 2^21, n_units <= 2^30
+ *   workspace, workspace_bytes  device scratch of at least the size
+ *                rc_select_workspace_size() returns, 16-byte aligned; may be
+ *                NULL / 0 when that size is 0. Too small: REVISIT_ERR_SHAPE; NULL
+ *                while needed: REVISIT_ERR_NULL.
+ * sets == 0 or keep == 0 is valid (nothing to do).
+ */
+int select_kept(const float* weight, int32_t sets, int32_t heads, int32_t n_units, int32_t unit,
+                int32_t keep, int32_t first, int32_t last,
+                int32_t* out_idx, float* out_score,
+                void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+int rc_select_workspace_size(int32_t sets, int32_t heads, int32_t n_units, int32_t unit, size_t* bytes);
+
+/*
+ * compact_kv -- move of a cache's kept units into a smaller cache.
+ *
+ * For every layer l, kept place i, head h, row r of a unit, with
+ * u = sel[l][h or 0][i]:
+ *     dst_k[l][dst_row0 + i unit + r][h] = src_k[l][u unit + r][h]   (dst_v alike)
+ *     dst_weight[l][h][dst_row0 + i unit + r] = src_weight[l][h][u unit + r]
+ * Keys' first rope_t_pairs pairs are turned as pack_retrieved_kv turns
+ * them, from the unit's frame position to the one of its new place:
+ *     delta = dst_pos + i frames_per_unit - (src_pos ? src_pos[u] : u frames_per_unit),
+ * with the precision of rotary_embed; where delta is 0, and everywhere else, elements
+ * are copied bit for bit.
+ *
+ *   dtype        REVISIT_BF16, REVISIT_F32 (D a multiple of 8 up to 512), or
+ *                REVISIT_FP8_QK (keys fp8, values bf16, D a multiple of 16;
+ *                rope_t_pairs must be 0, REVISIT_ERR_UNSUPPORTED otherwise)
+ *   src_k, src_v [n_layers][src_rows][H][D], of which n_units * unit rows are units
+ *   dst_k, dst_v [n_layers][dst_rows][H][D]; rows outside
+ *                [dst_row0, dst_row0 + keep * unit) are left as they are
+ *   sel          [n_layers][sel_heads][keep] int32, sel_heads 1 (all heads keep the
+ *                same units) or H (each its own; select_kept with sets = layers or
+ *                layers * H). Any order, repeats allowed; an entry outside
+ *                [0, n_units) leaves its unit's rows of the destination as they are
+ *   src_weight, dst_weight  both NULL, or [n_layers][H][src_weight_cols] and
+ *                [n_layers][H][dst_weight_cols] fp32
+ *   src_pos      nullable [n_units] int32 (read with rope_t_pairs > 0 only)
+ *   rope_t_pairs 0..D/2 (0 = plain copy); rope_theta > 0, frames_per_unit >= 0
+ *                (read with rope_t_pairs > 0 only)
+ *
+ * Source and destination must not overlap (REVISIT_ERR_SHAPE); caches must be
+ * 16-byte aligned. n_layers == 0 or keep == 0 is valid (nothing to do).
+ */
+int compact_kv(const void* src_k, const void* src_v, int32_t src_rows,
+               const int32_t* sel, int32_t sel_heads, int32_t keep, int32_t unit, int32_t n_units,
+               void* dst_k, void* dst_v, int32_t dst_rows, int32_t dst_row0,
+               const float* src_weight, int32_t src_weight_cols,
+               float* dst_weight, int32_t dst_weight_cols,
+               int32_t n_layers, int32_t dtype, int32_t H, int32_t D,
+               const int32_t* src_pos, int32_t dst_pos, int32_t frames_per_unit,
+               int32_t rope_t_pairs, float rope_theta, hipStream_t stream);
 
 /*
  * Streaming driver -- Sec. 4.2 (cache layout, loop-closure retrieval, cache

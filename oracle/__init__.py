@@ -24,6 +24,8 @@ Modules, each citing the passage of the paper it writes out:
 * ``stream``       -- the cache layout run chunk by chunk over a trajectory:
   history ring, retrieval, slot table, correspondence, packing and biased
   attention composed as the method runs them (Sec. 4.2, Sec. 4.3);
+* ``cache``        -- the operators around the attention cache: rotary positions,
+  the weight of every key, the choice of kept units and their move;
 * ``brute``        -- pure-Python loop versions of the first three, for tiny
   inputs, used to pin the vectorised ones.
 
@@ -31,4 +33,4 @@ Every function here has pins in ``tests/test_oracle_*.py`` (closed forms,
 invariants, library reductions, brute force); none is "parity unpinned".
 """
 
-from . import attention, brute, kvpack, reprojection, retrieval, stream  # noqa: F401
+from . import attention, brute, cache, kvpack, reprojection, retrieval, stream  # noqa: F401

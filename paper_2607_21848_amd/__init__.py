@@ -12,12 +12,17 @@ current HIP stream. The entry points mirror include/revisit.h:
                                   homography without depth (Sec. 4.3)
 * ``biased_chunk_attention``   -- attention with the Gaussian correspondence
                                   bias (Sec. 4.3, Eq. bias)
+* ``rotary_embed``             -- rotary positions of q and k (time, row, column)
+* ``attention_key_weight``     -- the weight of every cached key in the attention
+* ``select_kept``              -- which units of the cache to keep, by weight
+* ``compact_kv``               -- move of the kept units into a smaller cache
 
 Each accepts optional preallocated outputs (``out=``) and, where a kernel
 needs scratch memory, a preallocated ``workspace=`` (a uint8 GPU tensor of at
-least ``attention_workspace_size(...)`` / ``retrieve_workspace_size(...)``
-bytes), so a caller can run the path without allocating; without one the
-binding allocates the workspace with torch on the current stream.
+least ``attention_workspace_size(...)`` / ``retrieve_workspace_size(...)`` /
+``key_weight_workspace_size(...)`` / ``select_workspace_size(...)`` bytes), so
+a caller can run the path without allocating; without one the binding
+allocates the workspace with torch on the current stream.
 """
 
 from __future__ import annotations
@@ -31,7 +36,8 @@ from . import _lib
 from ._lib import BF16, F32, FP8_QK, MAX_K, RevisitError, last_error, lib, status_string  # noqa: F401
 
 __all__ = ["retrieve_chunks", "reproject_correspondence", "reproject_rotation", "biased_chunk_attention", "pack_retrieved_kv",
-           "pool_token_depth", "StreamDriver", "attention_workspace_size", "retrieve_workspace_size",
+           "pool_token_depth", "rotary_embed", "attention_key_weight", "select_kept", "compact_kv", "StreamDriver",
+           "attention_workspace_size", "retrieve_workspace_size", "key_weight_workspace_size", "select_workspace_size",
            "RevisitError", "lib"]
 
 
@@ -98,6 +104,13 @@ def attention_workspace_size(dtype: torch.dtype, Lq: int, Lk: int, H: int, D: in
                lib().rc_attention_workspace_size(_attn_dtype(dtype), int(Lq), int(Lk), int(H), int(D), int(key_parts),
                                                  ctypes.byref(n)))
     return int(n.value)
+
+
+def _attn_dtype_of(t: torch.Tensor, name: str) -> int:
+    try:
+        return _attn_dtype(t.dtype)
+    except TypeError:
+        raise TypeError(f"{name} must be bfloat16, float32 or float8_e4m3fn (got {t.dtype})") from None
 
 
 def _attn_dtype(dtype: torch.dtype) -> int:
@@ -360,6 +373,231 @@ def pool_token_depth(depth: torch.Tensor, p: int, out: Optional[torch.Tensor] = 
     _need(out, "out", torch.float32, (n, h, w), dev)
     _lib.check("pool_token_depth", lib().pool_token_depth(_ptr(depth), n, h, w, p, _ptr(out), _stream(dev)))
     return out
+
+
+def _call(dev: torch.device, name: str, *args):
+    """lib().<name>(*args, stream) on dev and its current stream, whichever device is current."""
+    if _current_device() == dev.index:
+        return _lib.check(name, getattr(lib(), name)(*args, _raw_stream(dev.index)))
+    with torch.cuda.device(dev):
+        return _lib.check(name, getattr(lib(), name)(*args, _raw_stream(dev.index)))
+
+
+def _rows(t: torch.Tensor, name: str, dtype: torch.dtype, n: int, D: int, device):
+    """A [n, H, D] tensor of whole rows (heads and elements contiguous, rows any distance apart); its H and row stride."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be a GPU tensor (got {t.device}); there is no CPU path")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
+    if t.dim() != 3 or t.shape[0] != n or t.shape[2] != D:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({n}, heads, {D})")
+    H = t.shape[1]
+    row, head, one = t.stride()
+    if n > 0 and (one != 1 or (H > 1 and head != D)):
+        raise ValueError(f"{name}: a token's heads must be contiguous (strides {t.stride()})")
+    return H, row if n > 1 else H * D
+
+
+def rotary_embed(q: torch.Tensor, k: Optional[torch.Tensor] = None, *, pairs: Sequence[int], theta: float, h: int = 0,
+                 w: int = 0, t0: int = 0, pos: Optional[torch.Tensor] = None, inverse: bool = False,
+                 out_dtype: Optional[torch.dtype] = None, fp8_scale: Sequence[float] = (1.0, 1.0), out=None):
+    """Rotary position embedding of q and k over time, row and column.
+
+    q [n, Hq, D], k None or [n, Hk, D] (bf16 or fp32; rows may lie apart, as views
+    of a packed projection do). pairs = (time, row, column) pairs of the bands.
+    Token r stands at (t0 + r // (h*w), r // w % h, r % w), or at pos[r] with pos
+    [n, 3] i32. inverse=True turns back, which is also the gradient with respect
+    to q and k. out_dtype: q's, or float8_e4m3fn for bf16 (values times
+    fp8_scale = (q's, k's)). out = (q_out, k_out), which may be q and k themselves
+    where the type stays. Returns (q_out, k_out); k_out is None without k."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a tensor [n, heads, D]")
+    dev, n, D = q.device, q.shape[0], q.shape[2]
+    if out is not None:
+        q_out, k_out = out
+        if (k is None) != (k_out is None):
+            raise ValueError("out k must be given exactly when k is")
+        if out_dtype is None:
+            out_dtype = q_out.dtype
+    odt = q.dtype if out_dtype is None else out_dtype
+    if q.dtype == torch.bfloat16 and odt == torch.float8_e4m3fn:
+        dt = FP8_QK
+    elif q.dtype == torch.bfloat16 and odt == q.dtype:
+        dt = BF16
+    elif q.dtype == torch.float32 and odt == q.dtype:
+        dt = F32
+    else:
+        raise TypeError(f"q must be bfloat16 or float32 with outputs of the same type, or bfloat16 with float8_e4m3fn "
+                        f"(got {q.dtype} and {odt})")
+    Hq, q_row = _rows(q, "q", q.dtype, n, D, dev)
+    Hk, k_row = _rows(k, "k", q.dtype, n, D, dev) if k is not None else (0, 0)
+    if out is None:
+        q_out = torch.empty((n, Hq, D), dtype=odt, device=dev)
+        k_out = torch.empty((n, Hk, D), dtype=odt, device=dev) if k is not None else None
+    Ho, qo_row = _rows(q_out, "out q", odt, n, D, dev)
+    if Ho != Hq:
+        raise ValueError(f"out q has {Ho} heads, expected {Hq}")
+    ko_row = 0
+    if k is not None:
+        Ho, ko_row = _rows(k_out, "out k", odt, n, D, dev)
+        if Ho != Hk:
+            raise ValueError(f"out k has {Ho} heads, expected {Hk}")
+    if pos is not None:
+        _need(pos, "pos", torch.int32, (n, 3), dev)
+    nt, ny, nx = pairs
+    qs, ks = fp8_scale
+    _call(dev, "rotary_embed", _ptr(q), q_row, _ptr(k), k_row, _ptr(q_out), qo_row, _ptr(k_out), ko_row, dt, n, Hq, Hk, D,
+          _ptr(pos), t0, h, w, nt, ny, nx, theta, 1 if inverse else 0, qs, ks)
+    return q_out, k_out
+
+
+def key_weight_workspace_size(dtype: torch.dtype, Lq: int, Lk: int, H: int, D: int, h: int, w: int, S: int = 0,
+                              query_parts: int = 0) -> int:
+    """Bytes of workspace attention_key_weight needs on the current device (S = 0 where lam is 0)."""
+    n = ctypes.c_size_t(0)
+    _lib.check("rc_key_weight_workspace_size",
+               lib().rc_key_weight_workspace_size(_attn_dtype(dtype), Lq, Lk, H, D, h, w, S, query_parts, ctypes.byref(n)))
+    return int(n.value)
+
+
+def attention_key_weight(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, kv_frame_slot: Optional[torch.Tensor],
+                         corr_uv: Optional[torch.Tensor], corr_idx: Optional[torch.Tensor], *, h: int, w: int,
+                         softmax_scale: float, lam: float, sigma: float, prev: Optional[torch.Tensor] = None,
+                         decay: float = 1.0, query_parts: int = 0, out: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Weight of every key in the attention: decay * prev + the sum over the
+    queries of exp(logit - lse), with the logits of biased_chunk_attention.
+
+    q [Lq,H,D], k [Lk,H,D], the slot table and correspondences as for
+    biased_chunk_attention, lse [H,Lq] f32 as it returns; prev None or [H,Lk]
+    f32. Queries whose lse is not finite add nothing. out may be prev. Returns
+    the weights [H,Lk] f32."""
+    dev = q.device
+    Lq, H, D = q.shape
+    Lk = k.shape[0]
+    dt = _attn_dtype(q.dtype)
+    _need(q, "q", q.dtype, None, dev)
+    _need(k, "k", q.dtype, (Lk, H, D), dev)
+    _need(lse, "lse", torch.float32, (H, Lq), dev)
+    if h < 1 or w < 1 or Lk % (h * w):
+        raise ValueError(f"Lk={Lk} is not a whole number of {h}x{w} frames")
+    S = 0
+    if corr_uv is not None:
+        S = corr_uv.shape[0]
+        _need(corr_uv, "corr_uv", torch.float32, (S, Lq, 2), dev)
+        _need(corr_idx, "corr_idx", torch.int32, (S, Lq), dev)
+        _need(kv_frame_slot, "kv_frame_slot", torch.int32, (Lk // (h * w),), dev)
+    if prev is not None:
+        _need(prev, "prev", torch.float32, (H, Lk), dev)
+    if out is None:
+        out = torch.empty((H, Lk), dtype=torch.float32, device=dev)
+    else:
+        _need(out, "out", torch.float32, (H, Lk), dev)
+    size = (q.dtype, Lq, Lk, H, D, h, w, S if lam != 0 else 0, query_parts)
+    if _current_device() == dev.index:
+        nbytes = key_weight_workspace_size(*size)
+    else:
+        with torch.cuda.device(dev):
+            nbytes = key_weight_workspace_size(*size)
+    ws = _workspace(nbytes, workspace, dev, "workspace")
+    _call(dev, "attention_key_weight", _ptr(q), _ptr(k), _ptr(lse), dt, Lq, Lk, H, D, h, w, _ptr(kv_frame_slot), _ptr(corr_uv),
+          _ptr(corr_idx), S, softmax_scale, lam, sigma, _ptr(prev), decay, _ptr(out), query_parts, _ptr(ws),
+          ws.numel() if ws is not None else 0)
+    return out
+
+
+def select_workspace_size(sets: int, heads: int, n_units: int, unit: int) -> int:
+    """Bytes of workspace select_kept needs."""
+    n = ctypes.c_size_t(0)
+    _lib.check("rc_select_workspace_size", lib().rc_select_workspace_size(sets, heads, n_units, unit, ctypes.byref(n)))
+    return int(n.value)
+
+
+def select_kept(weight: torch.Tensor, *, unit: int, keep: int, first: int = 0, last: int = 0, return_score: bool = True,
+                out=None, workspace: Optional[torch.Tensor] = None):
+    """Which units of a cache stay, by accumulated weight.
+
+    weight [sets, heads, n_units * unit] f32 (one set per choice: a layer with its
+    heads, or a layer's head); the first `first` and last `last` units stay in
+    any case, of the others those of largest summed weight, `keep` in all.
+    Returns (idx [sets, keep] i32 ascending, score [sets, keep] f32 or None)."""
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 3:
+        raise ValueError("weight must be a tensor [sets, heads, n_units * unit]")
+    dev = weight.device
+    sets, heads, cols = weight.shape
+    _need(weight, "weight", torch.float32, None, dev)
+    if unit < 1 or cols % unit:
+        raise ValueError(f"{cols} weights are not a whole number of units of {unit}")
+    if keep < 0:
+        raise ValueError(f"keep={keep}")
+    n_units = cols // unit
+    if out is None:
+        idx = torch.empty((sets, keep), dtype=torch.int32, device=dev)
+        score = torch.empty((sets, keep), dtype=torch.float32, device=dev) if return_score else None
+    else:
+        idx, score = out
+        _need(idx, "out idx", torch.int32, (sets, keep), dev)
+        if score is not None:
+            _need(score, "out score", torch.float32, (sets, keep), dev)
+    ws = _workspace(select_workspace_size(sets, heads, n_units, unit), workspace, dev, "workspace")
+    _call(dev, "select_kept", _ptr(weight), sets, heads, n_units, unit, keep, first, last, _ptr(idx), _ptr(score), _ptr(ws),
+          ws.numel() if ws is not None else 0)
+    return idx, score
+
+
+def compact_kv(src_k: torch.Tensor, src_v: torch.Tensor, sel: torch.Tensor, dst_k: torch.Tensor, dst_v: torch.Tensor, *,
+               unit: int, dst_row0: int = 0, weight: Optional[torch.Tensor] = None, out_weight: Optional[torch.Tensor] = None,
+               src_pos: Optional[torch.Tensor] = None, dst_pos: int = 0, frames_per_unit: int = 0, rope_t_pairs: int = 0,
+               rope_theta: float = 0.0) -> None:
+    """Move the kept units of a cache into a smaller one, in place of dst's rows.
+
+    src_k, src_v [L, rows, H, D], dst_k, dst_v [L, dst_rows, H, D] (bf16 or fp32,
+    or fp8 keys with bf16 values); sel [L, 1 or H, keep] i32 units of `unit` rows
+    (entries outside the source leave their rows as they are), going to rows
+    dst_row0 + i*unit. weight [L, H, >= rows of the units] and out_weight [L, H, >=
+    dst_row0 + keep*unit] f32 move alike. With rope_t_pairs > 0 keys are turned from
+    their unit's frame position (src_pos [units] i32, else u*frames_per_unit) to
+    dst_pos + i*frames_per_unit."""
+    for t, name in ((src_k, "src_k"), (dst_k, "dst_k")):
+        if not isinstance(t, torch.Tensor) or t.dim() != 4:
+            raise ValueError(f"{name} must be a tensor [layers, rows, heads, D]")
+    dev = dst_k.device
+    L, rows, H, D = src_k.shape
+    dst_rows = dst_k.shape[1]
+    dt = _attn_dtype_of(src_k, "src_k")
+    vdt = torch.bfloat16 if dt == FP8_QK else src_k.dtype
+    _need(src_k, "src_k", src_k.dtype, None, dev)
+    _need(src_v, "src_v", vdt, (L, rows, H, D), dev)
+    _need(dst_k, "dst_k", src_k.dtype, (L, dst_rows, H, D), dev)
+    _need(dst_v, "dst_v", vdt, (L, dst_rows, H, D), dev)
+    _need(sel, "sel", torch.int32, None, dev)
+    if sel.dim() != 3 or sel.shape[0] != L or sel.shape[1] not in (1, H):
+        raise ValueError(f"sel has shape {tuple(sel.shape)}, expected ({L}, 1 or {H}, keep)")
+    if unit < 1:
+        raise ValueError(f"unit={unit}")
+    n_units = rows // unit
+    if src_pos is not None:
+        _need(src_pos, "src_pos", torch.int32, None, dev)
+        if src_pos.dim() != 1 or src_pos.shape[0] > n_units:
+            raise ValueError(f"src_pos has shape {tuple(src_pos.shape)}, expected (units,), at most {n_units}")
+        n_units = src_pos.shape[0]
+    cols = dst_cols = 0
+    if weight is not None or out_weight is not None:
+        for t, name in ((weight, "weight"), (out_weight, "out_weight")):
+            if t is None:
+                raise ValueError("weight and out_weight are given together or not at all")
+            _need(t, name, torch.float32, None, dev)
+            if t.dim() != 3 or t.shape[0] != L or t.shape[1] != H:
+                raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({L}, {H}, tokens)")
+        cols, dst_cols = weight.shape[2], out_weight.shape[2]
+        n_units = min(n_units, cols // unit)
+    _call(dev, "compact_kv", _ptr(src_k), _ptr(src_v), rows, _ptr(sel), sel.shape[1], sel.shape[2], unit, n_units, _ptr(dst_k),
+          _ptr(dst_v), dst_rows, dst_row0, _ptr(weight), cols, _ptr(out_weight), dst_cols, L, dt, H, D, _ptr(src_pos), dst_pos,
+          frames_per_unit, rope_t_pairs, rope_theta)
 
 
 class StreamDriver:

@@ -20,12 +20,14 @@ EXPORTED = ("rc_status_string", "rc_last_error", "retrieve_chunks", "reproject_c
             "reproject_rotation", "biased_chunk_attention", "biased_chunk_attention_noalloc", "rc_retrieve_workspace_size",
             "rc_attention_workspace_size",
             "pack_retrieved_kv", "pool_token_depth", "rc_stream_create", "rc_stream_step", "rc_stream_view",
-            "rc_stream_destroy")
+            "rc_stream_destroy", "rotary_embed", "attention_key_weight", "rc_key_weight_workspace_size", "select_kept",
+            "rc_select_workspace_size", "compact_kv")
 
 _p = ctypes.c_void_p
 _i = ctypes.c_int32
 _f = ctypes.c_float
 _z = ctypes.c_size_t
+_l = ctypes.c_int64
 
 
 class StreamConfig(ctypes.Structure):
@@ -93,6 +95,21 @@ def lib() -> ctypes.CDLL:
         L.rc_stream_view.argtypes = [_p, ctypes.POINTER(StreamState)]
         L.rc_stream_destroy.restype = ctypes.c_int
         L.rc_stream_destroy.argtypes = [_p]
+        L.rotary_embed.restype = ctypes.c_int
+        L.rotary_embed.argtypes = [_p, _l, _p, _l, _p, _l, _p, _l, _i, _i, _i, _i, _i, _p, _i, _i, _i, _i, _i, _i, _f, _i,
+                                   _f, _f, _p]
+        L.attention_key_weight.restype = ctypes.c_int
+        L.attention_key_weight.argtypes = [_p, _p, _p, _i, _i, _i, _i, _i, _i, _i, _p, _p, _p, _i, _f, _f, _f, _p, _f, _p,
+                                           _i, _p, _z, _p]
+        L.rc_key_weight_workspace_size.restype = ctypes.c_int
+        L.rc_key_weight_workspace_size.argtypes = [_i, _i, _i, _i, _i, _i, _i, _i, _i, ctypes.POINTER(ctypes.c_size_t)]
+        L.select_kept.restype = ctypes.c_int
+        L.select_kept.argtypes = [_p, _i, _i, _i, _i, _i, _i, _i, _p, _p, _p, _z, _p]
+        L.rc_select_workspace_size.restype = ctypes.c_int
+        L.rc_select_workspace_size.argtypes = [_i, _i, _i, _i, ctypes.POINTER(ctypes.c_size_t)]
+        L.compact_kv.restype = ctypes.c_int
+        L.compact_kv.argtypes = [_p, _p, _i, _p, _i, _i, _i, _i, _p, _p, _i, _i, _p, _i, _p, _i, _i, _i, _i, _i, _p, _i, _i,
+                                 _i, _f, _p]
         _LIB = L
     return _LIB
 

@@ -577,3 +577,338 @@ int pool_token_depth(const float* depth, int32_t n_frames, int32_t h, int32_t w,
 }
 
 }  // extern "C"
+
+namespace {
+
+// Quarter turns per position of a band of n pairs: theta^(-j / n) radians.
+void band_quarters(double theta, int n, double* out) {
+    for (int j = 0; j < n; ++j) out[j] = pow(theta, -((double)j / (double)n)) * (2.0 / M_PI);
+}
+
+bool overlap(const void* a, double a_bytes, const void* b, double b_bytes) {
+    const double x = (double)(uintptr_t)a, y = (double)(uintptr_t)b;
+    return x < y + b_bytes && y < x + a_bytes;
+}
+
+}  // namespace
+
+extern "C" {
+
+int rotary_embed(const void* q, int64_t q_row, const void* k, int64_t k_row, void* q_out, int64_t q_out_row, void* k_out,
+                 int64_t k_out_row, int32_t dtype, int32_t n_tokens, int32_t Hq, int32_t Hk, int32_t D, const int32_t* pos,
+                 int32_t t0, int32_t h, int32_t w, int32_t pairs_t, int32_t pairs_y, int32_t pairs_x, float theta,
+                 int32_t inverse, float q_scale, float k_scale, hipStream_t stream) {
+    const char* fn = "rotary_embed";
+    if (dtype != REVISIT_BF16 && dtype != REVISIT_F32 && dtype != REVISIT_FP8_QK)
+        return fail(REVISIT_ERR_UNSUPPORTED, "%s: dtype %d not supported", fn, dtype);
+    if (D < 8 || D > 512 || D % 8 != 0)
+        return fail(REVISIT_ERR_UNSUPPORTED, "%s: D=%d (need a multiple of 8 in [8, 512])", fn, D);
+    if (n_tokens < 0 || Hq < 1 || Hq > 65535 || (k && (Hk < 1 || Hk > 65535)))
+        return fail(REVISIT_ERR_SHAPE, "%s: need n_tokens >= 0 and 1 to 65535 heads", fn);
+    if (pairs_t < 0 || pairs_y < 0 || pairs_x < 0 || (int64_t)pairs_t + pairs_y + pairs_x > D / 2)
+        return fail(REVISIT_ERR_PARAM, "%s: bands of %d + %d + %d pairs in a head of %d", fn, pairs_t, pairs_y, pairs_x, D / 2);
+    if (!(finite(theta) && theta > 0.0f)) return fail(REVISIT_ERR_PARAM, "%s: theta must be finite and > 0", fn);
+    if (inverse != 0 && inverse != 1) return fail(REVISIT_ERR_PARAM, "%s: inverse=%d (0 or 1)", fn, inverse);
+    const bool fp8 = dtype == REVISIT_FP8_QK;
+    if (fp8 && !(finite(q_scale) && q_scale > 0.0f && finite(k_scale) && k_scale > 0.0f))
+        return fail(REVISIT_ERR_PARAM, "%s: q_scale and k_scale must be finite and > 0", fn);
+    if (!pos && (h < 1 || w < 1 || (int64_t)h * w > INT32_MAX))
+        return fail(REVISIT_ERR_SHAPE, "%s: without positions the token grid is needed: h, w >= 1", fn);
+    const int esize = dtype == REVISIT_F32 ? 4 : 2, osize = fp8 ? 1 : esize;
+    revisit::RotaryArgs a{};
+    const void* x[2] = {q, k};
+    void* o[2] = {q_out, k_out};
+    const int64_t x_row[2] = {q_row, k_row}, o_row[2] = {q_out_row, k_out_row};
+    const int32_t heads[2] = {Hq, Hk};
+    for (int i = 0; i < 2; ++i) {
+        if (i == 1 && !k) break;
+        const int64_t row = (int64_t)heads[i] * D;
+        if ((double)n_tokens * (double)row > (double)kMaxElems) return fail(REVISIT_ERR_SHAPE, "%s: problem too large", fn);
+        const int64_t most = kMaxElems / (n_tokens > 1 ? n_tokens : 1);
+        if (x_row[i] < row || o_row[i] < row || x_row[i] > most || o_row[i] > most)
+            return fail(REVISIT_ERR_SHAPE, "%s: a row stride is below the row's %lld elements or too large", fn, (long long)row);
+        if (x_row[i] * esize % 16 != 0 || o_row[i] * osize % (16 * osize / esize) != 0)
+            return fail(REVISIT_ERR_SHAPE, "%s: rows of q and k must start on 16 bytes (on 8 for fp8 output)", fn);
+    }
+    if (n_tokens == 0) return REVISIT_OK;
+    if (!q || !q_out || (k && !k_out)) return fail(REVISIT_ERR_NULL, "%s: q and q_out (and k_out with k) are required", fn);
+    if (!aligned(pos, 4)) return fail(REVISIT_ERR_SHAPE, "%s: pos must be 4-byte aligned", fn);
+    for (int i = 0; i < 2; ++i) {
+        if (i == 1 && !k) break;
+        if (!aligned(x[i], 16) || !aligned(o[i], fp8 ? 8 : 16))
+            return fail(REVISIT_ERR_SHAPE, "%s: q and k must be 16-byte aligned, outputs too (8-byte for fp8)", fn);
+        const int64_t row = (int64_t)heads[i] * D;
+        revisit::RotaryTensor& t = a.t[i];
+        t.x = x[i];
+        t.o = o[i];
+        t.x_row_bytes = x_row[i] * esize;
+        t.o_row_bytes = o_row[i] * osize;
+        t.H = heads[i];
+        t.scale = i ? k_scale : q_scale;
+        t.inv_row_vecs = 16.0 / ((double)row * esize);
+        // in place only element by element
+        if (x[i] == o[i] ? (fp8 || x_row[i] != o_row[i]) : false)
+            return fail(REVISIT_ERR_SHAPE, "%s: an output in its input's place needs the same type and rows", fn);
+    }
+    a.n_tokens = n_tokens;
+    a.D = D;
+    a.esize = esize;
+    a.fp8_out = fp8;
+    a.pos = pos;
+    a.t0 = t0;
+    a.hw = pos ? 1 : h * w;
+    a.w = pos ? 1 : w;
+    a.n_t = pairs_t;
+    a.n_y = pairs_y;
+    a.n_x = pairs_x;
+    a.inverse = inverse;
+    const int pairs = pairs_t + pairs_y + pairs_x;
+    a.inv_pairs = pairs > 0 ? 1.0f / (float)pairs : 0.0f;
+    a.inv_hw = 1.0 / a.hw;
+    a.inv_w = 1.0 / a.w;
+    if (revisit::rotary_blocks(a) > INT32_MAX) return fail(REVISIT_ERR_SHAPE, "%s: problem too large", fn);
+    revisit::RotaryFreq f;
+    band_quarters((double)theta, pairs_t, f.quarter);
+    band_quarters((double)theta, pairs_y, f.quarter + pairs_t);
+    band_quarters((double)theta, pairs_x, f.quarter + pairs_t + pairs_y);
+    return launched(revisit::launch_rotary(a, f, stream), fn);
+}
+
+}  // extern "C"
+
+namespace {
+
+// Shape, type and part checks shared by attention_key_weight and its workspace
+// query; fills the plan of `a` and its parts.
+int prepare_key_weight(const char* fn, int32_t dtype, int32_t Lq, int32_t Lk, int32_t H, int32_t D, int32_t h, int32_t w, int32_t S,
+                       int32_t query_parts, revisit::KeyWeightArgs& a, size_t* bytes) {
+    *bytes = 0;
+    const int st = check_attention_shape(fn, dtype, Lq, Lk, H, D, 0);
+    if (st != REVISIT_OK) return st;
+    if (h < 1 || w < 1 || S < 0) return fail(REVISIT_ERR_SHAPE, "%s: need h, w >= 1, S >= 0", fn);
+    const int64_t hw = (int64_t)h * w;
+    if (Lk % hw != 0) return fail(REVISIT_ERR_SHAPE, "%s: Lk=%d not a multiple of h*w=%lld", fn, Lk, (long long)hw);
+    if (Lk / hw > kMaxFrames) return fail(REVISIT_ERR_SHAPE, "%s: more than %d KV frames", fn, kMaxFrames);
+    if (S > 0 && dtype != REVISIT_F32 && (h > kMaxGridSide || w > kMaxGridSide))
+        return fail(REVISIT_ERR_SHAPE, "%s: bf16 / fp8 with bias needs h, w <= %d (got %d x %d)", fn, kMaxGridSide, h, w);
+    if (query_parts < 0 || query_parts > revisit::kKeyWeightMaxParts)
+        return fail(REVISIT_ERR_PARAM, "%s: query_parts=%d outside [0, %d]", fn, query_parts, revisit::kKeyWeightMaxParts);
+    a.type = dtype;
+    a.Lq = Lq;
+    a.Lk = Lk;
+    a.H = H;
+    a.D = D;
+    a.hw = (int32_t)hw;
+    a.h = h;
+    a.w = w;
+    a.S = S;
+    revisit::key_weight_plan(a);
+    a.parts = revisit::kKeyWeightMaxParts;
+    if (revisit::key_weight_items(a) > INT32_MAX - revisit::kXcds) return fail(REVISIT_ERR_SHAPE, "%s: problem too large", fn);
+    a.parts = query_parts;
+    if (a.parts == 0) {
+        int cus = 0;
+        const hipError_t e = device_compute_units(&cus);
+        if (e != hipSuccess) return fail(REVISIT_ERR_LAUNCH, "%s: device query failed: %s", fn, hipGetErrorString(e));
+        a.parts = revisit::key_weight_parts(a, cus);
+    }
+    const int32_t tiles = (int32_t)(((int64_t)Lq + 31) / 32);
+    if (a.parts > tiles) a.parts = tiles > 1 ? tiles : 1;  // at least one tile of 32 queries per part
+    *bytes = a.parts > 1 ? (size_t)a.parts * H * Lk * sizeof(float) : 0;
+    return REVISIT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int rc_key_weight_workspace_size(int32_t dtype, int32_t Lq, int32_t Lk, int32_t H, int32_t D, int32_t h, int32_t w, int32_t S,
+                                 int32_t query_parts, size_t* bytes) {
+    if (!bytes) return fail(REVISIT_ERR_NULL, "rc_key_weight_workspace_size: bytes is NULL");
+    revisit::KeyWeightArgs a{};
+    return prepare_key_weight("rc_key_weight_workspace_size", dtype, Lq, Lk, H, D, h, w, S, query_parts, a, bytes);
+}
+
+int attention_key_weight(const void* q, const void* k, const float* lse, int32_t dtype, int32_t Lq, int32_t Lk, int32_t H, int32_t D,
+                         int32_t h, int32_t w, const int32_t* kv_frame_slot, const float* corr_uv, const int32_t* corr_idx, int32_t S,
+                         float softmax_scale, float lambda, float sigma, const float* prev, float decay, float* out,
+                         int32_t query_parts, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    const char* fn = "attention_key_weight";
+    if (!(finite(softmax_scale) && softmax_scale > 0.0f))
+        return fail(REVISIT_ERR_PARAM, "%s: softmax_scale must be finite and > 0", fn);
+    if (!(finite(sigma) && sigma > 0.0f)) return fail(REVISIT_ERR_PARAM, "%s: sigma must be finite and > 0", fn);
+    if (!finite(lambda)) return fail(REVISIT_ERR_PARAM, "%s: lambda must be finite", fn);
+    if (!finite(decay)) return fail(REVISIT_ERR_PARAM, "%s: decay must be finite", fn);
+    const float gamma = lambda / (2.0f * sigma * sigma * softmax_scale), gamma2 = lambda / (2.0f * sigma * sigma);
+    if (!finite(gamma) || !finite(gamma2)) return fail(REVISIT_ERR_PARAM, "%s: lambda / (2 sigma^2 scale) overflows", fn);
+    revisit::KeyWeightArgs a{};
+    size_t need = 0;
+    const bool bias = S > 0 && lambda != 0.0f;
+    int st = prepare_key_weight(fn, dtype, Lq, Lk, H, D, h, w, S < 0 ? S : (bias ? S : 0), query_parts, a, &need);
+    if (st != REVISIT_OK) return st;
+    if (bias && (double)S * Lq > (double)kMaxElems) return fail(REVISIT_ERR_SHAPE, "%s: problem too large", fn);
+    if (!k || !out || (Lq > 0 && (!q || !lse))) return fail(REVISIT_ERR_NULL, "%s: q, k, lse and out are required", fn);
+    if (bias && (!kv_frame_slot || !corr_uv || !corr_idx) && Lq > 0)
+        return fail(REVISIT_ERR_NULL, "%s: slot table and correspondence map are required when S > 0", fn);
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(lse, 4) || !aligned(prev, 4) || !aligned(out, 4) ||
+        (bias && (!aligned(corr_uv, 8) || !aligned(corr_idx, 4) || !aligned(kv_frame_slot, 4))))
+        return fail(REVISIT_ERR_SHAPE, "%s: q and k must be 16-byte aligned, corr_uv 8-byte, arrays of words 4-byte", fn);
+    st = check_workspace(fn, need, workspace, workspace_bytes);
+    if (st != REVISIT_OK) return st;
+    if (Lq == 0) {  // no query: nothing of the bias is read
+        a.S = 0;
+        revisit::key_weight_plan(a);
+    }
+    a.q = q;
+    a.k = k;
+    a.lse = lse;
+    a.prev = prev;
+    a.out = out;
+    a.partial = static_cast<float*>(workspace);
+    a.slot = kv_frame_slot;
+    a.corr_uv = corr_uv;
+    a.corr_idx = corr_idx;
+    a.c_log2 = (float)((double)softmax_scale * M_LOG2E);
+    a.gamma2 = (float)((double)gamma2 * M_LOG2E);
+    a.decay = decay;
+    return launched(revisit::launch_key_weight(a, stream), fn);
+}
+
+}  // extern "C"
+
+namespace {
+
+int prepare_select(const char* fn, int32_t sets, int32_t heads, int32_t n_units, int32_t unit, revisit::SelectArgs& a, size_t* bytes) {
+    *bytes = 0;
+    if (sets < 0 || heads < 1 || n_units < 0 || unit < 1)
+        return fail(REVISIT_ERR_SHAPE, "%s: need sets, n_units >= 0 and heads, unit >= 1", fn);
+    if (n_units > (1 << 30) || (int64_t)n_units * unit > INT32_MAX || sets > (1 << 21) ||
+        (int64_t)sets * n_units > INT32_MAX || (double)sets * heads * n_units * unit > (double)kMaxElems)
+        return fail(REVISIT_ERR_SHAPE, "%s: problem too large", fn);
+    a.sets = sets;
+    a.heads = heads;
+    a.n_units = n_units;
+    a.unit = unit;
+    *bytes = revisit::select_workspace_bytes(a);
+    return REVISIT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int rc_select_workspace_size(int32_t sets, int32_t heads, int32_t n_units, int32_t unit, size_t* bytes) {
+    if (!bytes) return fail(REVISIT_ERR_NULL, "rc_select_workspace_size: bytes is NULL");
+    revisit::SelectArgs a{};
+    return prepare_select("rc_select_workspace_size", sets, heads, n_units, unit, a, bytes);
+}
+
+int select_kept(const float* weight, int32_t sets, int32_t heads, int32_t n_units, int32_t unit, int32_t keep, int32_t first,
+                int32_t last, int32_t* out_idx, float* out_score, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    const char* fn = "select_kept";
+    revisit::SelectArgs a{};
+    size_t need = 0;
+    int st = prepare_select(fn, sets, heads, n_units, unit, a, &need);
+    if (st != REVISIT_OK) return st;
+    if (first < 0 || last < 0 || (int64_t)first + last > keep || keep > n_units)
+        return fail(REVISIT_ERR_PARAM, "%s: need first, last >= 0 and first + last <= keep <= n_units (got %d, %d, %d, %d)", fn, first,
+                    last, keep, n_units);
+    if (sets == 0 || keep == 0) return REVISIT_OK;
+    if (!weight || !out_idx) return fail(REVISIT_ERR_NULL, "%s: weight and out_idx are required", fn);
+    if (!aligned(weight, 4) || !aligned(out_idx, 4) || !aligned(out_score, 4))
+        return fail(REVISIT_ERR_SHAPE, "%s: arrays must be 4-byte aligned", fn);
+    st = check_workspace(fn, need, workspace, workspace_bytes);
+    if (st != REVISIT_OK) return st;
+    a.weight = weight;
+    a.keep = keep;
+    a.first = first;
+    a.last = last;
+    a.out_idx = out_idx;
+    a.out_score = out_score;
+    a.unit_score = static_cast<float*>(workspace);
+    return launched(revisit::launch_select(a, stream), fn);
+}
+
+int compact_kv(const void* src_k, const void* src_v, int32_t src_rows, const int32_t* sel, int32_t sel_heads, int32_t keep,
+               int32_t unit, int32_t n_units, void* dst_k, void* dst_v, int32_t dst_rows, int32_t dst_row0, const float* src_weight,
+               int32_t src_weight_cols, float* dst_weight, int32_t dst_weight_cols, int32_t n_layers, int32_t dtype, int32_t H,
+               int32_t D, const int32_t* src_pos, int32_t dst_pos, int32_t frames_per_unit, int32_t rope_t_pairs, float rope_theta,
+               hipStream_t stream) {
+    const char* fn = "compact_kv";
+    if (dtype != REVISIT_BF16 && dtype != REVISIT_F32 && dtype != REVISIT_FP8_QK)
+        return fail(REVISIT_ERR_UNSUPPORTED, "%s: dtype %d not supported", fn, dtype);
+    const bool fp8 = dtype == REVISIT_FP8_QK;
+    const int step = fp8 ? 16 : 8;
+    if (D < step || D > 512 || D % step != 0)
+        return fail(REVISIT_ERR_UNSUPPORTED, "%s: D=%d (need a multiple of %d up to 512)", fn, D, step);
+    if (n_layers < 0 || keep < 0 || n_units < 0 || unit < 1 || H < 1 || H > 65535 || src_rows < 0 || dst_rows < 0 || dst_row0 < 0)
+        return fail(REVISIT_ERR_SHAPE, "%s: need n_layers, keep, n_units, rows >= 0, unit >= 1 and 1 to 65535 heads", fn);
+    if (sel_heads != 1 && sel_heads != H) return fail(REVISIT_ERR_SHAPE, "%s: a selection for 1 or all %d heads (got %d)", fn, H, sel_heads);
+    if ((int64_t)n_units * unit > src_rows)
+        return fail(REVISIT_ERR_SHAPE, "%s: %d units of %d rows exceed src_rows=%d", fn, n_units, unit, src_rows);
+    if ((int64_t)dst_row0 + (int64_t)keep * unit > dst_rows)
+        return fail(REVISIT_ERR_SHAPE, "%s: %d units of %d rows from row %d exceed dst_rows=%d", fn, keep, unit, dst_row0, dst_rows);
+    const double row = (double)H * D;
+    if ((double)n_layers * src_rows * row > (double)kMaxElems || (double)n_layers * dst_rows * row > (double)kMaxElems ||
+        (double)n_layers * sel_heads * keep > (double)kMaxElems)
+        return fail(REVISIT_ERR_SHAPE, "%s: problem too large", fn);
+    if (rope_t_pairs < 0 || rope_t_pairs > D / 2) return fail(REVISIT_ERR_PARAM, "%s: rope_t_pairs=%d outside [0, D/2]", fn, rope_t_pairs);
+    if (rope_t_pairs > 0) {
+        if (fp8) return fail(REVISIT_ERR_UNSUPPORTED, "%s: fp8 keys are not turned (they would be rounded to 8 bits a second time)", fn);
+        if (!(finite(rope_theta) && rope_theta > 0.0f)) return fail(REVISIT_ERR_PARAM, "%s: rope_theta must be finite and > 0", fn);
+        if (frames_per_unit < 0) return fail(REVISIT_ERR_PARAM, "%s: frames_per_unit=%d", fn, frames_per_unit);
+    }
+    if ((src_weight == nullptr) != (dst_weight == nullptr))
+        return fail(REVISIT_ERR_NULL, "%s: src_weight and dst_weight are given together or not at all", fn);
+    if (src_weight) {
+        if (src_weight_cols < (int64_t)n_units * unit || dst_weight_cols < (int64_t)dst_row0 + (int64_t)keep * unit)
+            return fail(REVISIT_ERR_SHAPE, "%s: weight rows are shorter than the units' rows", fn);
+        if ((double)n_layers * H * src_weight_cols > (double)kMaxElems || (double)n_layers * H * dst_weight_cols > (double)kMaxElems)
+            return fail(REVISIT_ERR_SHAPE, "%s: problem too large", fn);
+    }
+    if (n_layers == 0 || keep == 0) return REVISIT_OK;
+    if (!sel || !dst_k || !dst_v || (n_units > 0 && (!src_k || !src_v)))
+        return fail(REVISIT_ERR_NULL, "%s: required pointer is NULL", fn);
+    if (!aligned(src_k, 16) || !aligned(src_v, 16) || !aligned(dst_k, 16) || !aligned(dst_v, 16) || !aligned(sel, 4) ||
+        !aligned(src_pos, 4) || !aligned(src_weight, 4) || !aligned(dst_weight, 4))
+        return fail(REVISIT_ERR_SHAPE, "%s: caches must be 16-byte aligned, arrays of words 4-byte", fn);
+    revisit::CompactArgs a{};
+    a.src_k = src_k;
+    a.src_v = src_v;
+    a.dst_k = dst_k;
+    a.dst_v = dst_v;
+    a.sel = sel;
+    a.n_layers = n_layers;
+    a.sel_heads = sel_heads;
+    a.keep = keep;
+    a.unit = unit;
+    a.n_units = n_units;
+    a.H = H;
+    a.D = D;
+    a.src_rows = src_rows;
+    a.dst_rows = dst_rows;
+    a.dst_row0 = dst_row0;
+    a.k_bytes = fp8 ? 1 : (dtype == REVISIT_BF16 ? 2 : 4);
+    a.v_bytes = dtype == REVISIT_F32 ? 4 : 2;
+    a.src_w = src_weight;
+    a.dst_w = dst_weight;
+    a.src_w_cols = src_weight_cols;
+    a.dst_w_cols = dst_weight_cols;
+    a.src_pos = src_pos;
+    a.dst_pos = dst_pos;
+    a.step = frames_per_unit;
+    a.n_t = rope_t_pairs;
+    a.inv_unit = 1.0 / unit;
+    a.inv_kept = 1.0 / ((double)keep * unit);
+    // units move within no cache: a vector could be overwritten before another block has read it
+    const double src_bytes = (double)n_layers * src_rows * row, dst_bytes = (double)n_layers * dst_rows * row;
+    if (overlap(src_k, src_bytes * a.k_bytes, dst_k, dst_bytes * a.k_bytes) || overlap(src_v, src_bytes * a.v_bytes, dst_v, dst_bytes * a.v_bytes) ||
+        (src_weight && overlap(src_weight, 4.0 * n_layers * H * src_weight_cols, dst_weight, 4.0 * n_layers * H * dst_weight_cols)))
+        return fail(REVISIT_ERR_SHAPE, "%s: source and destination overlap", fn);
+    if (revisit::compact_blocks(a) > (double)INT32_MAX) return fail(REVISIT_ERR_SHAPE, "%s: problem too large", fn);
+    revisit::CompactFreq f;
+    band_quarters((double)rope_theta, rope_t_pairs, f.quarter);
+    return launched(revisit::launch_compact(a, f, stream), fn);
+}
+
+}  // extern "C"

@@ -227,6 +227,96 @@ hipError_t launch_stream_slots(const StreamSlotsArgs& a, hipStream_t stream);
 hipError_t launch_pool_depth(const float* depth, int64_t n_tokens, int32_t h, int32_t w, int32_t p, float* out,
                              hipStream_t stream);
 
+// Rotary position embedding (rotary.hip) of q (t[0]) and k (t[1], x NULL: none).
+struct RotaryTensor {
+    const void* x;
+    void* o;
+    int64_t x_row_bytes, o_row_bytes;
+    int32_t H;
+    float scale;          // fp8 output: the value rounded is the embedded one times this
+    double inv_row_vecs;  // 1 / 16-byte vectors of x per token
+};
+struct RotaryArgs {
+    RotaryTensor t[2];
+    int32_t n_tokens, D;
+    int32_t esize, fp8_out;  // bytes of an input element; output in e4m3
+    const int32_t* pos;      // nullable [n_tokens][3]: time, row, column
+    int32_t t0, hw, w;       // pos NULL: the grid's tokens in order
+    int32_t n_t, n_y, n_x;   // pairs of each band
+    int32_t inverse;
+    float inv_pairs;         // 1 / (n_t + n_y + n_x)
+    double inv_hw, inv_w;
+};
+constexpr int kRotaryMaxPairs = 256;  // D <= 512
+struct RotaryFreq {
+    double quarter[kRotaryMaxPairs];  // quarter turns per position, of every pair
+};
+int64_t rotary_blocks(const RotaryArgs& a);
+hipError_t launch_rotary(const RotaryArgs& a, const RotaryFreq& f, hipStream_t stream);
+
+// Attention weight of every key (keyweight.hip). key_weight_plan fills
+// the block counts from the shape.
+struct KeyWeightArgs {
+    const void* q;
+    const void* k;
+    const float* lse;        // [H][Lq]
+    const float* prev;       // nullable [H][Lk]
+    float* out;              // [H][Lk]
+    float* partial;          // [parts][H][Lk] when parts > 1
+    int32_t type;            // REVISIT_BF16 / F32 / FP8_QK
+    int32_t Lq, Lk, H, D;
+    int32_t hw, h, w;
+    const int32_t* slot;
+    const float* corr_uv;
+    const int32_t* corr_idx;
+    int32_t S;               // 0 = bias off
+    float c_log2, gamma2;    // softmax_scale log2 e; lambda log2 e / (2 sigma^2)
+    float decay;
+    int32_t parts;           // query parts
+    int32_t frame_blocks, n_blocks;  // key blocks per frame and per head
+};
+constexpr int32_t kKeyWeightMaxParts = 64;
+void key_weight_plan(KeyWeightArgs& a);
+int64_t key_weight_items(const KeyWeightArgs& a);
+int32_t key_weight_parts(const KeyWeightArgs& a, int32_t cus);
+hipError_t launch_key_weight(const KeyWeightArgs& a, hipStream_t stream);
+
+// The choice of kept units (select.hip).
+struct SelectArgs {
+    const float* weight;  // [sets][heads][n_units unit]
+    int32_t sets, heads, unit, n_units;
+    int32_t keep, first, last;
+    int32_t* out_idx;     // [sets][keep]
+    float* out_score;     // nullable [sets][keep]
+    float* unit_score;    // [sets][n_units], workspace (select_workspace_bytes)
+};
+size_t select_workspace_bytes(const SelectArgs& a);
+hipError_t launch_select(const SelectArgs& a, hipStream_t stream);
+
+// The move of kept units into a smaller cache (compact.hip).
+struct CompactArgs {
+    const void* src_k;
+    const void* src_v;
+    void* dst_k;
+    void* dst_v;
+    const int32_t* sel;   // [n_layers][sel_heads][keep]
+    int32_t n_layers, sel_heads, keep, unit, n_units, H, D;
+    int32_t src_rows, dst_rows, dst_row0;
+    int32_t k_bytes, v_bytes;  // of an element
+    const float* src_w;   // nullable [n_layers][H][src_w_cols]
+    float* dst_w;         // [n_layers][H][dst_w_cols]
+    int32_t src_w_cols, dst_w_cols;
+    const int32_t* src_pos;  // nullable [n_units]: unit u at frame position step u
+    int32_t dst_pos, step;
+    int32_t n_t;          // temporal pairs to turn, 0: none
+    double inv_unit, inv_kept;  // 1 / unit, 1 / (keep unit)
+};
+struct CompactFreq {
+    double quarter[kRotaryMaxPairs];  // quarter turns per frame position, of every temporal pair
+};
+double compact_blocks(const CompactArgs& a);
+hipError_t launch_compact(const CompactArgs& a, const CompactFreq& f, hipStream_t stream);
+
 // Sets the calling thread's last-error string and returns status (capi.cpp).
 int fail_status(int status, const char* fmt, ...);
 

@@ -1,0 +1,175 @@
+"""attention_key_weight against its fp64 oracle: types, lengths from one query and one key on, frames that end inside a
+tile, biased and unbiased frames, queries without an LSE, the query parts.
+
+Tolerance, per logit. The dot product is a sum of D products in fp32: within (D + 4) 2^-24 of scale |q| . |k|. The bias
+is within 4 * 2^-24 of itself where it is evaluated directly (fp32) and within 32 * 2^-24 of lam (h^2 + w^2) / (4 sigma^2)
+where it is a sum of products on the matrix cores (bf16, fp8; correspondences on the grid). LSE, its multiple and the sum of
+the three are rounded: 4 * 2^-24 of |A| + 2 |LSE|. A weight is then within that, relatively, plus 2^-22 for the
+exponential, and the sum of n weights adds n/16 + 20 roundings (16 queries of a tile first). A weight below fp32's normal
+range (2^-126; the bias of a far key makes such) may be taken as 0."""
+
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_21848_amd as rv
+from oracle import cache as OC
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+
+
+def _case(seed, dtype, Lq, nf, h, w, H, D, S, spread=1.0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    Lk = nf * h * w
+    q, k = (spread * torch.randn(n, H, D, generator=g, device=DEV) for n in (Lq, Lk))
+    q, k = (x.to(dtype) for x in (q, k))
+    slot = torch.full((nf,), -1, dtype=torch.int32, device=DEV)
+    at = min(1, nf - S)
+    slot[at:at + S] = torch.arange(S, dtype=torch.int32, device=DEV).flip(0)
+    uv = idx = None
+    if S:
+        uv = torch.rand(S, Lq, 2, generator=g, device=DEV) * torch.tensor([float(w), float(h)], device=DEV)
+        idx = torch.randint(-3, h * w, (S, Lq), generator=g, device=DEV, dtype=torch.int32)
+        uv[idx < -1] = math.nan
+    return q, k, slot, uv, idx
+
+
+def _oracle(q, k, slot, uv, idx, h, w, scale, lam, sigma):
+    n = lambda x: None if x is None else (x.float() if x.dtype != torch.float32 and x.is_floating_point() else x).cpu().numpy()  # noqa: E731
+    A = OC.logits(n(q), n(k), n(slot), n(uv), n(idx), h, w, scale, lam, sigma)
+    m = A.max(axis=2)
+    return A, np.ascontiguousarray((m + np.log(np.exp(A - m[:, :, None]).sum(axis=2))).astype(np.float32))
+
+
+def _tolerance(q, k, A, lse, h, w, scale, lam, sigma, D, biased):
+    a, b = (np.abs(x.float().cpu().numpy().astype(np.float64)) for x in (q, k))
+    rel = (D + 4) * U * scale * np.einsum("phd,khd->hpk", a, b) + 4 * U * (np.abs(A) + 2 * np.abs(lse.astype(np.float64))[:, :, None])
+    if biased:
+        rel = rel + 32 * U * abs(lam) * (h * h + w * w) / (4 * sigma * sigma)
+    p = np.exp(A - lse.astype(np.float64)[:, :, None])
+    return (p * (np.expm1(rel) + 2.0 ** -22)).sum(axis=1) + p.sum(axis=1) * (A.shape[1] / 16 + 20) * U + A.shape[1] * 2.0 ** -126
+
+
+SHAPES = [
+    # Lq, frames, h, w, H, S
+    (1, 1, 1, 1, 1, 0), (1, 1, 1, 1, 1, 1), (1, 24, 5, 13, 3, 0), (31, 3, 4, 8, 2, 2), (33, 4, 8, 8, 1, 2), (64, 4, 8, 8, 1, 2),
+    (97, 5, 3, 11, 3, 3), (128, 2, 1, 257, 2, 1), (200, 7, 9, 7, 2, 5), (65, 18, 2, 3, 4, 6), (300, 3, 16, 20, 2, 0), (1, 6, 30, 52, 2, 3),
+    (129, 2, 33, 31, 3, 2), (700, 2, 7, 19, 1, 1),
+]
+
+
+@pytest.mark.parametrize("dtype,D", [(torch.bfloat16, 128), (torch.float32, 128), (torch.float32, 64), (torch.float8_e4m3fn, 128)])
+@pytest.mark.parametrize("Lq,nf,h,w,H,S", SHAPES)
+def test_weights(dtype, D, Lq, nf, h, w, H, S):
+    q, k, slot, uv, idx = _case(Lq + nf, dtype, Lq, nf, h, w, H, D, S)
+    scale, lam, sigma = D ** -0.5, 1.3, 2.0
+    A, lse = _oracle(q, k, slot, uv, idx, h, w, scale, lam, sigma)
+    tol = _tolerance(q, k, A, lse, h, w, scale, lam, sigma, D, S > 0)
+    want = OC.key_weight(A, lse)
+    lse_d = torch.from_numpy(lse).to(DEV)
+    kw = dict(h=h, w=w, softmax_scale=scale, lam=lam, sigma=sigma)
+    if S and dtype != torch.float32 and max(h, w) > 256:  # beyond the bias tables of the attention
+        with pytest.raises(rv.RevisitError, match="256"):
+            rv.attention_key_weight(q, k, lse_d, slot, uv, idx, **kw)
+        return
+    for parts in (0, 1, 2, 5, 64):
+        got = rv.attention_key_weight(q, k, lse_d, slot, uv, idx, query_parts=parts, **kw)
+        off = np.abs(got.double().cpu().numpy() - want)
+        assert (off <= tol).all(), (parts, (off / tol).max())
+    # the weights of before, faded; into their own place
+    prev = torch.rand(got.shape, device=DEV)
+    want = OC.key_weight(A, lse, prev.cpu().numpy(), 0.75)
+    tol = tol + (0.75 * prev.cpu().numpy().astype(np.float64) + want) * U
+    got = rv.attention_key_weight(q, k, lse_d, slot, uv, idx, prev=prev, decay=0.75, **kw)
+    assert (np.abs(got.double().cpu().numpy() - want) <= tol).all()
+    again = rv.attention_key_weight(q, k, lse_d, slot, uv, idx, prev=prev, decay=0.75, out=prev, **kw)
+    assert again is prev and torch.equal(prev, got)
+
+
+@pytest.mark.parametrize("dtype,D", [(torch.bfloat16, 128), (torch.float32, 64), (torch.float8_e4m3fn, 128)])
+def test_queries_without_an_lse(dtype, D):
+    """Rows whose LSE is NaN or infinite add nothing, even where their logits are not finite."""
+    Lq, nf, h, w, H, S = 70, 4, 5, 9, 2, 2
+    q, k, slot, uv, idx = _case(9, dtype, Lq, nf, h, w, H, D, S)
+    scale, lam, sigma = D ** -0.5, 1.0, 2.0
+    A, lse = _oracle(q, k, slot, uv, idx, h, w, scale, lam, sigma)
+    tol = _tolerance(q, k, A, lse, h, w, scale, lam, sigma, D, True)
+    lse[0, 3], lse[1, :40], lse[0, 64:] = np.nan, np.inf, -np.inf
+    want = OC.key_weight(A, lse)
+    q = q.float()
+    q[64:, 0], q[:40, 1] = math.nan, 3e38 if dtype != torch.float8_e4m3fn else 448.0
+    got = rv.attention_key_weight(q.to(dtype), k, torch.from_numpy(lse).to(DEV), slot, uv, idx, h=h, w=w, softmax_scale=scale, lam=lam,
+                                  sigma=sigma)
+    off = np.abs(got.double().cpu().numpy() - want)
+    assert (off <= tol).all(), (off / tol).max()
+    none = rv.attention_key_weight(q.to(dtype), k, torch.full((H, Lq), math.nan, device=DEV), slot, uv, idx, h=h, w=w,
+                                   softmax_scale=scale, lam=lam, sigma=sigma)
+    assert not none.any()
+
+
+@pytest.mark.parametrize("dtype,D", [(torch.bfloat16, 128), (torch.float32, 64), (torch.float8_e4m3fn, 128)])
+def test_sharp_rows(dtype, D):
+    """Logits far apart: one key has nearly all of a query's weight and the others' underflow to 0."""
+    Lq, nf, h, w, H = 100, 3, 7, 10, 2
+    q, k, slot, _, _ = _case(10, dtype, Lq, nf, h, w, H, D, 0, spread=6.0)
+    A, lse = _oracle(q, k, slot, None, None, h, w, D ** -0.5, 0.0, 1.0)
+    tol = _tolerance(q, k, A, lse, h, w, D ** -0.5, 0.0, 1.0, D, False)
+    got = rv.attention_key_weight(q, k, torch.from_numpy(lse).to(DEV), None, None, None, h=h, w=w, softmax_scale=D ** -0.5, lam=0.0, sigma=1.0)
+    off = np.abs(got.double().cpu().numpy() - OC.key_weight(A, lse))
+    assert (off <= tol).all(), (off / tol).max()
+
+
+def test_no_queries():
+    k = torch.randn(30, 2, 128, device=DEV).bfloat16()
+    q = torch.empty(0, 2, 128, dtype=torch.bfloat16, device=DEV)
+    lse, prev = torch.empty(2, 0, device=DEV), torch.rand(2, 30, device=DEV)
+    kw = dict(h=5, w=6, softmax_scale=0.1, lam=0.0, sigma=1.0)
+    assert torch.equal(rv.attention_key_weight(q, k, lse, None, None, None, prev=prev, decay=0.5, **kw), 0.5 * prev)
+    assert not rv.attention_key_weight(q, k, lse, None, None, None, out=torch.ones(2, 30, device=DEV), **kw).any()
+
+
+@pytest.mark.parametrize("dtype,D", [(torch.bfloat16, 128), (torch.float32, 128), (torch.float8_e4m3fn, 128)])
+def test_whole_chunk_under_its_own_attention(dtype, D):
+    """A loop-closure chunk with the LSE that the attention returned: the weights of a head add up to its queries."""
+    h, w, H, nf, S = 30, 52, 3, 6, 3
+    q, k, slot, uv, idx = _case(11, dtype, 3 * h * w, nf, h, w, H, D, S)
+    v = torch.randn(k.shape, device=DEV).to(torch.bfloat16 if dtype != torch.float32 else dtype)
+    uv = uv.nan_to_num(1.0)
+    kw = dict(h=h, w=w, softmax_scale=D ** -0.5, lam=1.0, sigma=2.0)
+    _, lse = rv.biased_chunk_attention(q, k, v, slot, uv, idx, **kw)
+    got = rv.attention_key_weight(q, k, lse, slot, uv, idx, **kw)
+    total = got.double().sum(1)
+    # the bf16 / fp8 attention sums probabilities rounded to bf16: its LSE is within 4e-3 (its own tests' bar)
+    near = 4e-3 if dtype != torch.float32 else 1e-4
+    assert ((total / q.shape[0] - 1).abs() <= near).all()
+    assert torch.equal(got, rv.attention_key_weight(q, k, lse, slot, uv, idx, **kw))  # the same bits again
+
+
+def test_retrieved_slots_out_of_range_are_unbiased():
+    h, w, H, D, nf = 4, 5, 2, 128, 4
+    q, k, slot, uv, idx = _case(12, torch.bfloat16, 40, nf, h, w, H, D, 2)
+    slot[:] = torch.tensor([2, -7, 1000, 1], dtype=torch.int32)
+    A, lse = _oracle(q, k, torch.tensor([-1, -1, -1, 1]), uv, idx, h, w, 0.1, 1.0, 2.0)
+    got = rv.attention_key_weight(q, k, torch.from_numpy(lse).to(DEV), slot, uv, idx, h=h, w=w, softmax_scale=0.1, lam=1.0, sigma=2.0)
+    off = np.abs(got.double().cpu().numpy() - OC.key_weight(A, lse))
+    assert (off <= _tolerance(q, k, A, lse, h, w, 0.1, 1.0, 2.0, D, True)).all()
+
+
+def test_refusals_of_the_binding():
+    q, k, slot, uv, idx = _case(13, torch.bfloat16, 40, 4, 4, 5, 2, 128, 2)
+    lse = torch.zeros(2, 40, device=DEV)
+    kw = dict(h=4, w=5, softmax_scale=0.1, lam=1.0, sigma=2.0)
+    with pytest.raises(ValueError, match="lse"):
+        rv.attention_key_weight(q, k, lse[:, :39].contiguous(), slot, uv, idx, **kw)
+    with pytest.raises(ValueError, match="contiguous"):
+        rv.attention_key_weight(q[::2], k, lse[:, ::2].contiguous(), slot, uv, idx, **kw)
+    with pytest.raises(ValueError, match="whole number"):
+        rv.attention_key_weight(q, k, lse, slot, uv, idx, **dict(kw, w=7))
+    with pytest.raises(rv.RevisitError):
+        rv.attention_key_weight(q, k, lse, slot, uv, idx, query_parts=2, workspace=torch.empty(16, dtype=torch.uint8, device=DEV), **kw)
