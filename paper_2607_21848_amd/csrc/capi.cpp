@@ -769,6 +769,7 @@ int attention_key_weight(const void* q, const void* k, const float* lse, int32_t
     a.corr_uv = corr_uv;
     a.corr_idx = corr_idx;
     a.c_log2 = (float)((double)softmax_scale * M_LOG2E);
+    a.gamma = gamma;
     a.gamma2 = (float)((double)gamma2 * M_LOG2E);
     a.decay = decay;
     return launched(revisit::launch_key_weight(a, stream), fn);

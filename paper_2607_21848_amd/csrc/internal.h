@@ -270,7 +270,8 @@ struct KeyWeightArgs {
     const float* corr_uv;
     const int32_t* corr_idx;
     int32_t S;               // 0 = bias off
-    float c_log2, gamma2;    // softmax_scale log2 e; lambda log2 e / (2 sigma^2)
+    float c_log2;            // softmax_scale log2 e
+    float gamma, gamma2;     // lambda / (2 sigma^2 softmax_scale); lambda log2 e / (2 sigma^2)
     float decay;
     int32_t parts;           // query parts
     int32_t frame_blocks, n_blocks;  // key blocks per frame and per head
