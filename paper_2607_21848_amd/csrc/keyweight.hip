@@ -89,8 +89,8 @@ __device__ __forceinline__ KeyBlock key_block(const KeyWeightArgs& a, int kb, bo
 
 template <bool kFp8, bool kBias>
 __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeightArgs a, unsigned n_items) {
-    __shared__ __attribute__((aligned(16))) uint8_t lds_q[2][kStepBytes];
-    __shared__ __attribute__((aligned(16))) float lds_row[2][kStep];  // -LSE log2 e of the step's queries
+    __shared__ __attribute__((aligned(256))) uint8_t lds_q[3 * kStepBytes];
+    __shared__ floatx4 lds_row[3 * kStep / 4];  // -LSE log2 e of the step's queries
 
     const int tid = threadIdx.x;
     const int lane = tid & 63;
@@ -118,29 +118,42 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
     constexpr int kLoads = kStep * kChunks / (64 * kWaves);
     u32x4 stage[kLoads];
     float stage_lse = 0.0f;
-    auto fetch = [&](int q0) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int e = tid + i * 64 * kWaves;
-            const int q = min(q0 + e / kChunks, a.Lq - 1);
-            stage[i] = *reinterpret_cast<const u32x4*>(Qg + q * row_bytes + 16 * (e % kChunks));
-        }
-        if (tid < kStep) stage_lse = a.lse[(int64_t)hd * a.Lq + min(q0 + tid, a.Lq - 1)];
+    // offsets of a step's loads from its first row (below 2^30); a step that runs past the last row repeats that one
+    uint32_t off[kLoads];
+    auto chunk_off = [&](int i, int last) -> uint32_t {
+        const int e = tid + i * 64 * kWaves;
+        return (uint32_t)(min(e / kChunks, last) * (int)row_bytes + 16 * (e % kChunks));
     };
-    auto put = [&](int q0, int buf) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) off[i] = chunk_off(i, kStep);
+    auto fetch = [&](int q0) {
+        const uint8_t* base = Qg + q0 * row_bytes;
+        const float* lse = a.lse + (int64_t)hd * a.Lq + q0;
+        if (q0 + kStep <= a.Lq) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) stage[i] = *reinterpret_cast<const u32x4*>(base + off[i]);
+            stage_lse = lse[lane];
+        } else {
+            const int last = a.Lq - 1 - q0;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) stage[i] = *reinterpret_cast<const u32x4*>(base + chunk_off(i, last));
+            stage_lse = lse[min(lane, last)];
+        }
+    };
+    auto put = [&](int q0, int to, int to_row) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int e = tid + i * 64 * kWaves;
             const int r = e / kChunks, c = e % kChunks;
             if constexpr (kFp8) {
-                *reinterpret_cast<u32x4*>(lds_q[buf] + chunk_at(r, 2 * c)) = wide(stage[i][0], stage[i][1]);
-                *reinterpret_cast<u32x4*>(lds_q[buf] + chunk_at(r, 2 * c + 1)) = wide(stage[i][2], stage[i][3]);
+                *reinterpret_cast<u32x4*>(lds_q + to + chunk_at(r, 2 * c)) = wide(stage[i][0], stage[i][1]);
+                *reinterpret_cast<u32x4*>(lds_q + to + chunk_at(r, 2 * c + 1)) = wide(stage[i][2], stage[i][3]);
             } else {
-                *reinterpret_cast<u32x4*>(lds_q[buf] + chunk_at(r, c)) = stage[i];
+                *reinterpret_cast<u32x4*>(lds_q + to + chunk_at(r, c)) = stage[i];
             }
         }
         // a query past the end, or one without an LSE, has no weight to give
-        if (tid < kStep) lds_row[buf][tid] = q0 + tid < q_end && __builtin_isfinite(stage_lse) ? -stage_lse * kLog2e : -INFINITY;
+        if (wave == 0) reinterpret_cast<float*>(lds_row + to_row)[lane] = q0 + lane < q_end && __builtin_isfinite(stage_lse) ? -stage_lse * kLog2e : -INFINITY;
     };
     if (t0 < t1) fetch(t0 * 32);
 
@@ -171,69 +184,169 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
             kbias[b] = as_bf16x8(u32x4{pack2(twice, twice), pack2(twice, ph), pack2(pm, pl), hh ? kOne : pack2(kOne, kOne)});
         }
     }
-    // query side of the bias products of 32 queries from q0 on, for retrieved frame s
-    auto query_bias = [&](int s, int q0) -> bf16x8 {
-        const int64_t o = (int64_t)s * a.Lq + min(q0 + n, a.Lq - 1);
-        const float2 u = reinterpret_cast<const float2*>(a.corr_uv)[o];
-        u32x4 v = u32x4{0, 0, 0, 0};
-        if (a.corr_idx[o] >= 0 && !__builtin_isnan(u.x)) {
-            const float ux = u.x - cx, uy = u.y - cy;
-            uint32_t ah, am, al, zh, zm, zl;
-            split3(a.gamma * (hh ? uy : ux), ah, am, al);
-            split3(-a.gamma * (ux * ux + uy * uy), zh, zm, zl);
-            v = u32x4{pack2(ah, am), pack2(al, kOne), pack2(kOne, kOne), hh ? zl : pack2(zh, zm)};
+    // Bias products: query side of a step's two halves, for each block's frame.
+    // A lane takes one of the step's 64 queries, evaluates both contraction halves
+    // (x terms for the first, y terms for the second) and one swap of wave
+    // halves hands each to the lanes of its half.
+    const int slot0 = kb[0].slot, slot1 = kb[1].slot;
+    float2 corr_u[2];
+    int corr_i[2];
+    auto fetch_corr = [&](int q0) {
+        const int q = min(q0 + lane, a.Lq - 1);
+        if (slot0 >= 0) {
+            corr_u[0] = reinterpret_cast<const float2*>(a.corr_uv)[(int64_t)slot0 * a.Lq + q];
+            corr_i[0] = a.corr_idx[(int64_t)slot0 * a.Lq + q];
         }
-        return as_bf16x8(v);
+        if (slot1 >= 0 && slot1 != slot0) {
+            corr_u[1] = reinterpret_cast<const float2*>(a.corr_uv)[(int64_t)slot1 * a.Lq + q];
+            corr_i[1] = a.corr_idx[(int64_t)slot1 * a.Lq + q];
+        }
+    };
+    u32x4 qb[2][2];  // [block][half of the step]
+    auto query_bias = [&](float2 u, int idx, u32x4* out) {
+        const bool ok = idx >= 0 && !__builtin_isnan(u.x);
+        const float ux = ok ? u.x - cx : 0.0f, uy = ok ? u.y - cy : 0.0f;
+        uint32_t xh, xm, xl, yh, ym, yl, zh, zm, zl;
+        split3(a.gamma * ux, xh, xm, xl);
+        split3(a.gamma * uy, yh, ym, yl);
+        split3(-a.gamma * (ux * ux + uy * uy), zh, zm, zl);
+        const uint32_t one = ok ? kOne : 0;
+        const u32x4 x = {pack2(xh, xm), pack2(xl, one), pack2(one, one), pack2(zh, zm)}, y = {pack2(yh, ym), pack2(yl, one), pack2(one, one), zl};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const auto s = __builtin_amdgcn_permlane32_swap(x[i], y[i], false, false);
+            out[0][i] = s[0];
+            out[1][i] = s[1];
+        }
+    };
+    auto make_bias = [&]() {
+        if (slot0 >= 0) query_bias(corr_u[0], corr_i[0], qb[0]);
+        if (slot1 >= 0) {
+            if (slot1 == slot0) {
+                qb[1][0] = qb[0][0];
+                qb[1][1] = qb[0][1];
+            } else {
+                query_bias(corr_u[1], corr_i[1], qb[1]);
+            }
+        }
+    };
+#pragma unroll
+    for (int b = 0; b < 2; ++b) qb[b][0] = qb[b][1] = u32x4{0, 0, 0, 0};
+
+    const int n_steps = (t1 - t0 + 1) / 2;
+    const int q_begin = t0 * 32;
+    float sum[2] = {0.0f, 0.0f};
+    floatx16 accA[2], accB[2];
+    u32x4 qf[4];     // queries of the next four products
+    floatx4 rc[2];   // row constants of the next eight exponentials
+    // chunk 2 j + hh of this lane's row: 32 j has no bit in common with a row's start
+    const int lane_at = chunk_at(n, hh);
+    auto read_q = [&](int rows, int j) { qf[j & 3] = *reinterpret_cast<const u32x4*>(lds_q + ((rows + lane_at) ^ (32 * j))); };
+    auto read_rc = [&](int row, int i) { rc[i & 1] = lds_row[row + 2 * i + hh]; };
+    auto first = [&](floatx16* acc, int half) {  // the products start from the bias, or from 0
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            acc[b] = floatx16{0};
+            if constexpr (kBias) acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qb[b][half]), kbias[b], acc[b], 0, 0, 0);
+        }
+    };
+    constexpr int kHalf = 32 * kRowBytes, kRow = kStep / 4;  // half a step's rows; a step's row constants, in quads
+
+    // Half of a step: the products of the next half (rows) beside the exponentials of
+    // this one (row constants row), one MFMA to two of them. Operands are read four
+    // products, row constants eight exponentials ahead: past the end, those of the half after.
+    auto do_half = [&](auto last_tag, floatx16* cur, floatx16* next, int next_half, int rows, int rows_after, int row, int row_after) __attribute__((always_inline)) {
+        constexpr bool kLast = decltype(last_tag)::value;
+        if constexpr (!kLast) first(next, next_half);
+        float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kD / 16; ++j) {
+            if constexpr (!kLast) {
+                next[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qf[j & 3]), kf[0][j], next[0], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 2 * j; i < 2 * j + 2; ++i) {
+                // a probability: at most 1, and 0 where the row has no LSE whatever its logits are
+                const float e = __builtin_amdgcn_exp2f(fmaf(cur[0][i], a.c_log2, rc[(i >> 2) & 1][i & 3]));
+                s0 += fminf(fmaxf(e, 0.0f), 1.0f);
+            }
+            asm volatile("" : "+v"(s0));  // keeps the exponentials here
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (!kLast) {
+                next[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qf[j & 3]), kf[1][j], next[1], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 2 * j; i < 2 * j + 2; ++i) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(cur[1][i], a.c_log2, rc[(i >> 2) & 1][i & 3]));
+                s1 += fminf(fmaxf(e, 0.0f), 1.0f);
+            }
+            asm volatile("" : "+v"(s1));
+            if constexpr (!kLast) read_q(j < 4 ? rows : rows_after, (j + 4) & 7);
+            if (j & 1) {
+                if (j < 4) read_rc(row, (j >> 1) + 2);
+                else if constexpr (!kLast) read_rc(row_after, (j >> 1) - 2);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        sum[0] += s0;
+        sum[1] += s1;
     };
 
-    float sum[2] = {0.0f, 0.0f};
-    int buf = 0;
-    if (t0 < t1) put(t0 * 32, 0);
-    __syncthreads();
-    for (int t = t0; t < t1; t += 2, buf ^= 1) {
-        const bool more = t + 2 < t1;
-        if (more) fetch((t + 2) * 32);
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            if (half && t + 1 >= t1) break;  // uniform
-            floatx16 acc[2] = {floatx16{0}, floatx16{0}};
-            if constexpr (kBias) {
-                if (kb[0].slot >= 0 || kb[1].slot >= 0) {  // uniform per wave
-                    bf16x8 qb = as_bf16x8(u32x4{0, 0, 0, 0});
-                    if (kb[0].slot >= 0) {
-                        qb = query_bias(kb[0].slot, (t + half) * 32);
-                        acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qb, kbias[0], acc[0], 0, 0, 0);
-                    }
-                    if (kb[1].slot >= 0) {
-                        if (kb[1].slot != kb[0].slot) qb = query_bias(kb[1].slot, (t + half) * 32);
-                        acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qb, kbias[1], acc[1], 0, 0, 0);
-                    }
-                }
-            }
-            const uint8_t* rows = lds_q[buf];
-#pragma unroll
-            for (int j = 0; j < kD / 16; ++j) {
-                const bf16x8 qf = as_bf16x8(*reinterpret_cast<const u32x4*>(rows + chunk_at(32 * half + n, 2 * j + hh)));
-                acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[0][j], acc[0], 0, 0, 0);
-                acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[1][j], acc[1], 0, 0, 0);
-            }
-            floatx4 rc[4];  // queries 8 i + 4 hh ..
-#pragma unroll
-            for (int i = 0; i < 4; ++i) rc[i] = *reinterpret_cast<const floatx4*>(&lds_row[buf][32 * half + 8 * i + 4 * hh]);
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                float s = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    // a probability: at most 1, and 0 where the row has no LSE whatever its logits are
-                    const float e = __builtin_amdgcn_exp2f(fmaf(acc[b][i], a.c_log2, rc[i >> 2][i & 3]));
-                    s += fminf(fmaxf(e, 0.0f), 1.0f);
-                }
-                sum[b] += s;
-            }
+    if (n_steps > 0) {
+        put(q_begin, 0, 0);
+        if constexpr (kBias) {
+            fetch_corr(q_begin);
+            make_bias();
         }
-        if (more) put((t + 2) * 32, buf ^ 1);
+        if (n_steps > 1) fetch(q_begin + kStep);
+        // the keys are waited for here: at their first use below the wait would drain the
+        // next step's query loads too, every time round the loop
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < kD / 16; ++j) asm volatile("" : "+v"(kf[b][j]));
         __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) read_q(0, j);
+        first(accA, 0);
+#pragma unroll
+        for (int j = 0; j < kD / 16; ++j) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) accA[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qf[j & 3]), kf[b][j], accA[b], 0, 0, 0);
+            read_q(j < 4 ? 0 : kHalf, (j + 4) & 7);
+        }
+        read_rc(0, 0);
+        read_rc(0, 1);
+        if (n_steps > 1) put(q_begin + kStep, kStepBytes, kRow);
+        if (n_steps > 2) fetch(q_begin + 2 * kStep);
+        if (kBias && n_steps > 1) fetch_corr(q_begin + kStep);
+        __syncthreads();
+        // At the top of step s: accA holds the logits of its first half, qf the first queries of
+        // its second, buffer s + 1 the next step, the stage registers the loads of step s + 2
+        // (buffers s mod 3).
+        int q0 = 0, q1 = kStepBytes, q2 = 2 * kStepBytes, r0 = 0, r1 = kRow, r2 = 2 * kRow;
+        for (int s = 0; s + 1 < n_steps; ++s) {
+            do_half(std::false_type{}, accA, accB, 1, q0 + kHalf, q1, r0, r0 + kRow / 2);
+            if (s + 2 < n_steps) put(q_begin + (s + 2) * kStep, q2, r2);
+            if (s + 3 < n_steps) fetch(q_begin + (s + 3) * kStep);
+            if constexpr (kBias) {
+                make_bias();  // of step s + 1
+                if (s + 2 < n_steps) fetch_corr(q_begin + (s + 2) * kStep);
+            }
+            do_half(std::false_type{}, accB, accA, 0, q1, q1 + kHalf, r0 + kRow / 2, r1);
+            __syncthreads();
+            const int qt = q0, rt = r0;
+            q0 = q1;
+            q1 = q2;
+            q2 = qt;
+            r0 = r1;
+            r1 = r2;
+            r2 = rt;
+        }
+        do_half(std::false_type{}, accA, accB, 1, q0 + kHalf, q0, r0, r0 + kRow / 2);
+        do_half(std::true_type{}, accB, accA, 0, 0, 0, r0 + kRow / 2, 0);
     }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
