@@ -790,6 +790,7 @@ int prepare_select(const char* fn, int32_t sets, int32_t heads, int32_t n_units,
     a.heads = heads;
     a.n_units = n_units;
     a.unit = unit;
+    a.splits = revisit::select_splits(a);
     *bytes = revisit::select_workspace_bytes(a);
     return REVISIT_OK;
 }
@@ -826,7 +827,7 @@ int select_kept(const float* weight, int32_t sets, int32_t heads, int32_t n_unit
     a.last = last;
     a.out_idx = out_idx;
     a.out_score = out_score;
-    a.unit_score = static_cast<float*>(workspace);
+    a.unit_sum = static_cast<double*>(workspace);
     return launched(revisit::launch_select(a, stream), fn);
 }
 

@@ -289,8 +289,10 @@ struct SelectArgs {
     int32_t keep, first, last;
     int32_t* out_idx;     // [sets][keep]
     float* out_score;     // nullable [sets][keep]
-    float* unit_score;    // [sets][n_units], workspace (select_workspace_bytes)
+    int32_t splits;       // head parts of the scores
+    double* unit_sum;     // [splits][sets][n_units], workspace (select_workspace_bytes)
 };
+int32_t select_splits(const SelectArgs& a);
 size_t select_workspace_bytes(const SelectArgs& a);
 hipError_t launch_select(const SelectArgs& a, hipStream_t stream);
 

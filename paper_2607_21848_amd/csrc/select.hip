@@ -1,5 +1,21 @@
-// The choice of what a cache keeps (select_kept): unit scores and the largest of
-// them, in order.
+// The choice of what a cache keeps (select_kept): unit scores, then the largest of
+// them in the order of their places.
+//
+// Scores. Every weight is read once: bound by HBM. A unit's weights are added in
+// double by a group of lanes that fits its length (one lane, 8, a wave or a
+// workgroup; units of a token go one to a lane, so that lanes read consecutive
+// words), four loads in flight; where few long units leave compute units idle, the
+// heads are cut into parts whose sums meet in the choice.
+//
+// Choice. One workgroup of 16 waves per set; a wave holds a contiguous range of units,
+// lane by lane, in registers. The keep-th largest score is found digit by digit
+// over the scores as ordered unsigned numbers, 12, 10 and 10 bits, with a histogram
+// in LDS: the first digit holds sign, exponent and three bits, so that the usual
+// scores spread over many bins, and the later ones see only the units in the
+// bin that the digit before left. Where a wave's units all have the same digit (equal
+// scores) one lane counts for all. With the threshold, every wave counts what it keeps, one
+// barrier gives each its place, and the units are written in order. Latency
+// bounds it: 96 sets of 37440 tokens are 14 MB.
 
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -10,123 +26,313 @@
 namespace revisit {
 namespace {
 
-// Unit scores: the sum of a unit's weights over its tokens and the set's heads,
-// in double (in any order it is within 2^-40 or so of the sum, so the one
-// rounding to fp32 gives what a reader of the definition gets). One block per unit.
-__global__ __launch_bounds__(256) void unit_score_kernel(SelectArgs a, unsigned n_items) {
-    const unsigned item = row_block();
-    if (item >= n_items) return;
-    const unsigned set = item / (unsigned)a.n_units, u = item - set * (unsigned)a.n_units;
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+constexpr int kScoreBlock = 256;
+
+// Sum of `count` vectors of VEC weights per unit, G lanes a unit; grid.y = head part.
+template <int G, int VEC>
+__global__ __launch_bounds__(kScoreBlock) void unit_score_kernel(SelectArgs a, int64_t n_items, double inv_len) {
+    constexpr int kUnits = kScoreBlock / G;
+    const int64_t item = (int64_t)blockIdx.x * kUnits + threadIdx.x / G;
+    const int part = blockIdx.y;
+    const int h0 = (int)((int64_t)part * a.heads / a.splits), h1 = (int)((int64_t)(part + 1) * a.heads / a.splits);
     const int64_t row = (int64_t)a.n_units * a.unit;
-    const float* w = a.weight + (int64_t)set * a.heads * row + (int64_t)u * a.unit;
     double sum = 0.0;
-    for (int h = 0; h < a.heads; ++h)
-        for (int i = threadIdx.x; i < a.unit; i += 256) sum += (double)w[h * row + i];
-    __shared__ double lds[256];
-    lds[threadIdx.x] = sum;
-    __syncthreads();
-    for (int k = 128; k > 0; k /= 2) {
-        if ((int)threadIdx.x < k) lds[threadIdx.x] += lds[threadIdx.x + k];
-        __syncthreads();
+    if (item < n_items) {
+        const int64_t set = item / a.n_units, u = item - set * a.n_units;
+        const float* w = a.weight + (set * a.heads + h0) * row + u * a.unit;
+        const int len = a.unit / VEC;
+        const int64_t total = (int64_t)(h1 - h0) * len;
+        for (int64_t e0 = threadIdx.x % G; e0 < total; e0 += 4 * G) {
+            float v[4][VEC];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int64_t e = e0 + k * G;
+                // (e + 1/2) / len truncates to e / len exactly below 2^50
+                const int64_t h = len == 1 ? e : (int64_t)(((double)e + 0.5) * inv_len);
+                const float* p = w + h * row + (e - h * len) * VEC;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[k][i] = 0.0f;
+                if (e < total) {
+                    if constexpr (VEC == 4) {
+                        const floatx4 x = *reinterpret_cast<const floatx4*>(p);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[k][i] = x[i];
+                    } else {
+                        v[k][0] = *p;
+                    }
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sum += (double)v[k][i];
+        }
     }
-    if (threadIdx.x == 0) a.unit_score[item] = (float)lds[0];
+#pragma unroll
+    for (int k = (G < 64 ? G : 64) / 2; k > 0; k /= 2) sum += __shfl_xor(sum, k);
+    if constexpr (G > 64) {
+        __shared__ double lds[G / 64];
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x / 64] = sum;
+        __syncthreads();
+        sum = 0.0;
+#pragma unroll
+        for (int k = 0; k < G / 64; ++k) sum += lds[k];
+    }
+    if (threadIdx.x % G == 0 && item < n_items) a.unit_sum[(int64_t)part * n_items + item] = sum;
 }
 
-// fp32 as an unsigned number in the same order: NaN below all, -0 equal to 0
+// fp32 as an unsigned number in the same order: NaN below all, -0 equal to 0; and back
 __device__ __forceinline__ uint32_t ordered(float x) {
     if (__builtin_isnan(x)) return 0;
-    uint32_t u = __float_as_uint(x);
-    if (u == 0x80000000u) u = 0;
+    const uint32_t u = __float_as_uint(x + 0.0f);  // -0 + 0 = 0
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
+__device__ __forceinline__ float number(uint32_t k) {
+    if (k == 0) return NAN;
+    return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
+}
 
-constexpr int kSelThreads = 1024;
+// score of an item: a set's unit
+template <bool kSums>
+__device__ __forceinline__ float score_of(const SelectArgs& a, int64_t item, int64_t n_items) {
+    if constexpr (kSums) {
+        double s = 0.0;
+        for (int p = 0; p < a.splits; ++p) s += a.unit_sum[(int64_t)p * n_items + item];
+        return (float)s;
+    } else {
+        return a.weight[item];
+    }
+}
 
-__global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a, const float* score) {
-    __shared__ unsigned hist[256];
-    __shared__ unsigned sh_digit, sh_want, wave_n[2][kSelThreads / 64];
-    const int tid = threadIdx.x;
-    const float* s = score + (int64_t)blockIdx.x * a.n_units;
+constexpr int kSelWaves = 16;
+constexpr int kSelThreads = 64 * kSelWaves;
+constexpr int kBins = 4096;
+
+// kHeld: units of a lane, held in registers; 0: any number, read again in every pass.
+template <int kHeld, bool kSums>
+__global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
+    __shared__ unsigned hist[kBins];
+    __shared__ unsigned wave_sum[kSelWaves], found[2], wave_gt[kSelWaves], wave_eq[kSelWaves];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t n_items = (int64_t)a.sets * a.n_units;
+    const int64_t base = (int64_t)blockIdx.x * a.n_units;
     int32_t* out = a.out_idx + (int64_t)blockIdx.x * a.keep;
     float* out_score = a.out_score ? a.out_score + (int64_t)blockIdx.x * a.keep : nullptr;
-    const int lo = a.first, hi = a.n_units - a.last;
-    const unsigned m = (unsigned)(a.keep - a.first - a.last);  // to choose of [lo, hi)
-    // the m-th largest of them, digit by digit; `want` of those equal to it are taken
+    auto score = [&](int64_t unit) -> float { return score_of<kSums>(a, base + unit, n_items); };
+    // the protected ends
+    const int from_last = a.n_units - a.last;
+    for (int i = tid; i < a.first + a.last; i += kSelThreads) {
+        const int u = i < a.first ? i : from_last + (i - a.first);
+        const int o = i < a.first ? i : a.keep - a.last + (i - a.first);
+        out[o] = u;
+        if (out_score) out_score[o] = score(u);
+    }
+    const unsigned m = (unsigned)(a.keep - a.first - a.last);  // to choose from the units between
+    if (m == 0) return;  // uniform
+    // this wave's share of them: rounds of 64, `count` in all, from u0 on
+    const int64_t open = (int64_t)from_last - a.first;
+    const int rounds = (int)((open + kSelThreads - 1) / kSelThreads);
+    const int64_t start = (int64_t)wave * rounds * 64, u0 = a.first + start;
+    int count = (int)max((int64_t)0, min((int64_t)rounds * 64, open - start));
+    uint32_t held[kHeld ? kHeld : 1];
+    if constexpr (kHeld > 0) {
+        float x[kHeld];
+#pragma unroll
+        for (int r = 0; r < kHeld; ++r) x[r] = r * 64 + lane < count ? score(u0 + r * 64 + lane) : 0.0f;
+#pragma unroll
+        for (int r = 0; r < kHeld; ++r) held[r] = ordered(x[r]);
+    }
+    // f(unit's place in the wave, whether there is one, its key) for this lane's units
+    auto each = [&](auto f) {
+        if constexpr (kHeld > 0) {
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) {
+                if (r * 64 < count) f(r * 64 + lane, r * 64 + lane < count, held[r]);  // uniform
+            }
+        } else {
+            for (int r = 0; r * 64 < count; ++r) {
+                const int i = r * 64 + lane;
+                f(i, i < count, i < count ? ordered(score(u0 + i)) : 0u);
+            }
+        }
+        // what a pass has found out about the lanes is found out again by the next, not kept
+        asm volatile("" : "+s"(count));
+    };
+
+    // the m-th largest: its leading digits so far, and how many equal to it are taken
     uint32_t prefix = 0, mask = 0;
     unsigned want = m;
-    for (int shift = 24; shift >= 0 && m > 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
+#pragma unroll
+    for (int digit = 0; digit < 3; ++digit) {
+        constexpr int kShift[3] = {20, 10, 0};
+        const int shift = kShift[digit], bins = digit == 0 ? kBins : 1024;
+        for (int b = tid; b < bins; b += kSelThreads) hist[b] = 0;
         __syncthreads();
-        for (int i = lo + tid; i < hi; i += kSelThreads) {
-            const uint32_t k = ordered(s[i]);
-            if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+        each([&](int, bool have, uint32_t k) {
+            const bool in = have && (k & mask) == prefix;
+            const uint64_t who = __ballot(in);
+            if (who == 0) return;
+            const unsigned bin = (k >> shift) & (bins - 1);
+            const int leader = __builtin_ctzll(who);
+            const unsigned bin0 = __builtin_amdgcn_readlane(bin, leader);
+            if (__ballot(in && bin == bin0) == who) {
+                if (lane == leader) atomicAdd(&hist[bin0], (unsigned)__popcll(who));
+            } else if (in) {
+                atomicAdd(&hist[bin], 1u);
+            }
+        });
+        __syncthreads();
+        // each thread takes some bins, from the highest down: the one where the count from above reaches `want`
+        const int per = bins / kSelThreads;
+        unsigned own[kBins / kSelThreads], mine = 0;
+#pragma unroll
+        for (int b = 0; b < kBins / kSelThreads; ++b) {
+            own[b] = b < per ? hist[bins - 1 - (tid * per + b)] : 0;
+            mine += own[b];
+        }
+        unsigned upto = mine;  // of this wave's lanes up to this one
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const unsigned y = __shfl_up(upto, d);
+            if (lane >= d) upto += y;
+        }
+        if (lane == 63) wave_sum[wave] = upto;
+        __syncthreads();
+        unsigned above = upto - mine;
+        for (int w = 0; w < wave; ++w) above += wave_sum[w];
+#pragma unroll
+        for (int b = 0; b < kBins / kSelThreads; ++b) {
+            if (b < per && above < want && above + own[b] >= want) {
+                found[0] = (unsigned)(bins - 1 - (tid * per + b));
+                found[1] = want - above;
+            }
+            above += own[b];
         }
         __syncthreads();
-        if (tid == 0) {
-            unsigned left = want;
-            int d = 255;
-            while (d > 0 && hist[d] < left) left -= hist[d--];
-            sh_digit = d;
-            sh_want = left;
-        }
-        __syncthreads();
-        prefix |= sh_digit << shift;
-        mask |= 255u << shift;
-        want = sh_want;
-        __syncthreads();
+        prefix |= __builtin_amdgcn_readfirstlane(found[0]) << shift;
+        mask |= (unsigned)(bins - 1) << shift;
+        want = __builtin_amdgcn_readfirstlane(found[1]);
     }
-    // the kept ones in order: all of the protected ends, what is above the threshold and the first `want` equal to it
-    unsigned base = 0, equal = 0;
-    for (int i0 = 0; i0 < a.n_units; i0 += kSelThreads) {
-        const int i = i0 + tid;
-        const bool in = i < a.n_units, open = in && i >= lo && i < hi;
-        const uint32_t k = open ? ordered(s[i]) : 0;
-        const bool eq = open && m > 0 && k == prefix;
-        const uint64_t eq_mask = __ballot(eq);
-        const int wv = tid >> 6, lane = tid & 63;
-        const uint64_t below = ((uint64_t)1 << lane) - 1;
-        if (lane == 0) wave_n[0][wv] = __popcll(eq_mask);
-        __syncthreads();
-        unsigned eq_before = equal + __popcll(eq_mask & below), eq_all = 0;
-        for (int j = 0; j < kSelThreads / 64; ++j) {
-            if (j < wv) eq_before += wave_n[0][j];
-            eq_all += wave_n[0][j];
-        }
-        const bool keep = in && (!open || (m > 0 && (k > prefix || (eq && eq_before < want))));
+
+    // what each wave keeps: above the threshold, and equal to it
+    unsigned gt = 0, eq = 0;
+    each([&](int, bool have, uint32_t k) {
+        gt += __popcll(__ballot(have && k > prefix));
+        eq += __popcll(__ballot(have && k == prefix));
+    });
+    if (lane == 0) {
+        wave_gt[wave] = gt;
+        wave_eq[wave] = eq;
+    }
+    __syncthreads();
+    unsigned at = a.first, eq_before = 0;
+    for (int w = 0; w < wave; ++w) {
+        at += wave_gt[w];
+        eq_before += wave_eq[w];
+    }
+    at += min(eq_before, want);
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    each([&](int i, bool have, uint32_t k) {
+        const bool same = have && k == prefix;
+        const uint64_t same_mask = __ballot(same);
+        const bool keep = (have && k > prefix) || (same && eq_before + __popcll(same_mask & below) < want);
         const uint64_t keep_mask = __ballot(keep);
-        if (lane == 0) wave_n[1][wv] = __popcll(keep_mask);
-        __syncthreads();
-        unsigned at = base + __popcll(keep_mask & below), all = 0;
-        for (int j = 0; j < kSelThreads / 64; ++j) {
-            if (j < wv) at += wave_n[1][j];
-            all += wave_n[1][j];
-        }
         if (keep) {
-            out[at] = i;
-            if (out_score) out_score[at] = s[i];
+            const unsigned o = at + __popcll(keep_mask & below);
+            out[o] = (int32_t)(u0 + i);
+            if (out_score) out_score[o] = number(k);
         }
-        base += all;
-        equal += eq_all;
-        __syncthreads();
+        at += __popcll(keep_mask);
+        eq_before += __popcll(same_mask);
+    });
+}
+
+// Up to 64 units to choose from: one wave per set, a unit per lane, which is kept if fewer than m
+// come before it.
+template <bool kSums>
+__global__ __launch_bounds__(64) void select_few_kernel(SelectArgs a) {
+    const int lane = threadIdx.x;
+    const int64_t n_items = (int64_t)a.sets * a.n_units;
+    const int64_t base = (int64_t)blockIdx.x * a.n_units;
+    int32_t* out = a.out_idx + (int64_t)blockIdx.x * a.keep;
+    float* out_score = a.out_score ? a.out_score + (int64_t)blockIdx.x * a.keep : nullptr;
+    auto score = [&](int64_t unit) -> float { return score_of<kSums>(a, base + unit, n_items); };
+    const int from_last = a.n_units - a.last, open = from_last - a.first, m = a.keep - a.first - a.last;
+    const bool have = lane < open;
+    const uint32_t k = have ? ordered(score(a.first + lane)) : 0;
+    int before = 0;
+    for (int j = 0; j < open; ++j) {
+        const uint32_t y = __builtin_amdgcn_readlane(k, j);
+        before += y > k || (y == k && j < lane) ? 1 : 0;
     }
+    const bool keep = have && before < m;
+    const uint64_t kept = __ballot(keep);
+    if (keep) {
+        const int o = a.first + __popcll(kept & (((uint64_t)1 << lane) - 1));
+        out[o] = a.first + lane;
+        if (out_score) out_score[o] = number(k);
+    }
+    // the protected ends
+    for (int i = lane; i < a.first + a.last; i += 64) {
+        const int u = i < a.first ? i : from_last + (i - a.first);
+        const int o = i < a.first ? i : a.keep - a.last + (i - a.first);
+        out[o] = u;
+        if (out_score) out_score[o] = score(u);
+    }
+}
+
+template <int G, int VEC>
+void launch_scores(const SelectArgs& a, hipStream_t stream) {
+    const int64_t n = (int64_t)a.sets * a.n_units;
+    const int64_t blocks = (n + kScoreBlock / G - 1) / (kScoreBlock / G);
+    hipLaunchKernelGGL((unit_score_kernel<G, VEC>), dim3((unsigned)blocks, a.splits), dim3(kScoreBlock), 0, stream, a, n,
+                       1.0 / (a.unit / VEC));
 }
 
 }  // namespace
 
 bool select_sums(const SelectArgs& a) { return a.heads > 1 || a.unit > 1; }
 
-size_t select_workspace_bytes(const SelectArgs& a) { return select_sums(a) ? (size_t)a.sets * a.n_units * sizeof(float) : 0; }
+// Head parts of the scores: where there are fewer long units than two workgroups per
+// compute unit of a large chip, the heads share them out.
+int32_t select_splits(const SelectArgs& a) {
+    const int64_t n = (int64_t)a.sets * a.n_units;
+    if (!select_sums(a) || n == 0 || n >= 512 || (int64_t)a.heads * a.unit < 8192) return 1;
+    const int64_t want = (512 + n - 1) / n;
+    return (int32_t)(want < a.heads ? want : a.heads);
+}
+
+size_t select_workspace_bytes(const SelectArgs& a) {
+    return select_sums(a) ? (size_t)a.sets * a.n_units * select_splits(a) * sizeof(double) : 0;
+}
 
 hipError_t launch_select(const SelectArgs& a, hipStream_t stream) {
-    const float* score = a.weight;
-    if (select_sums(a)) {
-        const unsigned n = (unsigned)((int64_t)a.sets * a.n_units);
-        hipLaunchKernelGGL(unit_score_kernel, grid_rows(n), dim3(256), 0, stream, a, n);
+    const bool sums = select_sums(a);
+    if (sums) {
+        const bool vec = a.unit % 4 == 0 && (uintptr_t)a.weight % 16 == 0;
+        if (a.unit >= 512) vec ? launch_scores<256, 4>(a, stream) : launch_scores<256, 1>(a, stream);
+        else if (a.unit >= 64) vec ? launch_scores<64, 4>(a, stream) : launch_scores<64, 1>(a, stream);
+        else if (a.unit >= 8) vec ? launch_scores<8, 4>(a, stream) : launch_scores<8, 1>(a, stream);
+        else launch_scores<1, 1>(a, stream);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        score = a.unit_score;
     }
-    hipLaunchKernelGGL(select_kernel, dim3(a.sets), dim3(kSelThreads), 0, stream, a, score);
+    const int64_t open = (int64_t)a.n_units - a.first - a.last;
+    if (open <= 64) {
+        if (sums) hipLaunchKernelGGL(select_few_kernel<true>, dim3(a.sets), dim3(64), 0, stream, a);
+        else hipLaunchKernelGGL(select_few_kernel<false>, dim3(a.sets), dim3(64), 0, stream, a);
+        return hipGetLastError();
+    }
+    const dim3 grid(a.sets), block(kSelThreads);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
+    const int64_t held = (open + kSelThreads - 1) / kSelThreads;  // units of a lane
+    if (held <= 1) sums ? go(select_kernel<1, true>) : go(select_kernel<1, false>);
+    else if (held <= 8) sums ? go(select_kernel<8, true>) : go(select_kernel<8, false>);
+    else if (held <= 40) sums ? go(select_kernel<40, true>) : go(select_kernel<40, false>);
+    else sums ? go(select_kernel<0, true>) : go(select_kernel<0, false>);
     return hipGetLastError();
 }
 
