@@ -493,7 +493,7 @@ int rotary_embed(const void* q, int64_t q_row, const void* k, int64_t k_row,
  * the result does not change between calls (no atomics).
  *
  *   query_parts  0 = chosen from the shape and the compute units of the current
- *                device, or a fixed number in [1, 64] (clamped to the number of
+ *                device (one below 256 queries, at most 16), or a fixed number in [1, 64] (clamped to the number of
  *                32-query tiles) of parts into which the queries are cut; the parts'
  *                sums are added in their order by a second kernel
  *   workspace, workspace_bytes  device scratch of at least the size

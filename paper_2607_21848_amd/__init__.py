@@ -377,29 +377,39 @@ def pool_token_depth(depth: torch.Tensor, p: int, out: Optional[torch.Tensor] = 
 
 def _call(dev: torch.device, name: str, *args):
     """lib().<name>(*args, stream) on dev and its current stream, whichever device is current."""
-    if _current_device() == dev.index:
-        return _lib.check(name, getattr(lib(), name)(*args, _raw_stream(dev.index)))
-    with torch.cuda.device(dev):
-        return _lib.check(name, getattr(lib(), name)(*args, _raw_stream(dev.index)))
+    index = dev.index
+    if _current_device() == index:
+        st = getattr(lib(), name)(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(dev):
+            st = getattr(lib(), name)(*args, _raw_stream(index))
+    if st:
+        _lib.check(name, st)
 
 
 def _rows(t: torch.Tensor, name: str, dtype: torch.dtype, n: int, D: int, device):
     """A [n, H, D] tensor of whole rows (heads and elements contiguous, rows any distance apart); its H and row stride."""
+    if isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == device:
+        shape = t.shape
+        if len(shape) == 3 and shape[0] == n and shape[2] == D:
+            H = shape[1]
+            if t.is_contiguous():
+                return H, H * D
+            row, head, one = t.stride()
+            if (one == 1 or D == 1) and (head == D or H == 1):
+                return H, row if n > 1 else H * D
+            raise ValueError(f"{name}: a token's heads must be contiguous (strides {t.stride()})")
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected ({n}, heads, {D})")
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.device.type != "cuda":
-        raise ValueError(f"{name} must be a GPU tensor (got {t.device}); there is no CPU path")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
-    if t.dim() != 3 or t.shape[0] != n or t.shape[2] != D:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({n}, heads, {D})")
-    H = t.shape[1]
-    row, head, one = t.stride()
-    if n > 0 and (one != 1 or (H > 1 and head != D)):
-        raise ValueError(f"{name}: a token's heads must be contiguous (strides {t.stride()})")
-    return H, row if n > 1 else H * D
+    raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
+
+
+# types of rotary_embed by those of its input and output
+_ROTARY_DTYPES = {(torch.bfloat16, torch.bfloat16): BF16, (torch.float32, torch.float32): F32,
+                  (torch.bfloat16, torch.float8_e4m3fn): FP8_QK}
 
 
 def rotary_embed(q: torch.Tensor, k: Optional[torch.Tensor] = None, *, pairs: Sequence[int], theta: float, h: int = 0,
@@ -416,33 +426,31 @@ def rotary_embed(q: torch.Tensor, k: Optional[torch.Tensor] = None, *, pairs: Se
     where the type stays. Returns (q_out, k_out); k_out is None without k."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor [n, heads, D]")
-    dev, n, D = q.device, q.shape[0], q.shape[2]
+    dev, dtype = q.device, q.dtype
+    n, _, D = q.shape
+    q_out = k_out = None
     if out is not None:
         q_out, k_out = out
         if (k is None) != (k_out is None):
             raise ValueError("out k must be given exactly when k is")
-        if out_dtype is None:
-            out_dtype = q_out.dtype
-    odt = q.dtype if out_dtype is None else out_dtype
-    if q.dtype == torch.bfloat16 and odt == torch.float8_e4m3fn:
-        dt = FP8_QK
-    elif q.dtype == torch.bfloat16 and odt == q.dtype:
-        dt = BF16
-    elif q.dtype == torch.float32 and odt == q.dtype:
-        dt = F32
-    else:
+    odt = out_dtype or (q_out.dtype if q_out is not None else dtype)
+    dt = _ROTARY_DTYPES.get((dtype, odt))
+    if dt is None:
         raise TypeError(f"q must be bfloat16 or float32 with outputs of the same type, or bfloat16 with float8_e4m3fn "
-                        f"(got {q.dtype} and {odt})")
-    Hq, q_row = _rows(q, "q", q.dtype, n, D, dev)
-    Hk, k_row = _rows(k, "k", q.dtype, n, D, dev) if k is not None else (0, 0)
-    if out is None:
+                        f"(got {dtype} and {odt})")
+    if not q.is_cuda:
+        raise ValueError(f"q must be a GPU tensor (got {dev}); there is no CPU path")
+    Hq, q_row = _rows(q, "q", dtype, n, D, dev)
+    if q_out is None:
         q_out = torch.empty((n, Hq, D), dtype=odt, device=dev)
-        k_out = torch.empty((n, Hk, D), dtype=odt, device=dev) if k is not None else None
     Ho, qo_row = _rows(q_out, "out q", odt, n, D, dev)
     if Ho != Hq:
         raise ValueError(f"out q has {Ho} heads, expected {Hq}")
-    ko_row = 0
+    Hk = k_row = ko_row = 0
     if k is not None:
+        Hk, k_row = _rows(k, "k", dtype, n, D, dev)
+        if k_out is None:
+            k_out = torch.empty((n, Hk, D), dtype=odt, device=dev)
         Ho, ko_row = _rows(k_out, "out k", odt, n, D, dev)
         if Ho != Hk:
             raise ValueError(f"out k has {Ho} heads, expected {Hk}")
@@ -450,7 +458,7 @@ def rotary_embed(q: torch.Tensor, k: Optional[torch.Tensor] = None, *, pairs: Se
         _need(pos, "pos", torch.int32, (n, 3), dev)
     nt, ny, nx = pairs
     qs, ks = fp8_scale
-    _call(dev, "rotary_embed", _ptr(q), q_row, _ptr(k), k_row, _ptr(q_out), qo_row, _ptr(k_out), ko_row, dt, n, Hq, Hk, D,
+    _call(dev, "rotary_embed", q.data_ptr(), q_row, _ptr(k), k_row, q_out.data_ptr(), qo_row, _ptr(k_out), ko_row, dt, n, Hq, Hk, D,
           _ptr(pos), t0, h, w, nt, ny, nx, theta, 1 if inverse else 0, qs, ks)
     return q_out, k_out
 
@@ -497,16 +505,20 @@ def attention_key_weight(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, kv
         out = torch.empty((H, Lk), dtype=torch.float32, device=dev)
     else:
         _need(out, "out", torch.float32, (H, Lk), dev)
-    size = (q.dtype, Lq, Lk, H, D, h, w, S if lam != 0 else 0, query_parts)
-    if _current_device() == dev.index:
-        nbytes = key_weight_workspace_size(*size)
-    else:
-        with torch.cuda.device(dev):
+    if workspace is not None:
+        _need(workspace, "workspace", torch.uint8, None, dev)
+    elif query_parts > 1 or Lq >= 256:  # below, the automatic choice is one part, which needs none
+        size = (q.dtype, Lq, Lk, H, D, h, w, S if lam != 0 else 0, query_parts)
+        if _current_device() == dev.index:
             nbytes = key_weight_workspace_size(*size)
-    ws = _workspace(nbytes, workspace, dev, "workspace")
+        else:
+            with torch.cuda.device(dev):
+                nbytes = key_weight_workspace_size(*size)
+        if nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     _call(dev, "attention_key_weight", _ptr(q), _ptr(k), _ptr(lse), dt, Lq, Lk, H, D, h, w, _ptr(kv_frame_slot), _ptr(corr_uv),
-          _ptr(corr_idx), S, softmax_scale, lam, sigma, _ptr(prev), decay, _ptr(out), query_parts, _ptr(ws),
-          ws.numel() if ws is not None else 0)
+          _ptr(corr_idx), S, softmax_scale, lam, sigma, _ptr(prev), decay, _ptr(out), query_parts,
+          _ptr(workspace), workspace.numel() if workspace is not None else 0)
     return out
 
 
@@ -543,9 +555,14 @@ def select_kept(weight: torch.Tensor, *, unit: int, keep: int, first: int = 0, l
         _need(idx, "out idx", torch.int32, (sets, keep), dev)
         if score is not None:
             _need(score, "out score", torch.float32, (sets, keep), dev)
-    ws = _workspace(select_workspace_size(sets, heads, n_units, unit), workspace, dev, "workspace")
-    _call(dev, "select_kept", _ptr(weight), sets, heads, n_units, unit, keep, first, last, _ptr(idx), _ptr(score), _ptr(ws),
-          ws.numel() if ws is not None else 0)
+    if workspace is not None:
+        _need(workspace, "workspace", torch.uint8, None, dev)
+    else:
+        nbytes = select_workspace_size(sets, heads, n_units, unit)
+        if nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _call(dev, "select_kept", weight.data_ptr(), sets, heads, n_units, unit, keep, first, last, idx.data_ptr(), _ptr(score),
+          _ptr(workspace), workspace.numel() if workspace is not None else 0)
     return idx, score
 
 

@@ -489,13 +489,28 @@ int64_t key_weight_items(const KeyWeightArgs& a) {
 }
 
 int32_t key_weight_parts(const KeyWeightArgs& a, int32_t cus) {
+    if (a.Lq < 256) return 1;  // a part's own start (its keys, its first queries) would cost more than it saves
     KeyWeightArgs b = a;
     b.parts = 1;
-    const int64_t items = key_weight_items(b), want = 4 * (int64_t)cus;
-    const int64_t tiles = (a.Lq + 31) / 32;
-    int64_t parts = (want + items - 1) / items;
-    parts = parts < tiles / 4 ? parts : tiles / 4;  // four query tiles a part at least
-    return (int32_t)(parts < 1 ? 1 : (parts > kKeyWeightMaxParts ? kKeyWeightMaxParts : parts));
+    const int64_t items = key_weight_items(b), tiles = (a.Lq + 31) / 32;
+    // Estimated time in steps of 64 queries: the rounds that the workgroups make on the chip's
+    // places, each as long as a part plus its start; a last round that leaves every
+    // compute unit at most one workgroup runs faster. With parts, the merge.
+    const bool f32 = a.type == kTypeF32;
+    const int64_t slots = (int64_t)cus * (f32 ? 3 : 2);
+    const double start = f32 ? 1.0 : 2.3, step_us = f32 ? 8.0 : (a.S > 0 ? 2.1 : 1.8);
+    double best = 0.0;
+    int32_t parts = 1;
+    for (int32_t p = 1; p <= 16 && tiles / p >= 4; ++p) {
+        const int64_t n = items * p, full = n / slots, rest = n % slots;
+        double t = ((double)full + (rest == 0 ? 0.0 : (rest <= cus ? 0.55 : 1.0))) * (start + (double)((tiles + p - 1) / p) / 2);
+        if (p > 1) t += (3.0 + (double)p * a.H * a.Lk * 4 / 4e6) / step_us;
+        if (p == 1 || t < best) {
+            best = t;
+            parts = p;
+        }
+    }
+    return parts;
 }
 
 hipError_t launch_key_weight(const KeyWeightArgs& a, hipStream_t stream) {
