@@ -361,22 +361,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
 }
 
 // ---------------------------------------------------------------------------
-// fp32 kernel.
+// fp32 kernel: v_mfma_f32_32x32x2_f32 (64 cycles each), so bound by the matrix
+// cores as long as nothing waits. A wave owns 32 keys; while the products of one
+// tile of 32 queries use up the query registers, the next tile's rows are loaded
+// into them from global memory (no LDS, no barrier: a tile's 4096 cycles at D =
+// 128 cover the loads), and the tile before has its exponentials and its bias, evaluated directly,
+// differences first, between the MFMAs.
 // ---------------------------------------------------------------------------
 
-// Row of D elements, lane half hh's share: MFMA step 4 g + i takes element 8 g + 4 hh + i.
-template <int D>
-struct Row {
-    floatx4 v[D / 8];
-    __device__ __forceinline__ void load(const uint8_t* row, int hh) {
-#pragma unroll
-        for (int j = 0; j < D / 8; ++j) v[j] = *reinterpret_cast<const floatx4*>(row + 32 * j + 16 * hh);
-    }
-};
-
 template <int D, bool kBias>
-__global__ __launch_bounds__(64 * kWaves) void key_weight_f32_kernel(KeyWeightArgs a, unsigned n_items) {
-    __shared__ float4 lds_row[kWaves][32];  // per query: u^ x, y, -gamma log2e or 0, -LSE log2e
+__global__ __launch_bounds__(64 * kWaves, 2) void key_weight_f32_kernel(KeyWeightArgs a, unsigned n_items) {
+    // per query of two tiles: u^ x, y, -lambda log2 e / (2 sigma^2) or 0, -LSE log2 e
+    __shared__ float4 lds_row[kWaves][2][32];
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -389,73 +385,120 @@ __global__ __launch_bounds__(64 * kWaves) void key_weight_f32_kernel(KeyWeightAr
     const int g = (int)(item % (unsigned)groups);
     const int hp = (int)(item / (unsigned)groups);
     const int hd = hp / a.parts, part = hp - hd * a.parts;
-    const int kb = g * kWaves + wave;
-    if (kb >= a.n_blocks) return;  // uniform per wave; no barrier below
-    const int frame = kb / a.frame_blocks;
-    const int in0 = (kb - frame * a.frame_blocks) * kKeys;  // first key within the frame
-    const int keys = min(kKeys, a.hw - in0);
-    const int64_t key0 = (int64_t)frame * a.hw + in0;
+    const KeyBlock kb = key_block(a, g * kWaves + wave, kBias);
+    if (kb.keys == 0) return;  // uniform per wave; no barrier below
 
-    constexpr int kSize = 4;
-    const int64_t row_bytes = (int64_t)a.H * D * kSize;
-    Row<D> kf, qf;
-    kf.load(static_cast<const uint8_t*>(a.k) + (key0 + min(n, keys - 1)) * row_bytes + (int64_t)hd * D * kSize, hh);
-    int s = -1;
-    if constexpr (kBias) {
-        s = a.slot[frame];
-        if (s >= a.S) s = -1;
+    constexpr int kG = D / 8;  // MFMA step 4 g + i takes element 8 g + 4 hh + i: 16 bytes of a row serve four
+    const int64_t row_bytes = (int64_t)a.H * D * 4;
+    const uint8_t* Qg = static_cast<const uint8_t*>(a.q) + (int64_t)hd * D * 4;
+    floatx4 kf[kG], qf[kG];
+    {
+        const uint8_t* row = static_cast<const uint8_t*>(a.k) + (kb.key0 + min(n, kb.keys - 1)) * row_bytes + (int64_t)hd * D * 4 + 16 * hh;
+#pragma unroll
+        for (int j = 0; j < kG; ++j) kf[j] = *reinterpret_cast<const floatx4*>(row + 32 * j);
     }
-    const int ky_i = (in0 + n) / a.w;
-    const float kx = (float)(in0 + n - ky_i * a.w) + 0.5f, ky = (float)ky_i + 0.5f;
+    const int ky_i = (kb.in0 + n) / a.w;
+    const float kx = (float)(kb.in0 + n - ky_i * a.w) + 0.5f, ky = (float)ky_i + 0.5f;
 
     const int n_tiles = (a.Lq + 31) / 32;
     const int t0 = (int)((int64_t)part * n_tiles / a.parts), t1 = (int)((int64_t)(part + 1) * n_tiles / a.parts);
-    float sum = 0.0f;
-    for (int t = t0; t < t1; ++t) {
-        const int q = t * 32 + n;
-        const int q_in = min(q, a.Lq - 1);
-        qf.load(static_cast<const uint8_t*>(a.q) + (int64_t)q_in * row_bytes + (int64_t)hd * D * kSize, hh);
-        float4 row = {0.0f, 0.0f, 0.0f, -INFINITY};
-        const float lse = a.lse[(int64_t)hd * a.Lq + q_in];
-        // a query past the end, or one without an LSE, has no weight to give
-        if (q < a.Lq && __builtin_isfinite(lse)) row.w = -lse * kLog2e;
-        if (kBias && s >= 0) {
-            const int64_t o = (int64_t)s * a.Lq + q_in;
-            const float2 u = reinterpret_cast<const float2*>(a.corr_uv)[o];
-            if (a.corr_idx[o] >= 0 && !__builtin_isnan(u.x)) {
-                row.x = u.x;
-                row.y = u.y;
-                row.z = -a.gamma2;
-            }
+    // query row of this lane in tile t; rows past the last repeat it
+    auto q_row = [&](int t) -> int { return min(t * 32 + n, a.Lq - 1); };
+    auto q_at = [&](int t) -> const uint8_t* { return Qg + q_row(t) * row_bytes + 16 * hh; };
+    // a tile's row data: loaded a tile ahead, made into what the exponentials take when its turn comes
+    float row_lse = 0.0f;
+    float2 row_u = {0.0f, 0.0f};
+    int row_i = -1;
+    auto fetch_row = [&](int t) {
+        const int q = q_row(t);
+        row_lse = a.lse[(int64_t)hd * a.Lq + q];
+        if (kBias && kb.slot >= 0) {
+            row_u = reinterpret_cast<const float2*>(a.corr_uv)[(int64_t)kb.slot * a.Lq + q];
+            row_i = a.corr_idx[(int64_t)kb.slot * a.Lq + q];
         }
-        __builtin_amdgcn_wave_barrier();
-        lds_row[wave][n] = row;  // both halves write the same
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        floatx16 acc = floatx16{0};
+    };
+    auto make_row = [&](int t) -> float4 {
+        float4 r = {0.0f, 0.0f, 0.0f, -INFINITY};
+        // a query past the end, or one without an LSE, has no weight to give
+        if (t * 32 + n < a.Lq && __builtin_isfinite(row_lse)) r.w = -row_lse * kLog2e;
+        if (kBias && row_i >= 0 && !__builtin_isnan(row_u.x)) {
+            r.x = row_u.x;
+            r.y = row_u.y;
+            r.z = -a.gamma2;
+        }
+        return r;
+    };
+    float sum = 0.0f, part_sum = 0.0f;
+    // the weight of logit i of a tile whose rows lie in `rows`; the next one's row is read meanwhile
+    float4 ahead;
+    auto unit = [&](const floatx16& acc, const float4* rows, int i) {
+        const float4 r = ahead;
+        if (i < 15) ahead = rows[acc_row(hh, i + 1)];
+        float x = fmaf(acc[i], a.c_log2, r.w);
+        if constexpr (kBias) {
+            const float dx = kx - r.x, dy = ky - r.y;
+            x = fmaf(r.z, dx * dx + dy * dy, x);
+        }
+        // a probability: at most 1, and 0 where the row has no LSE whatever its logits are
+        part_sum += fminf(fmaxf(__builtin_amdgcn_exp2f(x), 0.0f), 1.0f);
+        asm volatile("" : "+v"(part_sum));  // keeps it between its MFMAs
+    };
+    // tile t's products into `acc`, tile t - 1's exponentials from `before`
+    auto tile = [&](auto first_tag, int t, floatx16& acc, const floatx16& before) __attribute__((always_inline)) {
+        constexpr bool kFirst = decltype(first_tag)::value;
+        const float4* rows = lds_row[wave][(t - 1) & 1];
+        lds_row[wave][t & 1][n] = make_row(t);  // both halves write the same; this wave reads it in tile t + 1
+        if (t + 1 < t1) fetch_row(t + 1);
+        const uint8_t* next = q_at(t + 1 < t1 ? t + 1 : t);
+        acc = floatx16{0};
+        part_sum = 0.0f;
+        if constexpr (!kFirst) ahead = rows[acc_row(hh, 0)];
+        constexpr int kUnits = 16 / kG;  // logits of the tile before per four MFMAs
 #pragma unroll
-        for (int j = 0; j < D / 8; ++j)
+        for (int j = 0; j < kG; ++j) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(qf.v[j][i], kf.v[j][i], acc, 0, 0, 0);
-        float part_sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float4 r = lds_row[wave][acc_row(hh, i)];
-            float x = fmaf(acc[i], a.c_log2, r.w);
-            if (kBias && s >= 0) {
-                const float dx = kx - r.x, dy = ky - r.y;
-                if (r.z != 0.0f) x = fmaf(r.z, dx * dx + dy * dy, x);
+            for (int i = 0; i < 4; ++i) {
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(qf[j][i], kf[j][i], acc, 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (!kFirst) {
+                    if (i % (4 / kUnits) == 0) unit(before, rows, j * kUnits + i / (4 / kUnits));
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
-            // a probability: at most 1, and 0 where the row has no LSE whatever its logits are
-            part_sum += fminf(fmaxf(__builtin_amdgcn_exp2f(x), 0.0f), 1.0f);
+            qf[j] = *reinterpret_cast<const floatx4*>(next + 32 * j);
+            __builtin_amdgcn_sched_barrier(0);
         }
         sum += part_sum;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+    if (t0 < t1) {
+        floatx16 accA, accB;
+        const uint8_t* first = q_at(t0);
+#pragma unroll
+        for (int j = 0; j < kG; ++j) qf[j] = *reinterpret_cast<const floatx4*>(first + 32 * j);
+        fetch_row(t0);
+        // the keys are waited for here, not at their first use in the loop
+#pragma unroll
+        for (int j = 0; j < kG; ++j) asm volatile("" : "+v"(kf[j]));
+        tile(std::true_type{}, t0, accA, accB);
+        int t = t0 + 1;
+        for (; t + 1 < t1; t += 2) {
+            tile(std::false_type{}, t, accB, accA);
+            tile(std::false_type{}, t + 1, accA, accB);
+        }
+        if (t < t1) {
+            tile(std::false_type{}, t, accB, accA);
+            accA = accB;
+        }
+        part_sum = 0.0f;
+        ahead = lds_row[wave][(t1 - 1) & 1][acc_row(hh, 0)];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) unit(accA, lds_row[wave][(t1 - 1) & 1], i);
+        sum += part_sum;
     }
     const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
     sum = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-    if (hh == 0 && n < keys) {
-        const int64_t o = (int64_t)hd * a.Lk + key0 + n;
+    if (hh == 0 && n < kb.keys) {
+        const int64_t o = (int64_t)hd * a.Lk + kb.key0 + n;
         if (a.parts > 1) a.partial[(int64_t)part * a.H * a.Lk + o] = sum;
         else a.out[o] = a.prev ? fmaf(a.decay, a.prev[o], sum) : sum;
     }
