@@ -274,7 +274,7 @@ struct KeyWeightArgs {
     float gamma, gamma2;     // lambda / (2 sigma^2 softmax_scale); lambda log2 e / (2 sigma^2)
     float decay;
     int32_t parts;           // query parts
-    int32_t frame_blocks, n_blocks;  // key blocks per frame and per head
+    int32_t frame_blocks, n_blocks, wave_blocks;  // key blocks per frame, per head and per wave
 };
 constexpr int32_t kKeyWeightMaxParts = 64;
 void key_weight_plan(KeyWeightArgs& a);

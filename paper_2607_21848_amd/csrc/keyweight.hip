@@ -37,6 +37,9 @@ __device__ __forceinline__ int acc_row(int hh, int i) { return 8 * (i >> 2) + 4 
 // ---------------------------------------------------------------------------
 // bf16 and fp8 kernel.
 // ---------------------------------------------------------------------------
+template <int V>
+using Int = std::integral_constant<int, V>;
+
 constexpr int kD = 128;
 constexpr int kStep = 64;                    // queries of a step
 constexpr int kRowBytes = kD * 2;
@@ -68,6 +71,7 @@ __device__ __forceinline__ u32x4 wide(uint32_t a, uint32_t b) {
 
 // A block of 32 keys: where it is, and what its bias goes by.
 struct KeyBlock {
+    int frame;
     int64_t key0;
     int keys;     // of it within the frame; 0: no such block
     int slot;     // retrieved frame, -1: unbiased
@@ -75,13 +79,13 @@ struct KeyBlock {
 };
 __device__ __forceinline__ KeyBlock key_block(const KeyWeightArgs& a, int kb, bool bias) {
     KeyBlock b;
-    const int frame = kb / a.frame_blocks;
-    b.in0 = (kb - frame * a.frame_blocks) * kKeys;
+    b.frame = kb / a.frame_blocks;
+    b.in0 = (kb - b.frame * a.frame_blocks) * kKeys;
     b.keys = kb < a.n_blocks ? min(kKeys, a.hw - b.in0) : 0;
-    b.key0 = (int64_t)frame * a.hw + b.in0;
+    b.key0 = (int64_t)b.frame * a.hw + b.in0;
     b.slot = -1;
     if (bias && b.keys > 0) {
-        const int s = a.slot[frame];
+        const int s = __builtin_amdgcn_readfirstlane(a.slot[b.frame]);
         if (s >= 0 && s < a.S) b.slot = s;
     }
     return b;
@@ -91,6 +95,7 @@ template <bool kFp8, bool kBias>
 __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeightArgs a, unsigned n_items) {
     __shared__ __attribute__((aligned(256))) uint8_t lds_q[3 * kStepBytes];
     __shared__ floatx4 lds_row[3 * kStep / 4];  // -LSE log2 e of the step's queries
+    __shared__ u32x4 lds_bias[kBias ? 3 * kWaves : 1][2][kBias ? 64 : 1];  // [ring][frame][half of the step]
 
     const int tid = threadIdx.x;
     const int lane = tid & 63;
@@ -100,7 +105,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
     const unsigned item = xcd_item(block, n_items);
     if (block >= xcd_grid(n_items) || item >= n_items) return;  // grid padding (uniform, before any barrier)
     // item = (head, query part, group of key blocks)
-    const int groups = (a.n_blocks + 2 * kWaves - 1) / (2 * kWaves);
+    const int per_wave = a.wave_blocks, per_group = per_wave * kWaves;
+    const int groups = (a.n_blocks + per_group - 1) / per_group;
     const int g = (int)(item % (unsigned)groups);
     const int hp = (int)(item / (unsigned)groups);
     const int hd = hp / a.parts, part = hp - hd * a.parts;
@@ -118,27 +124,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
     constexpr int kLoads = kStep * kChunks / (64 * kWaves);
     u32x4 stage[kLoads];
     float stage_lse = 0.0f;
-    // offsets of a step's loads from its first row (below 2^30); a step that runs past the last row repeats that one
+    // A step that would run past the last query is moved back to end with it (its
+    // rows before q0 then have no weight to give again), so that the loads' offsets
+    // (below 2^30) are the same for every step; fewer queries than a step repeat the last.
+    const int last_base = max(0, a.Lq - kStep);
+    auto base_of = [&](int q0) -> int { return min(q0, last_base); };
     uint32_t off[kLoads];
-    auto chunk_off = [&](int i, int last) -> uint32_t {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
         const int e = tid + i * 64 * kWaves;
-        return (uint32_t)(min(e / kChunks, last) * (int)row_bytes + 16 * (e % kChunks));
-    };
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) off[i] = chunk_off(i, kStep);
+        off[i] = (uint32_t)(min(e / kChunks, a.Lq - 1) * (int)row_bytes + 16 * (e % kChunks));
+    }
+    const int my_query = min(lane, a.Lq - 1);
     auto fetch = [&](int q0) {
-        const uint8_t* base = Qg + q0 * row_bytes;
-        const float* lse = a.lse + (int64_t)hd * a.Lq + q0;
-        if (q0 + kStep <= a.Lq) {
+        const uint8_t* base = Qg + base_of(q0) * row_bytes;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) stage[i] = *reinterpret_cast<const u32x4*>(base + off[i]);
-            stage_lse = lse[lane];
-        } else {
-            const int last = a.Lq - 1 - q0;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) stage[i] = *reinterpret_cast<const u32x4*>(base + chunk_off(i, last));
-            stage_lse = lse[min(lane, last)];
-        }
+        for (int i = 0; i < kLoads; ++i) stage[i] = *reinterpret_cast<const u32x4*>(base + off[i]);
+        stage_lse = a.lse[(int64_t)hd * a.Lq + base_of(q0) + my_query];
+        __builtin_amdgcn_sched_barrier(0);
     };
     auto put = [&](int q0, int to, int to_row) {
 #pragma unroll
@@ -153,7 +156,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
             }
         }
         // a query past the end, or one without an LSE, has no weight to give
-        if (wave == 0) reinterpret_cast<float*>(lds_row + to_row)[lane] = q0 + lane < q_end && __builtin_isfinite(stage_lse) ? -stage_lse * kLog2e : -INFINITY;
+        const int q = base_of(q0) + lane;
+        __builtin_amdgcn_sched_barrier(0);  // the registers are loaded again only after this
+        if (wave == 0) reinterpret_cast<float*>(lds_row + to_row)[lane] = q >= q0 && q < q_end && __builtin_isfinite(stage_lse) ? -stage_lse * kLog2e : -INFINITY;
     };
     if (t0 < t1) fetch(t0 * 32);
 
@@ -164,7 +169,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
     const float cx = 0.5f * (float)a.w, cy = 0.5f * (float)a.h;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-        kb[b] = key_block(a, (g * kWaves + wave) * 2 + b, kBias);
+        kb[b] = key_block(a, b < per_wave ? g * per_group + wave * per_wave + b : a.n_blocks, kBias);
         const uint8_t* row = Kg + (kb[b].keys > 0 ? kb[b].key0 + min(n, kb[b].keys - 1) : 0) * row_bytes;
 #pragma unroll
         for (int j = 0; j < kD / 16; ++j) {
@@ -184,54 +189,48 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
             kbias[b] = as_bf16x8(u32x4{pack2(twice, twice), pack2(twice, ph), pack2(pm, pl), hh ? kOne : pack2(kOne, kOne)});
         }
     }
-    // Bias products: query side of a step's two halves, for each block's frame.
-    // A lane takes one of the step's 64 queries, evaluates both contraction halves
-    // (x terms for the first, y terms for the second) and one swap of wave
-    // halves hands each to the lanes of its half.
-    const int slot0 = kb[0].slot, slot1 = kb[1].slot;
-    float2 corr_u[2];
-    int corr_i[2];
+    // Bias products: the query side of each frame that the workgroup's blocks lie in (four
+    // at most, counted from its first block's) is made by one wave per frame, in
+    // LDS. A lane takes one of a step's 64 queries, evaluates both contraction halves
+    // (x terms for the first, y terms for the second), and one swap of wave halves
+    // hands each to the lanes of its half.
+    const int frame0 = g * per_group / a.frame_blocks;
+    const int last_block = min((g + 1) * per_group, a.n_blocks) - 1;
+    int made = -1;  // retrieved frame whose side this wave makes
+    if (kBias && frame0 + wave <= last_block / a.frame_blocks) {
+        const int s = a.slot[frame0 + wave];
+        if (s >= 0 && s < a.S) made = __builtin_amdgcn_readfirstlane(s);
+    }
+    float2 corr_u;
+    int corr_i;
     auto fetch_corr = [&](int q0) {
-        const int q = min(q0 + lane, a.Lq - 1);
-        if (slot0 >= 0) {
-            corr_u[0] = reinterpret_cast<const float2*>(a.corr_uv)[(int64_t)slot0 * a.Lq + q];
-            corr_i[0] = a.corr_idx[(int64_t)slot0 * a.Lq + q];
-        }
-        if (slot1 >= 0 && slot1 != slot0) {
-            corr_u[1] = reinterpret_cast<const float2*>(a.corr_uv)[(int64_t)slot1 * a.Lq + q];
-            corr_i[1] = a.corr_idx[(int64_t)slot1 * a.Lq + q];
-        }
+        if (made < 0) return;
+        const int64_t o = (int64_t)made * a.Lq + base_of(q0) + my_query;
+        corr_u = reinterpret_cast<const float2*>(a.corr_uv)[o];
+        corr_i = a.corr_idx[o];
     };
-    u32x4 qb[2][2];  // [block][half of the step]
-    auto query_bias = [&](float2 u, int idx, u32x4* out) {
-        const bool ok = idx >= 0 && !__builtin_isnan(u.x);
-        const float ux = ok ? u.x - cx : 0.0f, uy = ok ? u.y - cy : 0.0f;
+    auto make_bias = [&](int ring) {
+        if (made < 0) return;
+        const bool ok = corr_i >= 0 && !__builtin_isnan(corr_u.x);
+        const float ux = ok ? corr_u.x - cx : 0.0f, uy = ok ? corr_u.y - cy : 0.0f;
         uint32_t xh, xm, xl, yh, ym, yl, zh, zm, zl;
         split3(a.gamma * ux, xh, xm, xl);
         split3(a.gamma * uy, yh, ym, yl);
         split3(-a.gamma * (ux * ux + uy * uy), zh, zm, zl);
         const uint32_t one = ok ? kOne : 0;
         const u32x4 x = {pack2(xh, xm), pack2(xl, one), pack2(one, one), pack2(zh, zm)}, y = {pack2(yh, ym), pack2(yl, one), pack2(one, one), zl};
+        u32x4 half0, half1;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const auto s = __builtin_amdgcn_permlane32_swap(x[i], y[i], false, false);
-            out[0][i] = s[0];
-            out[1][i] = s[1];
+            half0[i] = s[0];
+            half1[i] = s[1];
         }
+        lds_bias[ring * kWaves + wave][0][lane] = half0;
+        lds_bias[ring * kWaves + wave][1][lane] = half1;
     };
-    auto make_bias = [&]() {
-        if (slot0 >= 0) query_bias(corr_u[0], corr_i[0], qb[0]);
-        if (slot1 >= 0) {
-            if (slot1 == slot0) {
-                qb[1][0] = qb[0][0];
-                qb[1][1] = qb[0][1];
-            } else {
-                query_bias(corr_u[1], corr_i[1], qb[1]);
-            }
-        }
-    };
-#pragma unroll
-    for (int b = 0; b < 2; ++b) qb[b][0] = qb[b][1] = u32x4{0, 0, 0, 0};
+    // this wave's blocks: whether they are biased, and by which wave's side
+    const int bias0 = kb[0].slot < 0 ? -1 : kb[0].frame - frame0, bias1 = kb[1].slot < 0 ? -1 : kb[1].frame - frame0;
 
     const int n_steps = (t1 - t0 + 1) / 2;
     const int q_begin = t0 * 32;
@@ -239,25 +238,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
     floatx16 accA[2], accB[2];
     u32x4 qf[4];     // queries of the next four products
     floatx4 rc[2];   // row constants of the next eight exponentials
-    // chunk 2 j + hh of this lane's row: 32 j has no bit in common with a row's start
-    const int lane_at = chunk_at(n, hh);
-    auto read_q = [&](int rows, int j) { qf[j & 3] = *reinterpret_cast<const u32x4*>(lds_q + ((rows + lane_at) ^ (32 * j))); };
-    auto read_rc = [&](int row, int i) { rc[i & 1] = lds_row[row + 2 * i + hh]; };
-    auto first = [&](floatx16* acc, int half) {  // the products start from the bias, or from 0
+    int q_lane[kD / 16];  // chunk 2 j + hh of this lane's row
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            acc[b] = floatx16{0};
-            if constexpr (kBias) acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qb[b][half]), kbias[b], acc[b], 0, 0, 0);
-        }
-    };
+    for (int j = 0; j < kD / 16; ++j) q_lane[j] = chunk_at(n, 2 * j + hh);
+    auto read_q = [&](int rows, int j) { qf[j & 3] = *reinterpret_cast<const u32x4*>(lds_q + q_lane[j] + rows); };
+    auto read_rc = [&](int row, int i) { rc[i & 1] = lds_row[hh + row + 2 * i]; };
     constexpr int kHalf = 32 * kRowBytes, kRow = kStep / 4;  // half a step's rows; a step's row constants, in quads
 
     // Half of a step: the products of the next half (rows) beside the exponentials of
     // this one (row constants row), one MFMA to two of them. Operands are read four
     // products, row constants eight exponentials ahead: past the end, those of the half after.
-    auto do_half = [&](auto last_tag, floatx16* cur, floatx16* next, int next_half, int rows, int rows_after, int row, int row_after) __attribute__((always_inline)) {
+    auto do_half = [&](auto last_tag, floatx16* cur, floatx16* next, auto rows, auto rows_after, auto row, auto row_after,
+                       auto bias_ring, auto bias_half) __attribute__((always_inline)) {
         constexpr bool kLast = decltype(last_tag)::value;
-        if constexpr (!kLast) first(next, next_half);
+        if constexpr (!kLast) next[0] = next[1] = floatx16{0};
+        u32x4 qb[2];
         float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
         for (int j = 0; j < kD / 16; ++j) {
@@ -284,6 +279,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
             }
             asm volatile("" : "+v"(s1));
             if constexpr (!kLast) read_q(j < 4 ? rows : rows_after, (j + 4) & 7);
+            if constexpr (kBias && !kLast) {
+                if (j == 0) {
+                    if (bias0 >= 0) qb[0] = lds_bias[bias_ring * kWaves + bias0][bias_half][lane];  // uniform per wave
+                    if (bias1 >= 0) qb[1] = lds_bias[bias_ring * kWaves + bias1][bias_half][lane];
+                }
+                if (j == 4) {
+                    if (bias0 >= 0) next[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qb[0]), kbias[0], next[0], 0, 0, 0);
+                    if (bias1 >= 0) next[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qb[1]), kbias[1], next[1], 0, 0, 0);
+                }
+            }
             if (j & 1) {
                 if (j < 4) read_rc(row, (j >> 1) + 2);
                 else if constexpr (!kLast) read_rc(row_after, (j >> 1) - 2);
@@ -298,9 +303,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
         put(q_begin, 0, 0);
         if constexpr (kBias) {
             fetch_corr(q_begin);
-            make_bias();
+            make_bias(0);
         }
-        if (n_steps > 1) fetch(q_begin + kStep);
+        fetch(q_begin + kStep);
+        if constexpr (kBias) fetch_corr(q_begin + kStep);
         // the keys are waited for here: at their first use below the wait would drain the
         // next step's query loads too, every time round the loop
 #pragma unroll
@@ -310,7 +316,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < 4; ++j) read_q(0, j);
-        first(accA, 0);
+        accA[0] = accA[1] = floatx16{0};
+        if constexpr (kBias) {
+            if (bias0 >= 0) accA[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(lds_bias[bias0][0][lane]), kbias[0], accA[0], 0, 0, 0);
+            if (bias1 >= 0) accA[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(lds_bias[bias1][0][lane]), kbias[1], accA[1], 0, 0, 0);
+        }
 #pragma unroll
         for (int j = 0; j < kD / 16; ++j) {
 #pragma unroll
@@ -319,34 +329,41 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
         }
         read_rc(0, 0);
         read_rc(0, 1);
-        if (n_steps > 1) put(q_begin + kStep, kStepBytes, kRow);
-        if (n_steps > 2) fetch(q_begin + 2 * kStep);
-        if (kBias && n_steps > 1) fetch_corr(q_begin + kStep);
+        put(q_begin + kStep, kStepBytes, kRow);
+        fetch(q_begin + 2 * kStep);
+        if constexpr (kBias) {
+            make_bias(1);
+            fetch_corr(q_begin + 2 * kStep);
+        }
         __syncthreads();
         // At the top of step s: accA holds the logits of its first half, qf the first queries of
         // its second, buffer s + 1 the next step, the stage registers the loads of step s + 2
         // (buffers s mod 3).
-        int q0 = 0, q1 = kStepBytes, q2 = 2 * kStepBytes, r0 = 0, r1 = kRow, r2 = 2 * kRow;
-        for (int s = 0; s + 1 < n_steps; ++s) {
-            do_half(std::false_type{}, accA, accB, 1, q0 + kHalf, q1, r0, r0 + kRow / 2);
-            if (s + 2 < n_steps) put(q_begin + (s + 2) * kStep, q2, r2);
-            if (s + 3 < n_steps) fetch(q_begin + (s + 3) * kStep);
-            if constexpr (kBias) {
-                make_bias();  // of step s + 1
-                if (s + 2 < n_steps) fetch_corr(q_begin + (s + 2) * kStep);
+        // (ring: s mod 3, and the two behind it)
+        auto step = [&](int s, auto ring0, auto ring1, auto ring2) __attribute__((always_inline)) {
+            do_half(std::false_type{}, accA, accB, ring0 * kStepBytes + kHalf, ring1 * kStepBytes, ring0 * kRow, ring0 * kRow + kRow / 2, ring0, 1);
+            if (s + 2 < n_steps) {
+                put(q_begin + (s + 2) * kStep, ring2 * kStepBytes, ring2 * kRow);
+                fetch(q_begin + (s + 3) * kStep);  // past the last step: in bounds, for nothing
+                if constexpr (kBias) {
+                    make_bias(ring2);
+                    fetch_corr(q_begin + (s + 3) * kStep);
+                }
             }
-            do_half(std::false_type{}, accB, accA, 0, q1, q1 + kHalf, r0 + kRow / 2, r1);
+            do_half(std::false_type{}, accB, accA, ring1 * kStepBytes, ring1 * kStepBytes + kHalf, ring0 * kRow + kRow / 2, ring1 * kRow, ring1, 0);
             __syncthreads();
-            const int qt = q0, rt = r0;
-            q0 = q1;
-            q1 = q2;
-            q2 = qt;
-            r0 = r1;
-            r1 = r2;
-            r2 = rt;
+        };
+        // three steps at a time, so that the ring's addresses are constants
+        int s = 0;
+        for (; s + 3 < n_steps; s += 3) {
+            step(s, Int<0>{}, Int<1>{}, Int<2>{});
+            step(s + 1, Int<1>{}, Int<2>{}, Int<0>{});
+            step(s + 2, Int<2>{}, Int<0>{}, Int<1>{});
         }
-        do_half(std::false_type{}, accA, accB, 1, q0 + kHalf, q0, r0, r0 + kRow / 2);
-        do_half(std::true_type{}, accB, accA, 0, 0, 0, r0 + kRow / 2, 0);
+        for (int r = 0; s + 1 < n_steps; ++s, ++r) step(s, r, r == 2 ? 0 : r + 1, r == 0 ? 2 : r - 1);
+        const int ring = s % 3, q0 = ring * kStepBytes, r0 = ring * kRow;
+        do_half(std::false_type{}, accA, accB, q0 + kHalf, q0, r0, r0 + kRow / 2, ring, 1);
+        do_half(std::true_type{}, accB, accA, 0, 0, r0 + kRow / 2, 0, 0, 0);
     }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
@@ -524,10 +541,12 @@ void key_weight_plan(KeyWeightArgs& a) {
     }
     a.frame_blocks = (a.hw + kKeys - 1) / kKeys;
     a.n_blocks = a.frame_blocks * (a.Lk / a.hw);
+    // a wave takes two blocks; where frames are single blocks, one, so that a workgroup meets four biased frames at most
+    a.wave_blocks = a.type == kTypeF32 || (a.S > 0 && a.frame_blocks == 1) ? 1 : 2;
 }
 
 int64_t key_weight_items(const KeyWeightArgs& a) {
-    const int per_group = a.type == kTypeF32 ? kWaves : 2 * kWaves;  // key blocks of a workgroup
+    const int per_group = a.wave_blocks * kWaves;  // key blocks of a workgroup
     return ((int64_t)a.n_blocks + per_group - 1) / per_group * a.H * a.parts;
 }
 
