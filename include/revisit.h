@@ -484,6 +484,7 @@ int rotary_embed(const void* q, int64_t q_row, const void* k, int64_t k_row,
  *
  *   q, k, dtype, Lq, Lk, H, D, h, w, kv_frame_slot, corr_uv, corr_idx, S,
  *   softmax_scale, lambda, sigma  as for biased_chunk_attention, with its limits
+ *                (and Lq <= 2^30)
  *   lse          [H][Lq] fp32
  *   prev         nullable [H][Lk] fp32 (NULL: nothing is added; may be out itself)
  *   decay        finite

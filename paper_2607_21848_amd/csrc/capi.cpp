@@ -690,6 +690,7 @@ int prepare_key_weight(const char* fn, int32_t dtype, int32_t Lq, int32_t Lk, in
     const int st = check_attention_shape(fn, dtype, Lq, Lk, H, D, 0);
     if (st != REVISIT_OK) return st;
     if (h < 1 || w < 1 || S < 0) return fail(REVISIT_ERR_SHAPE, "%s: need h, w >= 1, S >= 0", fn);
+    if (Lq > (1 << 30)) return fail(REVISIT_ERR_SHAPE, "%s: Lq=%d above 2^30", fn, Lq);
     const int64_t hw = (int64_t)h * w;
     if (Lk % hw != 0) return fail(REVISIT_ERR_SHAPE, "%s: Lk=%d not a multiple of h*w=%lld", fn, Lk, (long long)hw);
     if (Lk / hw > kMaxFrames) return fail(REVISIT_ERR_SHAPE, "%s: more than %d KV frames", fn, kMaxFrames);

@@ -28,6 +28,7 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kWaves = 4;
+constexpr int kFewQueries = 32;
 constexpr int kKeys = 32;  // keys of a block
 constexpr int kTypeF32 = 2, kTypeFp8 = 3;  // REVISIT_F32, REVISIT_FP8_QK
 
@@ -67,6 +68,29 @@ __device__ __forceinline__ u32x4 wide(uint32_t a, uint32_t b) {
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, decltype(hi)::value));
     };
     return u32x4{pair(a, std::false_type{}), pair(a, std::true_type{}), pair(b, std::false_type{}), pair(b, std::true_type{})};
+}
+
+// Bias products. With centred token coordinates a = u_k - c, u' = u^ - c:
+//     (lambda / scale) B = 2 gamma a.u' - gamma |a|^2 - gamma |u'|^2,
+// each fp32 factor as three bf16 pieces (the half-integers a are exact in one), x terms in the first
+// half of the contraction and y terms in the second:
+//     key side    [2 a (x3), -gamma a^2 (3 pieces), 1, 1 or 0]
+//     query side  [gamma u' (3 pieces), 1, 1, 1, -gamma |u'|^2 (2 pieces in the first half, the third in the second)]
+// A query without a correspondence (ok false) has zeros.
+__device__ __forceinline__ u32x4 key_side(float gamma, int t, int w, float cx, float cy, int hh) {
+    const int ky = t / w;
+    const float at = hh ? ((float)ky + 0.5f) - cy : ((float)(t - ky * w) + 0.5f) - cx;
+    const uint32_t twice = bf16_bits(2.0f * at);
+    uint32_t ph, pm, pl;
+    split3(-gamma * (at * at), ph, pm, pl);
+    return u32x4{pack2(twice, twice), pack2(twice, ph), pack2(pm, pl), hh ? kOne : pack2(kOne, kOne)};
+}
+__device__ __forceinline__ u32x4 query_side(float gamma, float ux, float uy, bool ok, int hh) {
+    uint32_t ah, am, al, zh, zm, zl;
+    split3(gamma * (hh ? uy : ux), ah, am, al);
+    split3(-gamma * (ux * ux + uy * uy), zh, zm, zl);
+    const uint32_t one = ok ? kOne : 0;
+    return u32x4{pack2(ah, am), pack2(al, one), pack2(one, one), hh ? zl : pack2(zh, zm)};
 }
 
 // A block of 32 keys: where it is, and what its bias goes by.
@@ -181,12 +205,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
             }
         }
         if constexpr (kBias) {
-            const int t = kb[b].in0 + n, ky = t / a.w;
-            const float at = hh ? ((float)ky + 0.5f) - cy : ((float)(t - ky * a.w) + 0.5f) - cx;
-            const uint32_t twice = bf16_bits(2.0f * at);  // exact: a half-integer below 128
-            uint32_t ph, pm, pl;
-            split3(-a.gamma * (at * at), ph, pm, pl);
-            kbias[b] = as_bf16x8(u32x4{pack2(twice, twice), pack2(twice, ph), pack2(pm, pl), hh ? kOne : pack2(kOne, kOne)});
+            kbias[b] = as_bf16x8(key_side(a.gamma, kb[b].in0 + n, a.w, cx, cy, hh));
         }
     }
     // Bias products: the query side of each frame that the workgroup's blocks lie in (four
@@ -378,6 +397,79 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
 }
 
 // ---------------------------------------------------------------------------
+// bf16 and fp8 kernel for at most kFewQueries queries, one tile: the keys are read
+// once and nothing is used twice, so it is bound by HBM, and small waves (32 keys
+// each, no ring, no barrier) keep more loads in flight than the kernel above. One
+// query of 12 heads against 37440 keys (115 MB, not in any cache): 26.9 us, 4.4 TB/s,
+// against 30 there; for 60 queries in two tiles it would take 42 us against 34.
+// All loads leave before the first is waited for (35 us without that), and the
+// keys pass through L1 (non-temporal loads, 46 us: each line is met by four of them).
+// ---------------------------------------------------------------------------
+template <bool kFp8, bool kBias>
+__global__ __launch_bounds__(64 * kWaves) void key_weight_few_kernel(KeyWeightArgs a, unsigned n_items) {
+    __shared__ floatx4 lds_row[kWaves][8];  // -LSE log2 e of the queries, for each wave its own
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int hh = lane >> 5, n = lane & 31;
+    const unsigned block = row_block();
+    const unsigned item = xcd_item(block, n_items);
+    if (block >= xcd_grid(n_items) || item >= n_items) return;  // grid padding (uniform)
+    const int groups = (a.n_blocks + kWaves - 1) / kWaves;
+    const int hd = (int)(item / (unsigned)groups);
+    const KeyBlock kb = key_block(a, (int)(item - (unsigned)hd * (unsigned)groups) * kWaves + wave, kBias);
+    if (kb.keys == 0) return;  // uniform per wave; no barrier below
+    // A lane's share of a row in loads of 16 bytes; of an fp8 load the first eight elements
+    // go to one MFMA step and the rest to the next (any numbering of the contraction
+    // will do that queries and keys share).
+    constexpr int kSize = kFp8 ? 1 : 2, kLoads = kD * kSize / 32;
+    const int64_t row_bytes = (int64_t)a.H * kD * kSize;
+    const uint8_t* kr = static_cast<const uint8_t*>(a.k) + (kb.key0 + min(n, kb.keys - 1)) * row_bytes + (int64_t)hd * kD * kSize + 16 * hh;
+    const uint8_t* Qg = static_cast<const uint8_t*>(a.q) + (int64_t)hd * kD * kSize + 16 * hh;
+    u32x4 kraw[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) kraw[j] = *reinterpret_cast<const u32x4*>(kr + 32 * j);
+    auto operand = [](const u32x4* raw, int step) -> bf16x8 {
+        if constexpr (kFp8) return as_bf16x8(wide(raw[step >> 1][2 * (step & 1)], raw[step >> 1][2 * (step & 1) + 1]));
+        else return as_bf16x8(raw[step]);
+    };
+    bf16x8 kbias = as_bf16x8(u32x4{0, 0, 0, 0});
+    const float cx = 0.5f * (float)a.w, cy = 0.5f * (float)a.h;
+    if (kBias && kb.slot >= 0) kbias = as_bf16x8(key_side(a.gamma, kb.in0 + n, a.w, cx, cy, hh));
+    float sum = 0.0f;
+    if (a.Lq > 0) {
+        const int q = min(n, a.Lq - 1);
+        const uint8_t* qr = Qg + q * row_bytes;
+        u32x4 qraw[kLoads];
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) qraw[j] = *reinterpret_cast<const u32x4*>(qr + 32 * j);
+        const float lse = a.lse[(int64_t)hd * a.Lq + q];
+        __builtin_amdgcn_sched_barrier(0);  // all loads leave before the first is waited for
+        floatx16 acc = floatx16{0};
+        if (kBias && kb.slot >= 0) {
+            const int64_t o = (int64_t)kb.slot * a.Lq + q;
+            const float2 u = reinterpret_cast<const float2*>(a.corr_uv)[o];
+            const bool ok = a.corr_idx[o] >= 0 && !__builtin_isnan(u.x);
+            const float ux = ok ? u.x - cx : 0.0f, uy = ok ? u.y - cy : 0.0f;
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(query_side(a.gamma, ux, uy, ok, hh)), kbias, acc, 0, 0, 0);
+        }
+        // a query past the end, or one without an LSE, has no weight to give; both halves write the same
+        reinterpret_cast<float*>(lds_row[wave])[n] = n < a.Lq && __builtin_isfinite(lse) ? -lse * kLog2e : -INFINITY;
+#pragma unroll
+        for (int j = 0; j < kD / 16; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(qraw, j), operand(kraw, j), acc, 0, 0, 0);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            sum += fminf(fmaxf(__builtin_amdgcn_exp2f(fmaf(acc[i], a.c_log2, lds_row[wave][2 * (i >> 2) + hh][i & 3])), 0.0f), 1.0f);
+    }
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+    sum = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    if (hh == 0 && n < kb.keys) {
+        const int64_t o = (int64_t)hd * a.Lk + kb.key0 + n;
+        a.out[o] = a.prev ? fmaf(a.decay, a.prev[o], sum) : sum;
+    }
+}
+
+// ---------------------------------------------------------------------------
 // fp32 kernel: v_mfma_f32_32x32x2_f32 (64 cycles each), so bound by the matrix
 // cores as long as nothing waits. A wave owns 32 keys; while the products of one
 // tile of 32 queries use up the query registers, the next tile's rows are loaded
@@ -531,6 +623,8 @@ __global__ __launch_bounds__(256) void key_weight_merge(const float* partial, co
     out[i] = prev ? fmaf(decay, prev[i], sum) : sum;
 }
 
+bool few_queries(const KeyWeightArgs& a) { return a.Lq <= kFewQueries; }
+
 }  // namespace
 
 void key_weight_plan(KeyWeightArgs& a) {
@@ -542,7 +636,7 @@ void key_weight_plan(KeyWeightArgs& a) {
     a.frame_blocks = (a.hw + kKeys - 1) / kKeys;
     a.n_blocks = a.frame_blocks * (a.Lk / a.hw);
     // a wave takes two blocks; where frames are single blocks, one, so that a workgroup meets four biased frames at most
-    a.wave_blocks = a.type == kTypeF32 || (a.S > 0 && a.frame_blocks == 1) ? 1 : 2;
+    a.wave_blocks = a.type == kTypeF32 || few_queries(a) || (a.S > 0 && a.frame_blocks == 1) ? 1 : 2;
 }
 
 int64_t key_weight_items(const KeyWeightArgs& a) {
@@ -583,6 +677,9 @@ hipError_t launch_key_weight(const KeyWeightArgs& a, hipStream_t stream) {
     if (a.type == kTypeF32) {
         if (a.D == 64) bias ? go(key_weight_f32_kernel<64, true>) : go(key_weight_f32_kernel<64, false>);
         else bias ? go(key_weight_f32_kernel<128, true>) : go(key_weight_f32_kernel<128, false>);
+    } else if (few_queries(a)) {
+        if (a.type == kTypeFp8) bias ? go(key_weight_few_kernel<true, true>) : go(key_weight_few_kernel<true, false>);
+        else bias ? go(key_weight_few_kernel<false, true>) : go(key_weight_few_kernel<false, false>);
     } else if (a.type == kTypeFp8) {
         bias ? go(key_weight_bf16_kernel<true, true>) : go(key_weight_bf16_kernel<true, false>);
     } else {
