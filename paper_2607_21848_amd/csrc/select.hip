@@ -250,37 +250,27 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     });
 }
 
-// Up to 64 units to choose from: one wave per set, a unit per lane, which is kept if fewer than m
-// come before it.
+// Up to 64 units: one wave per set, a unit per lane. Of those to choose from one is
+// kept if fewer than m come before it.
 template <bool kSums>
 __global__ __launch_bounds__(64) void select_few_kernel(SelectArgs a) {
     const int lane = threadIdx.x;
     const int64_t n_items = (int64_t)a.sets * a.n_units;
-    const int64_t base = (int64_t)blockIdx.x * a.n_units;
-    int32_t* out = a.out_idx + (int64_t)blockIdx.x * a.keep;
-    float* out_score = a.out_score ? a.out_score + (int64_t)blockIdx.x * a.keep : nullptr;
-    auto score = [&](int64_t unit) -> float { return score_of<kSums>(a, base + unit, n_items); };
-    const int from_last = a.n_units - a.last, open = from_last - a.first, m = a.keep - a.first - a.last;
-    const bool have = lane < open;
-    const uint32_t k = have ? ordered(score(a.first + lane)) : 0;
+    const float x = lane < a.n_units ? score_of<kSums>(a, (int64_t)blockIdx.x * a.n_units + lane, n_items) : 0.0f;
+    const uint32_t k = ordered(x);
+    const int hi = a.n_units - a.last, m = a.keep - a.first - a.last;
     int before = 0;
-    for (int j = 0; j < open; ++j) {
+    for (int j = a.first; j < hi; ++j) {
         const uint32_t y = __builtin_amdgcn_readlane(k, j);
         before += y > k || (y == k && j < lane) ? 1 : 0;
     }
-    const bool keep = have && before < m;
+    const bool open = lane >= a.first && lane < hi;
+    const bool keep = lane < a.n_units && (!open || before < m);
     const uint64_t kept = __ballot(keep);
     if (keep) {
-        const int o = a.first + __popcll(kept & (((uint64_t)1 << lane) - 1));
-        out[o] = a.first + lane;
-        if (out_score) out_score[o] = number(k);
-    }
-    // the protected ends
-    for (int i = lane; i < a.first + a.last; i += 64) {
-        const int u = i < a.first ? i : from_last + (i - a.first);
-        const int o = i < a.first ? i : a.keep - a.last + (i - a.first);
-        out[o] = u;
-        if (out_score) out_score[o] = score(u);
+        const int64_t o = (int64_t)blockIdx.x * a.keep + __popcll(kept & (((uint64_t)1 << lane) - 1));
+        a.out_idx[o] = lane;
+        if (a.out_score) a.out_score[o] = x;
     }
 }
 
@@ -321,7 +311,7 @@ hipError_t launch_select(const SelectArgs& a, hipStream_t stream) {
         if (e != hipSuccess) return e;
     }
     const int64_t open = (int64_t)a.n_units - a.first - a.last;
-    if (open <= 64) {
+    if (a.n_units <= 64) {
         if (sums) hipLaunchKernelGGL(select_few_kernel<true>, dim3(a.sets), dim3(64), 0, stream, a);
         else hipLaunchKernelGGL(select_few_kernel<false>, dim3(a.sets), dim3(64), 0, stream, a);
         return hipGetLastError();
