@@ -375,21 +375,20 @@ def pool_token_depth(depth: torch.Tensor, p: int, out: Optional[torch.Tensor] = 
     return out
 
 
-def _call(dev: torch.device, name: str, *args):
-    """lib().<name>(*args, stream) on dev and its current stream, whichever device is current."""
-    index = dev.index
+def _call(index: int, name: str, *args):
+    """lib().<name>(*args, stream) on device `index` and its current stream, whichever device is current."""
     if _current_device() == index:
-        st = getattr(lib(), name)(*args, _raw_stream(index))
+        st = getattr(_lib._LIB or lib(), name)(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(dev):
+        with torch.cuda.device(index):
             st = getattr(lib(), name)(*args, _raw_stream(index))
     if st:
         _lib.check(name, st)
 
 
-def _rows(t: torch.Tensor, name: str, dtype: torch.dtype, n: int, D: int, device):
+def _rows(t: torch.Tensor, name: str, dtype: torch.dtype, n: int, D: int, index: int):
     """A [n, H, D] tensor of whole rows (heads and elements contiguous, rows any distance apart); its H and row stride."""
-    if isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == device:
+    if isinstance(t, torch.Tensor) and t.dtype == dtype and t.get_device() == index:
         shape = t.shape
         if len(shape) == 3 and shape[0] == n and shape[2] == D:
             H = shape[1]
@@ -402,8 +401,8 @@ def _rows(t: torch.Tensor, name: str, dtype: torch.dtype, n: int, D: int, device
         raise ValueError(f"{name} has shape {tuple(shape)}, expected ({n}, heads, {D})")
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{index}")
     raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
 
 
@@ -426,7 +425,7 @@ def rotary_embed(q: torch.Tensor, k: Optional[torch.Tensor] = None, *, pairs: Se
     where the type stays. Returns (q_out, k_out); k_out is None without k."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor [n, heads, D]")
-    dev, dtype = q.device, q.dtype
+    dtype, index = q.dtype, q.get_device()
     n, _, D = q.shape
     q_out = k_out = None
     if out is not None:
@@ -438,27 +437,27 @@ def rotary_embed(q: torch.Tensor, k: Optional[torch.Tensor] = None, *, pairs: Se
     if dt is None:
         raise TypeError(f"q must be bfloat16 or float32 with outputs of the same type, or bfloat16 with float8_e4m3fn "
                         f"(got {dtype} and {odt})")
-    if not q.is_cuda:
-        raise ValueError(f"q must be a GPU tensor (got {dev}); there is no CPU path")
-    Hq, q_row = _rows(q, "q", dtype, n, D, dev)
+    if index < 0:
+        raise ValueError(f"q must be a GPU tensor (got {q.device}); there is no CPU path")
+    Hq, q_row = _rows(q, "q", dtype, n, D, index)
     if q_out is None:
-        q_out = torch.empty((n, Hq, D), dtype=odt, device=dev)
-    Ho, qo_row = _rows(q_out, "out q", odt, n, D, dev)
+        q_out = torch.empty((n, Hq, D), dtype=odt, device=q.device)
+    Ho, qo_row = _rows(q_out, "out q", odt, n, D, index)
     if Ho != Hq:
         raise ValueError(f"out q has {Ho} heads, expected {Hq}")
     Hk = k_row = ko_row = 0
     if k is not None:
-        Hk, k_row = _rows(k, "k", dtype, n, D, dev)
+        Hk, k_row = _rows(k, "k", dtype, n, D, index)
         if k_out is None:
-            k_out = torch.empty((n, Hk, D), dtype=odt, device=dev)
-        Ho, ko_row = _rows(k_out, "out k", odt, n, D, dev)
+            k_out = torch.empty((n, Hk, D), dtype=odt, device=q.device)
+        Ho, ko_row = _rows(k_out, "out k", odt, n, D, index)
         if Ho != Hk:
             raise ValueError(f"out k has {Ho} heads, expected {Hk}")
     if pos is not None:
-        _need(pos, "pos", torch.int32, (n, 3), dev)
+        _need(pos, "pos", torch.int32, (n, 3), q.device)
     nt, ny, nx = pairs
     qs, ks = fp8_scale
-    _call(dev, "rotary_embed", q.data_ptr(), q_row, _ptr(k), k_row, q_out.data_ptr(), qo_row, _ptr(k_out), ko_row, dt, n, Hq, Hk, D,
+    _call(index, "rotary_embed", q.data_ptr(), q_row, _ptr(k), k_row, q_out.data_ptr(), qo_row, _ptr(k_out), ko_row, dt, n, Hq, Hk, D,
           _ptr(pos), t0, h, w, nt, ny, nx, theta, 1 if inverse else 0, qs, ks)
     return q_out, k_out
 
@@ -516,7 +515,7 @@ def attention_key_weight(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, kv
                 nbytes = key_weight_workspace_size(*size)
         if nbytes:
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    _call(dev, "attention_key_weight", _ptr(q), _ptr(k), _ptr(lse), dt, Lq, Lk, H, D, h, w, _ptr(kv_frame_slot), _ptr(corr_uv),
+    _call(dev.index, "attention_key_weight", _ptr(q), _ptr(k), _ptr(lse), dt, Lq, Lk, H, D, h, w, _ptr(kv_frame_slot), _ptr(corr_uv),
           _ptr(corr_idx), S, softmax_scale, lam, sigma, _ptr(prev), decay, _ptr(out), query_parts,
           _ptr(workspace), workspace.numel() if workspace is not None else 0)
     return out
@@ -561,7 +560,7 @@ def select_kept(weight: torch.Tensor, *, unit: int, keep: int, first: int = 0, l
         nbytes = select_workspace_size(sets, heads, n_units, unit)
         if nbytes:
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    _call(dev, "select_kept", weight.data_ptr(), sets, heads, n_units, unit, keep, first, last, idx.data_ptr(), _ptr(score),
+    _call(dev.index, "select_kept", weight.data_ptr(), sets, heads, n_units, unit, keep, first, last, idx.data_ptr(), _ptr(score),
           _ptr(workspace), workspace.numel() if workspace is not None else 0)
     return idx, score
 
@@ -612,7 +611,7 @@ def compact_kv(src_k: torch.Tensor, src_v: torch.Tensor, sel: torch.Tensor, dst_
                 raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({L}, {H}, tokens)")
         cols, dst_cols = weight.shape[2], out_weight.shape[2]
         n_units = min(n_units, cols // unit)
-    _call(dev, "compact_kv", _ptr(src_k), _ptr(src_v), rows, _ptr(sel), sel.shape[1], sel.shape[2], unit, n_units, _ptr(dst_k),
+    _call(dev.index, "compact_kv", _ptr(src_k), _ptr(src_v), rows, _ptr(sel), sel.shape[1], sel.shape[2], unit, n_units, _ptr(dst_k),
           _ptr(dst_v), dst_rows, dst_row0, _ptr(weight), cols, _ptr(out_weight), dst_cols, L, dt, H, D, _ptr(src_pos), dst_pos,
           frames_per_unit, rope_t_pairs, rope_theta)
 

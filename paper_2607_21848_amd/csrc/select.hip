@@ -109,12 +109,16 @@ __device__ __forceinline__ float score_of(const SelectArgs& a, int64_t item, int
 constexpr int kSelWaves = 16;
 constexpr int kSelThreads = 64 * kSelWaves;
 constexpr int kBins = 4096;
+constexpr int kList = 2048;
 
 // kHeld: units of a lane, held in registers; 0: any number, read again in every pass.
 template <int kHeld, bool kSums>
 __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     __shared__ unsigned hist[kBins];
-    __shared__ unsigned wave_sum[kSelWaves], found[2], wave_gt[kSelWaves], wave_eq[kSelWaves];
+    __shared__ unsigned wave_sum[kSelWaves], found[3], wave_gt[kSelWaves], wave_eq[kSelWaves];
+    __shared__ uint32_t list_key[kList];  // the units in the first digit's bin, where they fit, and their waves
+    __shared__ uint8_t list_wave[kList];
+    __shared__ unsigned list_n;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t n_items = (int64_t)a.sets * a.n_units;
@@ -165,13 +169,15 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     // the m-th largest: its leading digits so far, and how many equal to it are taken
     uint32_t prefix = 0, mask = 0;
     unsigned want = m;
+    bool listed = false;
+    if (tid == 0) list_n = 0;
 #pragma unroll
     for (int digit = 0; digit < 3; ++digit) {
         constexpr int kShift[3] = {20, 10, 0};
         const int shift = kShift[digit], bins = digit == 0 ? kBins : 1024;
         for (int b = tid; b < bins; b += kSelThreads) hist[b] = 0;
         __syncthreads();
-        each([&](int, bool have, uint32_t k) {
+        auto count_in = [&](int, bool have, uint32_t k) {
             const bool in = have && (k & mask) == prefix;
             const uint64_t who = __ballot(in);
             if (who == 0) return;
@@ -183,7 +189,12 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
             } else if (in) {
                 atomicAdd(&hist[bin], 1u);
             }
-        });
+        };
+        if (digit > 0 && listed) {
+            for (unsigned i = tid - lane; i < list_n; i += kSelThreads) count_in(0, i + lane < list_n, list_key[(i + lane) % kList]);
+        } else {
+            each(count_in);
+        }
         __syncthreads();
         // each thread takes some bins, from the highest down: the one where the count from above reaches `want`
         const int per = bins / kSelThreads;
@@ -208,6 +219,7 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
             if (b < per && above < want && above + own[b] >= want) {
                 found[0] = (unsigned)(bins - 1 - (tid * per + b));
                 found[1] = want - above;
+                found[2] = own[b];
             }
             above += own[b];
         }
@@ -215,30 +227,70 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
         prefix |= __builtin_amdgcn_readfirstlane(found[0]) << shift;
         mask |= (unsigned)(bins - 1) << shift;
         want = __builtin_amdgcn_readfirstlane(found[1]);
+        if (digit == 0 && __builtin_amdgcn_readfirstlane(found[2]) <= kList) {
+            // few enough in the bin: they are listed, and the waves count what lies above it
+            listed = true;
+            unsigned gt = 0;
+            each([&](int, bool have, uint32_t k) {
+                const uint32_t top = k & mask;
+                gt += __popcll(__ballot(have && top > prefix));
+                const bool in = have && top == prefix;
+                const uint64_t who = __ballot(in);
+                if (who == 0) return;
+                unsigned at = 0;
+                const int leader = __builtin_ctzll(who);
+                if (lane == leader) at = atomicAdd(&list_n, (unsigned)__popcll(who));
+                at = __builtin_amdgcn_readlane(at, leader) + __popcll(who & (((uint64_t)1 << lane) - 1));
+                if (in) {
+                    list_key[at] = k;
+                    list_wave[at] = (uint8_t)wave;
+                }
+            });
+            if (lane == 0) {
+                wave_gt[wave] = gt;
+                wave_eq[wave] = 0;
+            }
+        }
     }
 
     // what each wave keeps: above the threshold, and equal to it
-    unsigned gt = 0, eq = 0;
-    each([&](int, bool have, uint32_t k) {
-        gt += __popcll(__ballot(have && k > prefix));
-        eq += __popcll(__ballot(have && k == prefix));
-    });
-    if (lane == 0) {
-        wave_gt[wave] = gt;
-        wave_eq[wave] = eq;
+    if (listed) {
+        for (unsigned i = tid; i < list_n; i += kSelThreads) {
+            const uint32_t k = list_key[i];
+            if (k > prefix) atomicAdd(&wave_gt[list_wave[i]], 1u);
+            else if (k == prefix) atomicAdd(&wave_eq[list_wave[i]], 1u);
+        }
+    } else {
+        unsigned gt = 0, eq = 0;
+        each([&](int, bool have, uint32_t k) {
+            gt += __popcll(__ballot(have && k > prefix));
+            eq += __popcll(__ballot(have && k == prefix));
+        });
+        if (lane == 0) {
+            wave_gt[wave] = gt;
+            wave_eq[wave] = eq;
+        }
     }
     __syncthreads();
-    unsigned at = a.first, eq_before = 0;
-    for (int w = 0; w < wave; ++w) {
-        at += wave_gt[w];
-        eq_before += wave_eq[w];
+    unsigned at = a.first, eq_before = 0, eq_all = 0;
+    for (int w = 0; w < kSelWaves; ++w) {
+        if (w < wave) {
+            at += wave_gt[w];
+            eq_before += wave_eq[w];
+        }
+        eq_all += wave_eq[w];
     }
     at += min(eq_before, want);
+    const bool all_equal = eq_all == want;  // nothing equal to the threshold is left out
     const uint64_t below = ((uint64_t)1 << lane) - 1;
     each([&](int i, bool have, uint32_t k) {
-        const bool same = have && k == prefix;
-        const uint64_t same_mask = __ballot(same);
-        const bool keep = (have && k > prefix) || (same && eq_before + __popcll(same_mask & below) < want);
+        bool keep = have && k >= prefix;
+        if (!all_equal) {
+            const bool same = have && k == prefix;
+            const uint64_t same_mask = __ballot(same);
+            if (same) keep = eq_before + __popcll(same_mask & below) < want;
+            eq_before += __popcll(same_mask);
+        }
         const uint64_t keep_mask = __ballot(keep);
         if (keep) {
             const unsigned o = at + __popcll(keep_mask & below);
@@ -246,7 +298,6 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
             if (out_score) out_score[o] = number(k);
         }
         at += __popcll(keep_mask);
-        eq_before += __popcll(same_mask);
     });
 }
 
