@@ -479,8 +479,8 @@ int rotary_embed(const void* q, int64_t q_row, const void* k, int64_t k_row,
  * with the logits A of biased_chunk_attention (bias included) and the LSE that
  * call returned for the same q, k, bias and scale, or for a larger set of keys
  * of which k is a part. A summand is a probability: one above 1, which such an LSE
- * gives by rounding only, counts as 1. A query whose LSE is not finite (no key had
- * weight, or NaN) adds nothing.
+ * gives by rounding only, counts as 1, and one that is NaN as 0. A query whose LSE
+ * is not finite (no key had weight, or NaN) adds nothing.
  *
  *   q, k, dtype, Lq, Lk, H, D, h, w, kv_frame_slot, corr_uv, corr_idx, S,
  *   softmax_scale, lambda, sigma  as for biased_chunk_attention, with its limits

@@ -557,6 +557,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_f32_kernel(KeyWeigh
         constexpr bool kFirst = decltype(first_tag)::value;
         const float4* rows = lds_row[wave][(t - 1) & 1];
         lds_row[wave][t & 1][n] = make_row(t);  // both halves write the same; this wave reads it in tile t + 1
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (t + 1 < t1) fetch_row(t + 1);
         const uint8_t* next = q_at(t + 1 < t1 ? t + 1 : t);
         acc = floatx16{0};

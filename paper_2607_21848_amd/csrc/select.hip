@@ -30,12 +30,12 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kScoreBlock = 256;
 
-// Sum of `count` vectors of VEC weights per unit, G lanes a unit; grid.y = head part.
+// Sum of a unit's weights in vectors of VEC, G lanes a unit; grid.z = head part.
 template <int G, int VEC>
 __global__ __launch_bounds__(kScoreBlock) void unit_score_kernel(SelectArgs a, int64_t n_items, double inv_len) {
     constexpr int kUnits = kScoreBlock / G;
-    const int64_t item = (int64_t)blockIdx.x * kUnits + threadIdx.x / G;
-    const int part = blockIdx.y;
+    const int64_t item = (int64_t)row_block() * kUnits + threadIdx.x / G;
+    const int part = blockIdx.z;
     const int h0 = (int)((int64_t)part * a.heads / a.splits), h1 = (int)((int64_t)(part + 1) * a.heads / a.splits);
     const int64_t row = (int64_t)a.n_units * a.unit;
     double sum = 0.0;
@@ -329,8 +329,9 @@ template <int G, int VEC>
 void launch_scores(const SelectArgs& a, hipStream_t stream) {
     const int64_t n = (int64_t)a.sets * a.n_units;
     const int64_t blocks = (n + kScoreBlock / G - 1) / (kScoreBlock / G);
-    hipLaunchKernelGGL((unit_score_kernel<G, VEC>), dim3((unsigned)blocks, a.splits), dim3(kScoreBlock), 0, stream, a, n,
-                       1.0 / (a.unit / VEC));
+    dim3 grid = grid_rows((unsigned)blocks);
+    grid.z = (unsigned)a.splits;
+    hipLaunchKernelGGL((unit_score_kernel<G, VEC>), grid, dim3(kScoreBlock), 0, stream, a, n, 1.0 / (a.unit / VEC));
 }
 
 }  // namespace

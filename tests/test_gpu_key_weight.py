@@ -161,6 +161,21 @@ def test_retrieved_slots_out_of_range_are_unbiased():
     assert (off <= _tolerance(q, k, A, lse, h, w, 0.1, 1.0, 2.0, D, True)).all()
 
 
+@pytest.mark.parametrize("dtype,D,Lq", [(torch.bfloat16, 128, 90), (torch.bfloat16, 128, 7), (torch.float32, 64, 90), (torch.float8_e4m3fn, 128, 90)])
+def test_a_part_of_the_keys_under_the_whole_lse(dtype, D, Lq):
+    """The LSE may be that of more keys than are weighed: a range of frames gets the weights it has among all."""
+    h, w, H, nf, S = 5, 7, 2, 9, 4
+    q, k, slot, uv, idx = _case(14, dtype, Lq, nf, h, w, H, D, S)
+    A, lse = _oracle(q, k, slot, uv, idx, h, w, D ** -0.5, 1.0, 2.0)
+    tol = _tolerance(q, k, A, lse, h, w, D ** -0.5, 1.0, 2.0, D, True)
+    frames = slice(2, 7)
+    rows = slice(2 * h * w, 7 * h * w)
+    got = rv.attention_key_weight(q, k[rows].contiguous(), torch.from_numpy(lse).to(DEV), slot[frames].contiguous(), uv, idx, h=h, w=w,
+                                  softmax_scale=D ** -0.5, lam=1.0, sigma=2.0)
+    off = np.abs(got.double().cpu().numpy() - OC.key_weight(A, lse)[:, rows])
+    assert (off <= tol[:, rows]).all(), (off / tol[:, rows]).max()
+
+
 def test_refusals_of_the_binding():
     q, k, slot, uv, idx = _case(13, torch.bfloat16, 40, 4, 4, 5, 2, 128, 2)
     lse = torch.zeros(2, 40, device=DEV)
