@@ -21,6 +21,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "internal.h"
 
 namespace revisit {
@@ -110,10 +112,17 @@ constexpr int kSelWaves = 16;
 constexpr int kSelThreads = 64 * kSelWaves;
 constexpr int kBins = 4096;
 constexpr int kList = 2048;
+constexpr size_t kSelLds = 128 << 10;  // of keys: with the histogram and the list below a compute unit's 160 KiB
 
-// kHeld: units of a lane, held in registers; 0: any number, read again in every pass.
-template <int kHeld, bool kSums>
+// lanes below this one in a ballot
+__device__ __forceinline__ unsigned lanes_below(uint64_t who) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+}
+
+// kLds: the keys to choose from lie in LDS after the first sweep; else every sweep reads the scores again.
+template <bool kLds, bool kSums>
 __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
+    extern __shared__ uint32_t keys[];  // kLds: [waves][rounds][64]
     __shared__ unsigned hist[kBins];
     __shared__ unsigned wave_sum[kSelWaves], found[3], wave_gt[kSelWaves], wave_eq[kSelWaves];
     __shared__ uint32_t list_key[kList];  // the units in the first digit's bin, where they fit, and their waves
@@ -140,30 +149,37 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     const int64_t open = (int64_t)from_last - a.first;
     const int rounds = (int)((open + kSelThreads - 1) / kSelThreads);
     const int64_t start = (int64_t)wave * rounds * 64, u0 = a.first + start;
-    int count = (int)max((int64_t)0, min((int64_t)rounds * 64, open - start));
-    uint32_t held[kHeld ? kHeld : 1];
-    if constexpr (kHeld > 0) {
-        float x[kHeld];
+    const int count = (int)max((int64_t)0, min((int64_t)rounds * 64, open - start));
+    // f(unit's place in the wave, whether there is one, its key) for this lane's units, eight
+    // rounds at a time with their loads in flight together
+    auto sweep = [&](auto first_tag, auto f) {
+        constexpr bool kFirst = decltype(first_tag)::value;
+        constexpr int kBatch = 8;
+        for (int r0 = 0; r0 < count; r0 += 64 * kBatch) {
+            uint32_t k[kBatch];
+            auto batch = [&](auto full_tag) __attribute__((always_inline)) {
+                constexpr bool kFull = decltype(full_tag)::value;
+                if constexpr (kLds && !kFirst) {
 #pragma unroll
-        for (int r = 0; r < kHeld; ++r) x[r] = r * 64 + lane < count ? score(u0 + r * 64 + lane) : 0.0f;
+                    for (int j = 0; j < kBatch; ++j) k[j] = kFull || r0 + j * 64 < count ? keys[start + r0 + j * 64 + lane] : 0u;
+                } else {
+                    float x[kBatch];
 #pragma unroll
-        for (int r = 0; r < kHeld; ++r) held[r] = ordered(x[r]);
-    }
-    // f(unit's place in the wave, whether there is one, its key) for this lane's units
-    auto each = [&](auto f) {
-        if constexpr (kHeld > 0) {
+                    for (int j = 0; j < kBatch; ++j) x[j] = kFull || r0 + j * 64 + lane < count ? score(u0 + r0 + j * 64 + lane) : 0.0f;
 #pragma unroll
-            for (int r = 0; r < kHeld; ++r) {
-                if (r * 64 < count) f(r * 64 + lane, r * 64 + lane < count, held[r]);  // uniform
-            }
-        } else {
-            for (int r = 0; r * 64 < count; ++r) {
-                const int i = r * 64 + lane;
-                f(i, i < count, i < count ? ordered(score(u0 + i)) : 0u);
-            }
+                    for (int j = 0; j < kBatch; ++j) {
+                        k[j] = ordered(x[j]);
+                        if (kLds && (kFull || r0 + j * 64 < count)) keys[start + r0 + j * 64 + lane] = k[j];
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j) {
+                    if (kFull || r0 + j * 64 < count) f(r0 + j * 64 + lane, kFull || r0 + j * 64 + lane < count, k[j]);
+                }
+            };
+            if (r0 + 64 * kBatch <= count) batch(std::true_type{});  // uniform
+            else batch(std::false_type{});
         }
-        // what a pass has found out about the lanes is found out again by the next, not kept
-        asm volatile("" : "+s"(count));
     };
 
     // the m-th largest: its leading digits so far, and how many equal to it are taken
@@ -192,8 +208,10 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
         };
         if (digit > 0 && listed) {
             for (unsigned i = tid - lane; i < list_n; i += kSelThreads) count_in(0, i + lane < list_n, list_key[(i + lane) % kList]);
+        } else if (digit == 0) {
+            sweep(std::true_type{}, count_in);
         } else {
-            each(count_in);
+            sweep(std::false_type{}, count_in);
         }
         __syncthreads();
         // each thread takes some bins, from the highest down: the one where the count from above reaches `want`
@@ -231,7 +249,7 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
             // few enough in the bin: they are listed, and the waves count what lies above it
             listed = true;
             unsigned gt = 0;
-            each([&](int, bool have, uint32_t k) {
+            sweep(std::false_type{}, [&](int, bool have, uint32_t k) {
                 const uint32_t top = k & mask;
                 gt += __popcll(__ballot(have && top > prefix));
                 const bool in = have && top == prefix;
@@ -240,7 +258,7 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
                 unsigned at = 0;
                 const int leader = __builtin_ctzll(who);
                 if (lane == leader) at = atomicAdd(&list_n, (unsigned)__popcll(who));
-                at = __builtin_amdgcn_readlane(at, leader) + __popcll(who & (((uint64_t)1 << lane) - 1));
+                at = __builtin_amdgcn_readlane(at, leader) + lanes_below(who);
                 if (in) {
                     list_key[at] = k;
                     list_wave[at] = (uint8_t)wave;
@@ -262,7 +280,7 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
         }
     } else {
         unsigned gt = 0, eq = 0;
-        each([&](int, bool have, uint32_t k) {
+        sweep(std::false_type{}, [&](int, bool have, uint32_t k) {
             gt += __popcll(__ballot(have && k > prefix));
             eq += __popcll(__ballot(have && k == prefix));
         });
@@ -282,18 +300,17 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     }
     at += min(eq_before, want);
     const bool all_equal = eq_all == want;  // nothing equal to the threshold is left out
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    each([&](int i, bool have, uint32_t k) {
+    sweep(std::false_type{}, [&](int i, bool have, uint32_t k) {
         bool keep = have && k >= prefix;
         if (!all_equal) {
             const bool same = have && k == prefix;
             const uint64_t same_mask = __ballot(same);
-            if (same) keep = eq_before + __popcll(same_mask & below) < want;
+            if (same) keep = eq_before + lanes_below(same_mask) < want;
             eq_before += __popcll(same_mask);
         }
         const uint64_t keep_mask = __ballot(keep);
         if (keep) {
-            const unsigned o = at + __popcll(keep_mask & below);
+            const unsigned o = at + lanes_below(keep_mask);
             out[o] = (int32_t)(u0 + i);
             if (out_score) out_score[o] = number(k);
         }
@@ -369,12 +386,10 @@ hipError_t launch_select(const SelectArgs& a, hipStream_t stream) {
         return hipGetLastError();
     }
     const dim3 grid(a.sets), block(kSelThreads);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
-    const int64_t held = (open + kSelThreads - 1) / kSelThreads;  // units of a lane
-    if (held <= 1) sums ? go(select_kernel<1, true>) : go(select_kernel<1, false>);
-    else if (held <= 8) sums ? go(select_kernel<8, true>) : go(select_kernel<8, false>);
-    else if (held <= 40) sums ? go(select_kernel<40, true>) : go(select_kernel<40, false>);
-    else sums ? go(select_kernel<0, true>) : go(select_kernel<0, false>);
+    auto go = [&](auto kernel, size_t bytes) { hipLaunchKernelGGL(kernel, grid, block, bytes, stream, a); };
+    const size_t lds = (size_t)((open + kSelThreads - 1) / kSelThreads) * kSelThreads * sizeof(uint32_t);
+    if (lds <= kSelLds) sums ? go(select_kernel<true, true>, lds) : go(select_kernel<true, false>, lds);
+    else sums ? go(select_kernel<false, true>, 0) : go(select_kernel<false, false>, 0);
     return hipGetLastError();
 }
 
