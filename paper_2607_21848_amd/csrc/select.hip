@@ -96,15 +96,27 @@ __device__ __forceinline__ float number(uint32_t k) {
     return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
 }
 
-// score of an item: a set's unit
-template <bool kSums>
-__device__ __forceinline__ float score_of(const SelectArgs& a, int64_t item, int64_t n_items) {
-    if constexpr (kSums) {
-        double s = 0.0;
-        for (int p = 0; p < a.splits; ++p) s += a.unit_sum[(int64_t)p * n_items + item];
-        return (float)s;
-    } else {
+// Where a unit's score comes from: it is its one weight, the sums of unit_score_kernel, or (units of
+// one token) the sum over the heads here.
+enum class Score { kWeight, kSums, kHeads };
+
+// score of unit u of a set
+template <Score kFrom>
+__device__ __forceinline__ float score_of(const SelectArgs& a, int64_t set, int64_t u) {
+    const int64_t item = set * a.n_units + u;
+    if constexpr (kFrom == Score::kWeight) {
         return a.weight[item];
+    } else {
+        double s = 0.0;
+        if constexpr (kFrom == Score::kSums) {
+            const int64_t n_items = (int64_t)a.sets * a.n_units;
+            for (int p = 0; p < a.splits; ++p) s += a.unit_sum[(int64_t)p * n_items + item];
+        } else {
+            const float* w = a.weight + set * a.heads * a.n_units + u;
+#pragma unroll 1
+            for (int h = 0; h < a.heads; ++h) s += (double)w[(int64_t)h * a.n_units];
+        }
+        return (float)s;
     }
 }
 
@@ -120,7 +132,7 @@ __device__ __forceinline__ unsigned lanes_below(uint64_t who) {
 }
 
 // kLds: the keys to choose from lie in LDS after the first sweep; else every sweep reads the scores again.
-template <bool kLds, bool kSums>
+template <bool kLds, Score kFrom>
 __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     extern __shared__ uint32_t keys[];  // kLds: [waves][rounds][64]
     __shared__ unsigned hist[kBins];
@@ -130,11 +142,9 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     __shared__ unsigned list_n;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t n_items = (int64_t)a.sets * a.n_units;
-    const int64_t base = (int64_t)blockIdx.x * a.n_units;
     int32_t* out = a.out_idx + (int64_t)blockIdx.x * a.keep;
     float* out_score = a.out_score ? a.out_score + (int64_t)blockIdx.x * a.keep : nullptr;
-    auto score = [&](int64_t unit) -> float { return score_of<kSums>(a, base + unit, n_items); };
+    auto score = [&](int64_t unit) -> float { return score_of<kFrom>(a, blockIdx.x, unit); };
     // the protected ends
     const int from_last = a.n_units - a.last;
     for (int i = tid; i < a.first + a.last; i += kSelThreads) {
@@ -164,8 +174,19 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
                     for (int j = 0; j < kBatch; ++j) k[j] = kFull || r0 + j * 64 < count ? keys[start + r0 + j * 64 + lane] : 0u;
                 } else {
                     float x[kBatch];
+                    if constexpr (kFrom == Score::kHeads) {
+                        double s[kBatch] = {};
+                        const float* w = a.weight + (int64_t)blockIdx.x * a.heads * a.n_units + u0 + r0 + lane;
+#pragma unroll 1
+                        for (int h = 0; h < a.heads; ++h, w += a.n_units)
 #pragma unroll
-                    for (int j = 0; j < kBatch; ++j) x[j] = kFull || r0 + j * 64 + lane < count ? score(u0 + r0 + j * 64 + lane) : 0.0f;
+                            for (int j = 0; j < kBatch; ++j) s[j] += kFull || r0 + j * 64 + lane < count ? (double)w[j * 64] : 0.0;
+#pragma unroll
+                        for (int j = 0; j < kBatch; ++j) x[j] = (float)s[j];
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < kBatch; ++j) x[j] = kFull || r0 + j * 64 + lane < count ? score(u0 + r0 + j * 64 + lane) : 0.0f;
+                    }
 #pragma unroll
                     for (int j = 0; j < kBatch; ++j) {
                         k[j] = ordered(x[j]);
@@ -318,13 +339,9 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     });
 }
 
-// Up to 64 units: one wave per set, a unit per lane. Of those to choose from one is
-// kept if fewer than m come before it.
-template <bool kSums>
-__global__ __launch_bounds__(64) void select_few_kernel(SelectArgs a) {
-    const int lane = threadIdx.x;
-    const int64_t n_items = (int64_t)a.sets * a.n_units;
-    const float x = lane < a.n_units ? score_of<kSums>(a, (int64_t)blockIdx.x * a.n_units + lane, n_items) : 0.0f;
+// Up to 64 units, whose scores x the lanes of one wave hold: of those to choose from
+// one is kept if fewer than m come before it.
+__device__ __forceinline__ void select_few(const SelectArgs& a, int64_t set, int lane, float x) {
     const uint32_t k = ordered(x);
     const int hi = a.n_units - a.last, m = a.keep - a.first - a.last;
     int before = 0;
@@ -336,10 +353,45 @@ __global__ __launch_bounds__(64) void select_few_kernel(SelectArgs a) {
     const bool keep = lane < a.n_units && (!open || before < m);
     const uint64_t kept = __ballot(keep);
     if (keep) {
-        const int64_t o = (int64_t)blockIdx.x * a.keep + __popcll(kept & (((uint64_t)1 << lane) - 1));
+        const int64_t o = set * a.keep + lanes_below(kept);
         a.out_idx[o] = lane;
         if (a.out_score) a.out_score[o] = x;
     }
+}
+
+template <Score kFrom>
+__global__ __launch_bounds__(64) void select_few_kernel(SelectArgs a) {
+    const int lane = threadIdx.x;
+    select_few(a, blockIdx.x, lane, lane < a.n_units ? score_of<kFrom>(a, blockIdx.x, lane) : 0.0f);
+}
+
+// The same from the weights: wave w sums units w, w + 16, ...
+__global__ __launch_bounds__(kSelThreads) void select_few_sums_kernel(SelectArgs a, double inv_unit) {
+    __shared__ float score[64];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int64_t row = (int64_t)a.n_units * a.unit;
+    const float* w = a.weight + (int64_t)blockIdx.x * a.heads * row;
+    const int total = a.heads * a.unit;  // at most kFewWeights
+    for (int u = wave; u < a.n_units; u += kSelWaves) {
+        double sum = 0.0;
+        for (int e0 = lane; e0 < total; e0 += 64 * 8) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int e = e0 + 64 * k;
+                const int h = (int)(((double)e + 0.5) * inv_unit);
+                v[k] = e < total ? w[h * row + (int64_t)u * a.unit + (e - h * a.unit)] : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += (double)v[k];
+        }
+#pragma unroll
+        for (int k = 32; k > 0; k /= 2) sum += __shfl_xor(sum, k);
+        if (lane == 0) score[u] = (float)sum;
+    }
+    __syncthreads();
+    if (wave == 0) select_few(a, blockIdx.x, lane, lane < a.n_units ? score[lane] : 0.0f);
 }
 
 template <int G, int VEC>
@@ -353,24 +405,43 @@ void launch_scores(const SelectArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-bool select_sums(const SelectArgs& a) { return a.heads > 1 || a.unit > 1; }
+// How a choice gets its scores. Where a set has few weights its own workgroup adds
+// them up: one launch instead of two (11 us instead of 14 for one set of 12 heads and 18 units of 130
+// tokens), which a set of more weights would spend reading them on one compute unit.
+constexpr int64_t kFewWeights = 1 << 15;
+enum class Plan { kWeights, kOwnHeads, kOwnUnits, kSums };
+
+namespace {
+Plan plan_of(const SelectArgs& a) {
+    if (a.heads == 1 && a.unit == 1) return Plan::kWeights;
+    if ((int64_t)a.n_units * a.unit <= kFewWeights / a.heads) {
+        if (a.unit == 1) return Plan::kOwnHeads;
+        if (a.n_units <= 64) return Plan::kOwnUnits;
+    }
+    return Plan::kSums;
+}
+}  // namespace
 
 // Head parts of the scores: where there are fewer long units than two workgroups per
 // compute unit of a large chip, the heads share them out.
 int32_t select_splits(const SelectArgs& a) {
     const int64_t n = (int64_t)a.sets * a.n_units;
-    if (!select_sums(a) || n == 0 || n >= 512 || (int64_t)a.heads * a.unit < 8192) return 1;
+    if (plan_of(a) != Plan::kSums || n == 0 || n >= 512 || (int64_t)a.heads * a.unit < 8192) return 1;
     const int64_t want = (512 + n - 1) / n;
     return (int32_t)(want < a.heads ? want : a.heads);
 }
 
 size_t select_workspace_bytes(const SelectArgs& a) {
-    return select_sums(a) ? (size_t)a.sets * a.n_units * select_splits(a) * sizeof(double) : 0;
+    return plan_of(a) == Plan::kSums ? (size_t)a.sets * a.n_units * select_splits(a) * sizeof(double) : 0;
 }
 
 hipError_t launch_select(const SelectArgs& a, hipStream_t stream) {
-    const bool sums = select_sums(a);
-    if (sums) {
+    const Plan plan = plan_of(a);
+    if (plan == Plan::kOwnUnits) {
+        hipLaunchKernelGGL(select_few_sums_kernel, dim3(a.sets), dim3(kSelThreads), 0, stream, a, 1.0 / a.unit);
+        return hipGetLastError();
+    }
+    if (plan == Plan::kSums) {
         const bool vec = a.unit % 4 == 0 && (uintptr_t)a.weight % 16 == 0;
         if (a.unit >= 512) vec ? launch_scores<256, 4>(a, stream) : launch_scores<256, 1>(a, stream);
         else if (a.unit >= 64) vec ? launch_scores<64, 4>(a, stream) : launch_scores<64, 1>(a, stream);
@@ -379,17 +450,21 @@ hipError_t launch_select(const SelectArgs& a, hipStream_t stream) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const int64_t open = (int64_t)a.n_units - a.first - a.last;
-    if (a.n_units <= 64) {
-        if (sums) hipLaunchKernelGGL(select_few_kernel<true>, dim3(a.sets), dim3(64), 0, stream, a);
-        else hipLaunchKernelGGL(select_few_kernel<false>, dim3(a.sets), dim3(64), 0, stream, a);
-        return hipGetLastError();
-    }
-    const dim3 grid(a.sets), block(kSelThreads);
-    auto go = [&](auto kernel, size_t bytes) { hipLaunchKernelGGL(kernel, grid, block, bytes, stream, a); };
-    const size_t lds = (size_t)((open + kSelThreads - 1) / kSelThreads) * kSelThreads * sizeof(uint32_t);
-    if (lds <= kSelLds) sums ? go(select_kernel<true, true>, lds) : go(select_kernel<true, false>, lds);
-    else sums ? go(select_kernel<false, true>, 0) : go(select_kernel<false, false>, 0);
+    auto run = [&](auto from) {
+        constexpr Score kFrom = decltype(from)::value;
+        if (a.n_units <= 64) {
+            hipLaunchKernelGGL(select_few_kernel<kFrom>, dim3(a.sets), dim3(64), 0, stream, a);
+            return;
+        }
+        const int64_t open = (int64_t)a.n_units - a.first - a.last;
+        const size_t lds = (size_t)((open + kSelThreads - 1) / kSelThreads) * kSelThreads * sizeof(uint32_t);
+        // (the few weights of kHeads always fit)
+        if (kFrom == Score::kHeads || lds <= kSelLds) hipLaunchKernelGGL((select_kernel<true, kFrom>), dim3(a.sets), dim3(kSelThreads), lds, stream, a);
+        else if constexpr (kFrom != Score::kHeads) hipLaunchKernelGGL((select_kernel<false, kFrom>), dim3(a.sets), dim3(kSelThreads), 0, stream, a);
+    };
+    if (plan == Plan::kWeights) run(std::integral_constant<Score, Score::kWeight>{});
+    else if (plan == Plan::kOwnHeads) run(std::integral_constant<Score, Score::kHeads>{});
+    else run(std::integral_constant<Score, Score::kSums>{});
     return hipGetLastError();
 }
 

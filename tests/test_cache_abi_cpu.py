@@ -95,11 +95,25 @@ def _select(L, **kw):
     (dict(n=1 << 20, unit=1 << 12), 2), (dict(keep=101), 4), (dict(keep=-1), 4), (dict(keep=8), 4), (dict(first=-1), 4),
     (dict(last=-1), 4), (dict(first=2**31 - 1, last=2**31 - 1), 4), (dict(weight=NULL), 1), (dict(idx=NULL), 1),
     (dict(weight=ctypes.c_void_p(0x10002)), 2),
-    (dict(heads=12), 2), (dict(heads=12, ws_bytes=1 << 20), 1), (dict(unit=3, ws=ODD, ws_bytes=1 << 20), 2),
+    # sums of 12 x 10000 weights a set go through the workspace: none, too small, NULL, misaligned
+    (dict(heads=12, n=10000), 2), (dict(heads=12, n=10000, ws=FAKE, ws_bytes=4 * 10000 * 8 - 1), 2),
+    (dict(heads=12, n=10000, ws_bytes=1 << 20), 1), (dict(n=30000, unit=3, ws=ODD, ws_bytes=1 << 30), 2),
 ])
 def test_select_rejects(L, kw, status):
     assert _select(L, **kw) == status
     assert "select_kept" in _lib.last_error()
+
+
+def test_select_workspace(L):
+    n = ctypes.c_size_t(7)
+    size = lambda *a: (L.rc_select_workspace_size(*a, ctypes.byref(n)), n.value)  # noqa: E731
+    assert size(96, 1, 37440, 1) == (0, 0)            # the weights are the scores
+    assert size(4, 12, 100, 1) == (0, 0)              # few weights a set: summed where they are chosen from
+    assert size(4, 12, 10000, 1) == (0, 4 * 10000 * 8)
+    assert size(30, 12, 18, 1560) == (0, 30 * 18 * 8)
+    assert size(1, 12, 18, 1560) == (0, 12 * 18 * 8)  # every head a part
+    assert size(-1, 1, 1, 1) == (2, 0)
+    assert L.rc_select_workspace_size(1, 1, 1, 1, None) == 1
 
 
 def test_select_nothing_to_do(L):
