@@ -406,9 +406,10 @@ void launch_scores(const SelectArgs& a, hipStream_t stream) {
 }  // namespace
 
 // How a choice gets its scores. Where a set has few weights its own workgroup adds
-// them up: one launch instead of two (11 us instead of 14 for one set of 12 heads and 18 units of 130
-// tokens), which a set of more weights would spend reading them on one compute unit.
-constexpr int64_t kFewWeights = 1 << 15;
+// them up: one launch instead of two (one head, 18 units of 390 tokens: 5.9 us
+// a call instead of 8.8, 4.6 instead of 5.2 on the device). One compute unit reads
+// more weights too slowly (12 heads, 18 units of 130 tokens: 9.4 us on the device, in two launches 6.9).
+constexpr int64_t kFewWeights = 1 << 13;
 enum class Plan { kWeights, kOwnHeads, kOwnUnits, kSums };
 
 namespace {
@@ -443,10 +444,13 @@ hipError_t launch_select(const SelectArgs& a, hipStream_t stream) {
     }
     if (plan == Plan::kSums) {
         const bool vec = a.unit % 4 == 0 && (uintptr_t)a.weight % 16 == 0;
-        if (a.unit >= 512) vec ? launch_scores<256, 4>(a, stream) : launch_scores<256, 1>(a, stream);
-        else if (a.unit >= 64) vec ? launch_scores<64, 4>(a, stream) : launch_scores<64, 1>(a, stream);
-        else if (a.unit >= 8) vec ? launch_scores<8, 4>(a, stream) : launch_scores<8, 1>(a, stream);
-        else launch_scores<1, 1>(a, stream);
+        // lanes for a unit by its loads, so that a lane has a few rounds of four; units of few tokens one lane
+        // each, whose neighbours' words lie beside its own
+        const int64_t loads = (int64_t)(a.heads / a.splits) * (vec ? a.unit / 4 : a.unit);
+        if (a.unit < 8) launch_scores<1, 1>(a, stream);
+        else if (loads >= 1024) vec ? launch_scores<256, 4>(a, stream) : launch_scores<256, 1>(a, stream);
+        else if (loads >= 64) vec ? launch_scores<64, 4>(a, stream) : launch_scores<64, 1>(a, stream);
+        else vec ? launch_scores<8, 4>(a, stream) : launch_scores<8, 1>(a, stream);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

@@ -29,7 +29,7 @@ def _choice(weight, **kw):
     (5, 1, 1000, 1, 500, 100, 150), (2, 3, 1023, 1, 17, 0, 17), (4, 1, 1025, 1, 1024, 1, 0), (2, 1, 4096, 1, 1, 0, 0), (1, 12, 7, 1560, 3, 1, 1),
     (3, 1, 28081, 1, 9999, 1560, 3120), (2, 1, 70001, 1, 35000, 11, 13), (1, 1, 300007, 1, 1234, 0, 5), (2, 5, 40, 1, 20, 20, 0),
     (2, 1, 37, 2, 20, 0, 20), (7, 1, 2047, 1, 1000, 0, 0), (1, 2, 65537, 1, 65000, 0, 0),
-    (3, 7, 4681, 1, 2000, 10, 20), (3, 8, 4097, 1, 2000, 10, 20), (2, 32, 64, 16, 9, 1, 1), (2, 31, 64, 17, 9, 1, 1), (1, 3, 63, 7, 62, 0, 1),
+    (3, 7, 4681, 1, 2000, 10, 20), (3, 8, 4097, 1, 2000, 10, 20), (2, 32, 64, 16, 9, 1, 1), (2, 31, 64, 17, 9, 1, 1), (2, 8, 64, 16, 9, 1, 1), (3, 1, 17, 480, 5, 0, 2), (5, 13, 630, 1, 300, 7, 7), (4, 40, 18, 40, 11, 0, 0), (1, 3, 63, 7, 62, 0, 1),
     (2, 40, 66, 3, 30, 4, 5), (1, 1, 33000, 1, 100, 0, 0), (1, 1, 32768, 1, 100, 0, 0), (1, 32768, 1, 1, 1, 0, 0), (2, 5, 65, 9, 64, 0, 0),
 ])
 @pytest.mark.parametrize("kind", ["spread", "ties", "equal"])
