@@ -127,6 +127,7 @@ constexpr int kSelWaves = 16;
 constexpr int kSelThreads = 64 * kSelWaves;
 constexpr int kBins = 4096;
 constexpr int kList = 2048;
+constexpr int kEnds = 8;
 constexpr size_t kSelLds = 128 << 10;  // of keys: with the histogram and the list below a compute unit's 160 KiB
 
 // lanes below this one in a ballot
@@ -148,13 +149,23 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     int32_t* out = a.out_idx + (int64_t)blockIdx.x * a.keep;
     float* out_score = a.out_score ? a.out_score + (int64_t)blockIdx.x * a.keep : nullptr;
     auto score = [&](int64_t unit) -> float { return score_of<kFrom>(a, blockIdx.x, unit); };
-    // the protected ends
+    // the protected ends, eight loads in flight (a store between would hold the next load back)
     const int from_last = a.n_units - a.last;
-    for (int i = tid; i < a.first + a.last; i += kSelThreads) {
-        const int u = i < a.first ? i : from_last + (i - a.first);
-        const int o = i < a.first ? i : a.keep - a.last + (i - a.first);
-        out[o] = u;
-        if (out_score) out_score[o] = score(u);
+    for (int i0 = tid; i0 < a.first + a.last; i0 += kSelThreads * kEnds) {
+        float x[kEnds];
+#pragma unroll
+        for (int j = 0; j < kEnds; ++j) {
+            const int i = i0 + j * kSelThreads;
+            x[j] = out_score && i < a.first + a.last ? score(i < a.first ? i : from_last + (i - a.first)) : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < kEnds; ++j) {
+            const int i = i0 + j * kSelThreads;
+            if (i >= a.first + a.last) break;
+            const int o = i < a.first ? i : a.keep - a.last + (i - a.first);
+            out[o] = i < a.first ? i : from_last + (i - a.first);
+            if (out_score) out_score[o] = x[j];
+        }
     }
     const unsigned m = (unsigned)(a.keep - a.first - a.last);  // to choose from the units between
     if (m == 0) return;  // uniform
