@@ -532,8 +532,8 @@ int rc_key_weight_workspace_size(int32_t dtype, int32_t Lq, int32_t Lk, int32_t 
  *   out_score    nullable [sets][keep] fp32: their scores
  *   first, last >= 0, first + last <= keep <= n_units (REVISIT_ERR_PARAM otherwise)
  *   sets <= 2^21, n_units <= 2^30
- *   workspace, workspace_bytes  device scratch of at least the size
- *                rc_select_workspace_size() returns, 16-byte aligned; may be
+ *   workspace, workspace_bytes  device scratch (unit sums; for long sets also histograms and a
+ *                list of keys) of at least the size rc_select_workspace_size() returns, 16-byte aligned; may be
  *                NULL / 0 when that size is 0. Too small: REVISIT_ERR_SHAPE; NULL
  *                while needed: REVISIT_ERR_NULL.
  * sets == 0 or keep == 0 is valid (nothing to do).

@@ -556,7 +556,7 @@ def select_kept(weight: torch.Tensor, *, unit: int, keep: int, first: int = 0, l
             _need(score, "out score", torch.float32, (sets, keep), dev)
     if workspace is not None:
         _need(workspace, "workspace", torch.uint8, None, dev)
-    elif heads > 1 or unit > 1:  # scores that are the weights themselves need none
+    elif heads > 1 or unit > 1 or cols > 1 << 10:  # few scores that are the weights themselves need none
         nbytes = select_workspace_size(sets, heads, n_units, unit)
         if nbytes:
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)

@@ -291,6 +291,8 @@ struct SelectArgs {
     float* out_score;     // nullable [sets][keep]
     int32_t splits;       // head parts of the scores
     double* unit_sum;     // [splits][sets][n_units], workspace (select_workspace_bytes)
+    uint32_t* wide;       // what the workgroups of a long set share, behind them
+    int32_t shares, share_blocks;  // of a long set
 };
 int32_t select_splits(const SelectArgs& a);
 size_t select_workspace_bytes(const SelectArgs& a);

@@ -15,7 +15,8 @@
 // that the usual scores spread over many bins, and the few units in the bin that it
 // leaves are listed for the other two. Where a round's units all have the same digit (equal
 // scores) one lane counts for all. With the threshold every wave knows how many it
-// keeps, one barrier gives each its place, and the units are written in order.
+// keeps, one barrier gives each its place, and the units are written in order. Long sets that
+// leave compute units idle are shared out over workgroups, in three launches.
 // Bound by its instructions (60 per round of 64 units and wave) on one compute unit
 // per set: 96 sets of 37440 tokens 26 us, with the keys in registers and code unrolled over them 31, with
 // four digits of 8 bits read from memory each time 98.
@@ -135,6 +136,31 @@ __device__ __forceinline__ unsigned lanes_below(uint64_t who) {
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
 }
 
+// The protected ends of a set, by threads `at` of `step`, eight loads in flight (a store between
+// would hold the next load back).
+template <Score kFrom>
+__device__ __forceinline__ void protected_ends(const SelectArgs& a, int64_t set, int64_t at, int64_t step) {
+    const int64_t ends = (int64_t)a.first + a.last;
+    int32_t* out = a.out_idx + set * a.keep;
+    float* out_score = a.out_score ? a.out_score + set * a.keep : nullptr;
+    for (int64_t i0 = at; i0 < ends; i0 += step * kEnds) {
+        float x[kEnds];
+#pragma unroll
+        for (int j = 0; j < kEnds; ++j) {
+            const int64_t i = i0 + j * step;
+            x[j] = out_score && i < ends ? score_of<kFrom>(a, set, i < a.first ? i : a.n_units - ends + i) : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < kEnds; ++j) {
+            const int64_t i = i0 + j * step;
+            if (i >= ends) break;
+            const int64_t o = i < a.first ? i : a.keep - ends + i;
+            out[o] = (int32_t)(i < a.first ? i : a.n_units - ends + i);
+            if (out_score) out_score[o] = x[j];
+        }
+    }
+}
+
 // kLds: the keys to choose from lie in LDS after the first sweep; else every sweep reads the scores again.
 template <bool kLds, Score kFrom>
 __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
@@ -149,24 +175,8 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     int32_t* out = a.out_idx + (int64_t)blockIdx.x * a.keep;
     float* out_score = a.out_score ? a.out_score + (int64_t)blockIdx.x * a.keep : nullptr;
     auto score = [&](int64_t unit) -> float { return score_of<kFrom>(a, blockIdx.x, unit); };
-    // the protected ends, eight loads in flight (a store between would hold the next load back)
     const int from_last = a.n_units - a.last;
-    for (int i0 = tid; i0 < a.first + a.last; i0 += kSelThreads * kEnds) {
-        float x[kEnds];
-#pragma unroll
-        for (int j = 0; j < kEnds; ++j) {
-            const int i = i0 + j * kSelThreads;
-            x[j] = out_score && i < a.first + a.last ? score(i < a.first ? i : from_last + (i - a.first)) : 0.0f;
-        }
-#pragma unroll
-        for (int j = 0; j < kEnds; ++j) {
-            const int i = i0 + j * kSelThreads;
-            if (i >= a.first + a.last) break;
-            const int o = i < a.first ? i : a.keep - a.last + (i - a.first);
-            out[o] = i < a.first ? i : from_last + (i - a.first);
-            if (out_score) out_score[o] = x[j];
-        }
-    }
+    protected_ends<kFrom>(a, blockIdx.x, tid, kSelThreads);
     const unsigned m = (unsigned)(a.keep - a.first - a.last);  // to choose from the units between
     if (m == 0) return;  // uniform
     // this wave's share of them: rounds of 64, `count` in all, from u0 on
@@ -353,6 +363,335 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
     });
 }
 
+// ---------------------------------------------------------------------------
+// Long sets: a set's units to choose from are shared out over workgroups, in shares of
+// whole blocks of kWideUnits. Three launches: wide_count_kernel leaves every
+// share's histogram of the first digit; wide_list_kernel finds from all of a
+// set's the bin that holds the threshold and lists the keys in it, the shares' one
+// behind the other; wide_write_kernel finds the threshold in the list
+// (each workgroup for itself), how many the shares before its own keep, and
+// writes its own. Nothing is added atomically outside a workgroup, so the
+// workspace needs no clearing.
+// ---------------------------------------------------------------------------
+constexpr int kWideRounds = 4;
+constexpr int kWideUnits = kSelThreads * kWideRounds;
+constexpr int kWideGroups = 256;          // workgroups of a launch: one per compute unit
+constexpr int64_t kWideFrom = 1 << 18;    // (wide_shares)
+// where a workgroup is, and its set's part of the workspace: per share the histogram, its sums over
+// 64 bins and the range of the listed keys, and the list
+struct Wide {
+    int64_t set, open, u0;  // u0: the share's first unit
+    int share, shares, blocks;
+    unsigned m;
+    uint32_t *fine, *coarse, *range, *list;
+};
+__device__ __forceinline__ Wide wide_of(const SelectArgs& a) {
+    Wide x;
+    x.open = (int64_t)a.n_units - a.first - a.last;
+    x.shares = a.shares;
+    x.blocks = a.share_blocks;
+    x.set = blockIdx.x / (unsigned)a.shares;
+    x.share = (int)(blockIdx.x - (unsigned)x.set * (unsigned)a.shares);
+    x.u0 = a.first + (int64_t)x.share * a.share_blocks * kWideUnits;
+    x.m = (unsigned)(a.keep - a.first - a.last);
+    x.fine = a.wide + x.set * a.shares * kBins;
+    x.coarse = a.wide + (int64_t)a.sets * a.shares * kBins + x.set * a.shares * 64;
+    x.range = a.wide + (int64_t)a.sets * a.shares * (kBins + 64) + x.set * a.shares * 2;
+    x.list = a.wide + (int64_t)a.sets * a.shares * (kBins + 66) + x.set * a.n_units;
+    return x;
+}
+// keys of block b of a share: k[j] of unit base + 64 j + lane of it, for those below `left`
+template <Score kFrom>
+__device__ __forceinline__ int64_t wide_load(const SelectArgs& a, const Wide& x, int b, int wave, int lane, uint32_t (&k)[kWideRounds],
+                                             bool (&have)[kWideRounds]) {
+    const int64_t u = x.u0 + (int64_t)b * kWideUnits + wave * 64 * kWideRounds;
+    const int64_t left = a.first + x.open - u;
+    float s[kWideRounds];
+#pragma unroll
+    for (int j = 0; j < kWideRounds; ++j) {
+        have[j] = 64 * j + lane < left;
+        s[j] = have[j] ? score_of<kFrom>(a, x.set, u + 64 * j + lane) : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < kWideRounds; ++j) k[j] = ordered(s[j]);
+    return u;
+}
+
+// one more in a bin of hist for every lane that is in; equal bins of a wave together
+__device__ __forceinline__ void count_bin(unsigned* hist, bool in, unsigned bin, int lane) {
+    const uint64_t who = __ballot(in);
+    if (who == 0) return;
+    const int leader = __builtin_ctzll(who);
+    const unsigned bin0 = __builtin_amdgcn_readlane(bin, leader);
+    if (__ballot(in && bin == bin0) == who) {
+        if (lane == leader) atomicAdd(&hist[bin0], (unsigned)__popcll(who));
+    } else if (in) {
+        atomicAdd(&hist[bin], 1u);
+    }
+}
+
+template <Score kFrom>
+__global__ __launch_bounds__(kSelThreads) void wide_count_kernel(SelectArgs a) {
+    __shared__ __attribute__((aligned(16))) unsigned hist[kBins];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Wide x = wide_of(a);
+    for (int b = tid; b < kBins; b += kSelThreads) hist[b] = 0;
+    __syncthreads();
+    for (int b = 0; b < x.blocks; ++b) {
+        uint32_t k[kWideRounds];
+        bool have[kWideRounds];
+        wide_load<kFrom>(a, x, b, wave, lane, k, have);
+#pragma unroll
+        for (int j = 0; j < kWideRounds; ++j) count_bin(hist, have[j], k[j] >> 20, lane);
+    }
+    protected_ends<kFrom>(a, x.set, (int64_t)x.share * kSelThreads + tid, (int64_t)x.shares * kSelThreads);
+    __syncthreads();
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    static_assert(kBins == 4 * kSelThreads, "four bins a thread");
+    const u32x4 own = *reinterpret_cast<const u32x4*>(hist + 4 * tid);
+    *reinterpret_cast<u32x4*>(x.fine + (int64_t)x.share * kBins + 4 * tid) = own;
+    unsigned sum = own[0] + own[1] + own[2] + own[3];  // of 64 bins: 16 threads
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) sum += __shfl_xor(sum, d);
+    if ((tid & 15) == 0) x.coarse[x.share * 64 + tid / 16] = sum;
+}
+
+// Of 64 bins in every share (lane's bin at p[share * stride + lane]): the one where the count from the
+// highest down reaches `want`.
+struct WideBin {
+    unsigned bin, want;     // in 0..63; how many are taken from it
+    unsigned all;           // units in it
+    unsigned before, above_before;  // in the shares before this workgroup's: in it, and above it
+};
+__device__ __forceinline__ WideBin wide_find(const Wide& x, const uint32_t* p, int stride, unsigned want, unsigned (*lds)[2][64], int wave, int lane) {
+    unsigned all = 0, before = 0;
+    for (int s0 = wave; s0 < x.shares; s0 += kSelWaves * 4) {
+        unsigned v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int s = s0 + i * kSelWaves;
+            v[i] = s < x.shares ? p[(int64_t)s * stride + lane] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            all += v[i];
+            before += s0 + i * kSelWaves < x.share ? v[i] : 0;
+        }
+    }
+    lds[wave][0][lane] = all;
+    lds[wave][1][lane] = before;
+    __syncthreads();
+    all = before = 0;
+#pragma unroll
+    for (int w = 0; w < kSelWaves; ++w) {
+        all += lds[w][0][lane];
+        before += lds[w][1][lane];
+    }
+    unsigned from = all, before_from = before;  // of this bin and those above
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const unsigned y = __shfl_down(from, d), z = __shfl_down(before_from, d);
+        if (lane + d < 64) {
+            from += y;
+            before_from += z;
+        }
+    }
+    const int at = __builtin_ctzll(__ballot(from >= want && from - all < want));
+    WideBin r;
+    r.bin = at;
+    r.all = __builtin_amdgcn_readlane(all, at);
+    r.want = want - (__builtin_amdgcn_readlane(from, at) - r.all);
+    r.before = __builtin_amdgcn_readlane(before, at);
+    r.above_before = __builtin_amdgcn_readlane(before_from, at) - r.before;
+    return r;
+}
+// the same of the first digit's bins
+__device__ __forceinline__ WideBin wide_digit(const Wide& x, unsigned (*lds)[kSelWaves][2][64], int wave, int lane) {
+    const WideBin c = wide_find(x, x.coarse, 64, x.m, lds[0], wave, lane);
+    WideBin f = wide_find(x, x.fine + c.bin * 64, kBins, c.want, lds[1], wave, lane);
+    f.bin += c.bin * 64;
+    f.above_before += c.above_before;
+    return f;
+}
+
+template <Score kFrom>
+__global__ __launch_bounds__(kSelThreads) void wide_list_kernel(SelectArgs a) {
+    __shared__ unsigned sums[2][kSelWaves][2][64];
+    __shared__ unsigned list_n, lo, hi;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Wide x = wide_of(a);
+    if (tid == 0) {
+        list_n = 0;
+        lo = ~0u;
+        hi = 0;
+    }
+    const WideBin d = wide_digit(x, sums, wave, lane);  // (with barriers)
+    uint32_t least = ~0u, most = 0;
+    for (int b = 0; b < x.blocks; ++b) {
+        uint32_t k[kWideRounds];
+        bool have[kWideRounds];
+        wide_load<kFrom>(a, x, b, wave, lane, k, have);
+#pragma unroll
+        for (int j = 0; j < kWideRounds; ++j) {
+            const bool in = have[j] && k[j] >> 20 == d.bin;
+            const uint64_t who = __ballot(in);
+            if (who == 0) continue;
+            const int leader = __builtin_ctzll(who);
+            unsigned at = 0;
+            if (lane == leader) at = atomicAdd(&list_n, (unsigned)__popcll(who));
+            at = __builtin_amdgcn_readlane(at, leader) + lanes_below(who);
+            if (in) {
+                x.list[d.before + at] = k[j];
+                least = min(least, k[j]);
+                most = max(most, k[j]);
+            }
+        }
+    }
+#pragma unroll
+    for (int s = 32; s > 0; s /= 2) {
+        least = min(least, (uint32_t)__shfl_xor(least, s));
+        most = max(most, (uint32_t)__shfl_xor(most, s));
+    }
+    if (lane == 0 && least <= most) {
+        atomicMin(&lo, least);
+        atomicMax(&hi, most);
+    }
+    __syncthreads();
+    if (tid < 2) x.range[2 * x.share + tid] = tid ? hi : lo;
+}
+
+template <Score kFrom>
+__global__ __launch_bounds__(kSelThreads) void wide_write_kernel(SelectArgs a) {
+    __shared__ unsigned sums[2][kSelWaves][2][64];
+    __shared__ unsigned hist[2][1024], wave_sum[2][kSelWaves], found[2][2], counts[2], range[2];
+    __shared__ unsigned wave_gt[2][kSelWaves], wave_eq[2][kSelWaves];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Wide x = wide_of(a);
+    static_assert(kSelThreads == 1024, "one bin a thread");
+    hist[0][tid] = hist[1][tid] = 0;
+    if (tid < 2) {
+        counts[tid] = 0;
+        range[tid] = tid ? 0u : ~0u;
+    }
+    const WideBin d = wide_digit(x, sums, wave, lane);  // (with barriers)
+    for (int s = tid; s < x.shares; s += kSelThreads) {
+        atomicMin(&range[0], x.range[2 * s]);
+        atomicMax(&range[1], x.range[2 * s + 1]);
+    }
+    __syncthreads();
+    // f(whether there is one, key) of the first n listed
+    auto listed = [&](unsigned n, auto f) {
+        for (unsigned i0 = tid - lane; i0 < n; i0 += 4 * kSelThreads) {
+            uint32_t k[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) k[i] = i0 + i * kSelThreads + lane < n ? x.list[i0 + i * kSelThreads + lane] : 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f(i0 + i * kSelThreads + lane < n, k[i]);
+        }
+    };
+    // the m-th largest key, how many equal to it are taken, and of the listed keys before this
+    // share's how many are larger and equal
+    uint32_t prefix = __builtin_amdgcn_readfirstlane(range[0]);
+    unsigned want = d.want, gt_before = 0, eq_before = d.before;
+    bool all_equal = d.want == d.all;
+    if (prefix != __builtin_amdgcn_readfirstlane(range[1])) {  // else all of them are equal
+        prefix = d.bin << 20;
+        uint32_t mask = 0xfffu << 20;
+#pragma unroll
+        for (int digit = 0; digit < 2; ++digit) {
+            const int shift = digit == 0 ? 10 : 0;
+            listed(d.all, [&](bool have, uint32_t k) { count_bin(hist[digit], have && (k & mask) == prefix, (k >> shift) & 1023, lane); });
+            __syncthreads();
+            const unsigned own = hist[digit][1023 - tid];  // thread t has the t-th highest bin
+            unsigned upto = own;
+#pragma unroll
+            for (int s = 1; s < 64; s *= 2) {
+                const unsigned y = __shfl_up(upto, s);
+                if (lane >= s) upto += y;
+            }
+            if (lane == 63) wave_sum[digit][wave] = upto;
+            __syncthreads();
+            for (int w = 0; w < wave; ++w) upto += wave_sum[digit][w];
+            if (upto >= want && upto - own < want) {
+                found[digit][0] = (unsigned)(1023 - tid);
+                found[digit][1] = want - (upto - own);
+                if (digit == 1) range[0] = own;  // (read by all before the first digit's barriers)
+            }
+            __syncthreads();
+            prefix |= __builtin_amdgcn_readfirstlane(found[digit][0]) << shift;
+            mask |= 1023u << shift;
+            want = __builtin_amdgcn_readfirstlane(found[digit][1]);
+        }
+        all_equal = __builtin_amdgcn_readfirstlane(range[0]) == want;
+        unsigned gt = 0, eq = 0;
+        listed(d.before, [&](bool have, uint32_t k) {
+            gt += have && k > prefix;
+            eq += have && k == prefix;
+        });
+#pragma unroll
+        for (int s = 32; s > 0; s /= 2) {
+            gt += __shfl_xor(gt, s);
+            eq += __shfl_xor(eq, s);
+        }
+        if (lane == 0) {
+            atomicAdd(&counts[0], gt);
+            atomicAdd(&counts[1], eq);
+        }
+        __syncthreads();
+        gt_before = __builtin_amdgcn_readfirstlane(counts[0]);
+        eq_before = __builtin_amdgcn_readfirstlane(counts[1]);
+    }
+    int32_t* out = a.out_idx + x.set * a.keep;
+    float* out_score = a.out_score ? a.out_score + x.set * a.keep : nullptr;
+    // places of the keys above the threshold, and of those equal to it, as they come
+    unsigned gt_at = a.first + d.above_before + gt_before, eq_at = eq_before;
+    for (int b = 0; b < x.blocks; ++b) {
+        uint32_t k[kWideRounds];
+        bool have[kWideRounds];
+        const int64_t u = wide_load<kFrom>(a, x, b, wave, lane, k, have);
+        unsigned gt = 0, eq = 0;
+#pragma unroll
+        for (int j = 0; j < kWideRounds; ++j) {
+            gt += __popcll(__ballot(have[j] && k[j] > prefix));
+            eq += __popcll(__ballot(have[j] && k[j] == prefix));
+        }
+        if (lane == 0) {
+            wave_gt[b & 1][wave] = gt;
+            wave_eq[b & 1][wave] = eq;
+        }
+        __syncthreads();  // (one per block: the other half of the counts is read before the next)
+        unsigned gt_here = gt_at, eq_here = eq_at;
+        for (int w = 0; w < kSelWaves; ++w) {
+            const unsigned g = wave_gt[b & 1][w], e = wave_eq[b & 1][w];
+            gt_here += w < wave ? g : 0;
+            eq_here += w < wave ? e : 0;
+            gt_at += g;
+            eq_at += e;
+        }
+        unsigned at = gt_here + min(eq_here, want);
+#pragma unroll
+        for (int j = 0; j < kWideRounds; ++j) {
+            bool keep = have[j] && k[j] >= prefix;
+            if (!all_equal) {
+                const bool same = have[j] && k[j] == prefix;
+                const uint64_t same_mask = __ballot(same);
+                if (same) keep = eq_here + lanes_below(same_mask) < want;
+                eq_here += __popcll(same_mask);
+            }
+            const uint64_t keep_mask = __ballot(keep);
+            if (keep) {
+                const unsigned o = at + lanes_below(keep_mask);
+                out[o] = (int32_t)(u + 64 * j + lane);
+                if (out_score) out_score[o] = number(k[j]);
+            }
+            at += __popcll(keep_mask);
+        }
+    }
+}
+
 // Up to 64 units, whose scores x the lanes of one wave hold: of those to choose from
 // one is kept if fewer than m come before it.
 __device__ __forceinline__ void select_few(const SelectArgs& a, int64_t set, int lane, float x) {
@@ -446,8 +785,30 @@ int32_t select_splits(const SelectArgs& a) {
     return (int32_t)(want < a.heads ? want : a.heads);
 }
 
-size_t select_workspace_bytes(const SelectArgs& a) {
+// Shares of a long set, 0 where one workgroup chooses from all of it. That one takes 0.65 ns per unit,
+// the three launches 20 us and a share of that, so they pay from n (1 - 1 / shares) = 31000 on; shares * n >
+// 2^18 is near that between 2 and 8 shares, and keeps off sets whose keys one workgroup holds in
+// LDS. One workgroup against shares, us: 30 sets of 37440 25.2, 22.7; 32 of 40000 32.6, 25.6; 60 of 70000
+// 54.6, 37.9; 128 of 140000 118, 98; one of 280800 181, 31, of 1000000 657, 52. On the other side of
+// the rule: one of 17000 16.2, 19.8; 96 of 37440 26.9, 59 (with eight shares each).
+static int32_t wide_shares(const SelectArgs& a) {
+    if (a.sets < 1 || a.sets > kWideGroups / 2) return 0;
+    const int64_t most = ((int64_t)a.n_units + kWideUnits - 1) / kWideUnits;
+    const int64_t shares = most < kWideGroups / a.sets ? most : kWideGroups / a.sets;
+    return shares * a.n_units > kWideFrom ? (int32_t)shares : 0;
+}
+
+// the workspace: unit sums in double, then what the workgroups of a long set share
+static size_t sum_bytes(const SelectArgs& a) {
     return plan_of(a) == Plan::kSums ? (size_t)a.sets * a.n_units * select_splits(a) * sizeof(double) : 0;
+}
+size_t select_workspace_bytes(const SelectArgs& a) {
+    size_t bytes = sum_bytes(a);
+    if (const int32_t shares = wide_shares(a)) {
+        bytes = (bytes + 15) / 16 * 16;
+        bytes += ((size_t)a.sets * shares * (kBins + 66) + (size_t)a.sets * a.n_units) * sizeof(uint32_t);
+    }
+    return bytes;
 }
 
 hipError_t launch_select(const SelectArgs& a, hipStream_t stream) {
@@ -475,6 +836,20 @@ hipError_t launch_select(const SelectArgs& a, hipStream_t stream) {
             return;
         }
         const int64_t open = (int64_t)a.n_units - a.first - a.last;
+        if (wide_shares(a) > 0) {
+            if constexpr (kFrom != Score::kHeads) {
+                SelectArgs b = a;
+                b.wide = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a.unit_sum) + (sum_bytes(a) + 15) / 16 * 16);
+                b.shares = wide_shares(a);
+                b.share_blocks = (int32_t)((open + (int64_t)b.shares * kWideUnits - 1) / ((int64_t)b.shares * kWideUnits));
+                const dim3 grid(a.sets * b.shares);
+                hipLaunchKernelGGL(wide_count_kernel<kFrom>, grid, dim3(kSelThreads), 0, stream, b);
+                if (a.keep == a.first + a.last) return;  // nothing to choose
+                hipLaunchKernelGGL(wide_list_kernel<kFrom>, grid, dim3(kSelThreads), 0, stream, b);
+                hipLaunchKernelGGL(wide_write_kernel<kFrom>, grid, dim3(kSelThreads), 0, stream, b);
+            }
+            return;
+        }
         const size_t lds = (size_t)((open + kSelThreads - 1) / kSelThreads) * kSelThreads * sizeof(uint32_t);
         // (the few weights of kHeads always fit)
         if (kFrom == Score::kHeads || lds <= kSelLds) hipLaunchKernelGGL((select_kernel<true, kFrom>), dim3(a.sets), dim3(kSelThreads), lds, stream, a);

@@ -113,6 +113,10 @@ def test_select_workspace(L):
     assert size(30, 12, 18, 1560) == (0, 30 * 18 * 8)
     assert size(1, 12, 18, 1560) == (0, 12 * 18 * 8)  # every head a part
     assert size(-1, 1, 1, 1) == (2, 0)
+    # long sets that leave compute units idle: histograms of 4096 + 64 bins and a range per share, a list per set
+    assert size(1, 1, 37440, 1) == (0, 4 * (10 * (4096 + 64 + 2) + 37440))
+    assert size(2, 12, 65536, 1) == (0, 2 * (65536 * 8 + 4 * (16 * (4096 + 64 + 2) + 65536)))
+    assert size(1, 1, 1 << 30, 1) == (0, 4 * (256 * (4096 + 64 + 2) + (1 << 30)))
     assert L.rc_select_workspace_size(1, 1, 1, 1, None) == 1
 
 

@@ -57,6 +57,44 @@ def test_choice_of_special_values():
     _choice(np.full((1, 2, 6), 3e38, np.float32), unit=2, keep=2)  # the sum passes fp32: infinite
 
 
+@pytest.mark.parametrize("sets,heads,n,unit,keep,first,last", [
+    (1, 1, 32769, 1, 9000, 0, 0), (1, 1, 37440, 1, 20000, 1560, 4680), (28, 1, 37441, 1, 1, 0, 0), (60, 1, 70001, 1, 35000, 17, 0),
+    (128, 1, 131073, 1, 65537, 1, 1), (129, 1, 131073, 1, 100, 1, 1), (1, 1, 1048577, 1, 300000, 0, 0), (1, 1, 2300001, 1, 1150000, 0, 70000),
+    (1, 1, 1 << 21, 1, 1 << 21, 1, 0), (3, 2, 90001, 3, 40000, 5, 0), (1, 12, 37440, 1, 37439, 0, 0), (2, 1, 280800, 1, 280000, 200000, 80000),
+    (1, 1, 65536, 1, 30, 10, 19), (1, 1, 65536, 1, 65535, 65535, 0), (1, 1, 65536, 1, 65536, 65536, 0),
+])
+@pytest.mark.parametrize("kind", ["spread", "ties", "equal", "binade", "mostly zero"])
+def test_choice_from_long_sets(sets, heads, n, unit, keep, first, last, kind):
+    """Around the sizes where a set is shared out over workgroups, to several blocks in a share. Sets repeat
+    after the second, so that the oracle has two to choose from."""
+    rng = np.random.default_rng(n + keep)
+    shape = (min(sets, 2), heads, n * unit)
+    if kind == "spread":
+        weight = np.exp(1.5 * rng.standard_normal(shape, np.float32))
+    elif kind == "ties":
+        weight = rng.integers(0, 5, shape).astype(np.float32)
+    elif kind == "equal":
+        weight = np.full(shape, 0.25, np.float32)
+    elif kind == "binade":  # one bin of the first digit, so that all units are listed
+        weight = rng.integers(1 << 20, (1 << 20) + (1 << 16), shape).astype(np.float32)
+    else:
+        weight = np.where(rng.random(shape, np.float32) < 0.01, 1.0 + rng.random(shape, np.float32), 0.0).astype(np.float32)
+    of = np.arange(sets) % len(weight)
+    idx, score = rv.select_kept(torch.from_numpy(weight).to(DEV)[torch.from_numpy(of).to(DEV)], unit=unit, keep=keep, first=first, last=last)
+    want, want_score = OC.select_kept(weight, unit, keep, first, last)
+    assert np.array_equal(idx.cpu().numpy(), want[of])
+    assert np.array_equal(score.cpu().numpy(), want_score[of], equal_nan=True)
+
+
+def test_choice_of_special_values_in_long_sets():
+    rng = np.random.default_rng(3)
+    vals = np.array([0.0, -0.0, 1.0, -1.0, math.inf, -math.inf, math.nan, 1e-45, -1e-45, 3e38, -3e38, 1e-38], np.float32)
+    weight = rng.choice(vals, (3, 1, 90000)).astype(np.float32)
+    weight[2] = math.nan
+    for keep in (1, 20000, 60000, 89000, 90000):
+        _choice(weight, unit=1, keep=keep, first=keep // 5)
+
+
 def test_choice_without_scores_and_into_buffers():
     w = torch.rand(3, 2, 100, device=DEV)
     idx, score = rv.select_kept(w, unit=5, keep=8, first=1, last=2)
