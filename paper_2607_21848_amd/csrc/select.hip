@@ -136,6 +136,19 @@ __device__ __forceinline__ unsigned lanes_below(uint64_t who) {
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
 }
 
+// one more in a bin of hist for every lane that is in; equal bins of a wave together
+__device__ __forceinline__ void count_bin(unsigned* hist, bool in, unsigned bin, int lane) {
+    const uint64_t who = __ballot(in);
+    if (who == 0) return;
+    const int leader = __builtin_ctzll(who);
+    const unsigned bin0 = __builtin_amdgcn_readlane(bin, leader);
+    if (__ballot(in && bin == bin0) == who) {
+        if (lane == leader) atomicAdd(&hist[bin0], (unsigned)__popcll(who));
+    } else if (in) {
+        atomicAdd(&hist[bin], 1u);
+    }
+}
+
 // The protected ends of a set, by threads `at` of `step`, eight loads in flight (a store between
 // would hold the next load back).
 template <Score kFrom>
@@ -238,19 +251,7 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
         const int shift = kShift[digit], bins = digit == 0 ? kBins : 1024;
         for (int b = tid; b < bins; b += kSelThreads) hist[b] = 0;
         __syncthreads();
-        auto count_in = [&](int, bool have, uint32_t k) {
-            const bool in = have && (k & mask) == prefix;
-            const uint64_t who = __ballot(in);
-            if (who == 0) return;
-            const unsigned bin = (k >> shift) & (bins - 1);
-            const int leader = __builtin_ctzll(who);
-            const unsigned bin0 = __builtin_amdgcn_readlane(bin, leader);
-            if (__ballot(in && bin == bin0) == who) {
-                if (lane == leader) atomicAdd(&hist[bin0], (unsigned)__popcll(who));
-            } else if (in) {
-                atomicAdd(&hist[bin], 1u);
-            }
-        };
+        auto count_in = [&](int, bool have, uint32_t k) { count_bin(hist, have && (k & mask) == prefix, (k >> shift) & (bins - 1), lane); };
         if (digit > 0 && listed) {
             for (unsigned i = tid - lane; i < list_n; i += kSelThreads) count_in(0, i + lane < list_n, list_key[(i + lane) % kList]);
         } else if (digit == 0) {
@@ -415,19 +416,6 @@ __device__ __forceinline__ int64_t wide_load(const SelectArgs& a, const Wide& x,
 #pragma unroll
     for (int j = 0; j < kWideRounds; ++j) k[j] = ordered(s[j]);
     return u;
-}
-
-// one more in a bin of hist for every lane that is in; equal bins of a wave together
-__device__ __forceinline__ void count_bin(unsigned* hist, bool in, unsigned bin, int lane) {
-    const uint64_t who = __ballot(in);
-    if (who == 0) return;
-    const int leader = __builtin_ctzll(who);
-    const unsigned bin0 = __builtin_amdgcn_readlane(bin, leader);
-    if (__ballot(in && bin == bin0) == who) {
-        if (lane == leader) atomicAdd(&hist[bin0], (unsigned)__popcll(who));
-    } else if (in) {
-        atomicAdd(&hist[bin], 1u);
-    }
 }
 
 template <Score kFrom>
