@@ -79,8 +79,9 @@ constexpr int kStepBytes = kStep * kRowBytes;
 
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 
-// Position of 16-byte chunk c of row r: 16 rows that read one chunk together touch 16 different positions.
-__device__ __forceinline__ int chunk_at(int r, int c) { return r * kRowBytes + ((c ^ (((r & 3) << 2) | ((r >> 2) & 3))) << 4); }
+// Position of 16-byte chunk c of row r: 16 rows that read one chunk together touch 16 different positions, and so
+// do the eight threads that write a row's even (or odd) chunks, modulo 8.
+__device__ __forceinline__ int chunk_at(int r, int c) { return r * kRowBytes + ((c ^ (c >> 3) ^ (r & 15)) << 4); }
 
 __device__ __forceinline__ uint32_t bf16_bits(float x) { return (uint32_t)__builtin_bit_cast(unsigned short, (__bf16)x); }
 __device__ __forceinline__ uint32_t pack2(uint32_t lo, uint32_t hi) { return lo | (hi << 16); }
