@@ -503,13 +503,15 @@ __global__ __launch_bounds__(64 * kWaves) void key_weight_few_kernel(KeyWeightAr
 
 // ---------------------------------------------------------------------------
 // fp32 kernel: v_mfma_f32_32x32x2_f32 (64 cycles each), so bound by the matrix
-// cores as long as nothing waits (12 heads of 4680 x 28080, D 128: 3.44 ms, 117 of the 154 TFLOP/s
-// that a large fp32 product reaches; with the bias 3.65. Against a form that loaded each tile when it
-// came to it: 2000 x 9360, 510 -> 502 us without and 735 -> 541 with the bias). A wave owns 32 keys; while the products of one
+// cores as long as nothing waits (12 heads of 4680 x 28080, D 128: 3.13 ms, 129 of the 154 TFLOP/s
+// that a large fp32 product reaches; with the bias 3.28). A wave owns 32 keys; while the products of one
 // tile of 32 queries use up the query registers, the next tile's rows are loaded
 // into them from global memory (no LDS, no barrier: a tile's 4096 cycles at D =
 // 128 cover the loads), and the tile before has its exponentials and its bias, evaluated directly,
-// differences first, between the MFMAs.
+// differences first, between the MFMAs (2000 x 9360, against a form that loaded each tile when it
+// came to it: 735 -> 541 us with the bias). The four loads of a row's 128-byte line leave together:
+// one at a time, as its registers came free, each met the line anew in L1, 3.39 ms and 3.63. Queries
+// shared by the workgroup through LDS instead: 3.18 and 3.33, not kept.
 // ---------------------------------------------------------------------------
 
 template <int D, bool kBias>
@@ -609,8 +611,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_f32_kernel(KeyWeigh
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            qf[j] = *reinterpret_cast<const floatx4*>(next + 32 * j);
-            __builtin_amdgcn_sched_barrier(0);
+            if (j % 4 == 3) {  // a row's whole line of 128 bytes at once
+#pragma unroll
+                for (int i = j - 3; i <= j; ++i) qf[i] = *reinterpret_cast<const floatx4*>(next + 32 * i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         sum += part_sum;
     };
