@@ -55,6 +55,19 @@ def test_scores_of_2_to_24_units():
     assert (idx[1] == torch.arange(5, device=DEV)).all() and not score[1].any()
 
 
+def test_choice_from_2_to_30_units():
+    """The largest set: 256 workgroups of 1024 blocks each; nearly all scores are equal, and the smaller units of them stay."""
+    n, keep, last = 1 << 30, 100000, 50
+    w = torch.zeros(1, 1, n, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    at = torch.randint(1 << 20, n - 1000, (70000,), generator=g, device=DEV).unique()
+    w[0, 0, at] = 1.0 + torch.rand(len(at), generator=g, device=DEV)
+    idx, score = rv.select_kept(w, unit=1, keep=keep, last=last)
+    zeros = keep - last - len(at)
+    want = torch.cat([torch.arange(zeros, device=DEV), at, torch.arange(n - last, n, device=DEV)]).int()
+    assert torch.equal(idx[0], want) and torch.equal(score[0], w[0, 0, want.long()])
+
+
 def test_move_of_64_gib():
     """One unit moved to more than 4096 places (repeats are allowed): 2^22 workgroups and some more."""
     H, D, unit = 16, 128, 4096  # 16 MiB a unit: 1024 workgroups

@@ -86,6 +86,36 @@ def test_choice_from_long_sets(sets, heads, n, unit, keep, first, last, kind):
     assert np.array_equal(score.cpu().numpy(), want_score[of], equal_nan=True)
 
 
+def test_choice_from_long_sets_in_a_graph():
+    """Choice and move by token, captured once; every replay of new weights equals the eager calls."""
+    H, D, n, keep = 2, 64, 50001, 20000
+    w = torch.rand(1, H, n, device=DEV)
+    kv = [torch.randn(1, n, H, D, device=DEV) for _ in range(2)]
+    out = [torch.zeros(1, keep, H, D, device=DEV) for _ in range(2)]
+    idx = (torch.zeros(H, keep, dtype=torch.int32, device=DEV), torch.zeros(H, keep, device=DEV))
+    ws = torch.empty(rv.select_workspace_size(H, 1, n, 1), dtype=torch.uint8, device=DEV)
+
+    def run():
+        rv.select_kept(w.view(H, 1, n), unit=1, keep=keep, first=7, last=300, out=idx, workspace=ws)
+        rv.compact_kv(*kv, idx[0].view(1, H, keep), *out, unit=1)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        run()
+    for seed in range(4):
+        w.copy_(torch.rand(1, H, n, generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV) ** (1 + 3 * seed))
+        ws.fill_(0xA5)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (*idx, *out)]
+        run()
+        assert all(torch.equal(a, b) for a, b in zip(got, (*idx, *out)))
+        want, _ = OC.select_kept(w.view(H, 1, n).cpu().numpy(), 1, keep, 7, 300)
+        assert np.array_equal(got[0].cpu().numpy(), want)
+
+
 def test_choice_of_special_values_in_long_sets():
     rng = np.random.default_rng(3)
     vals = np.array([0.0, -0.0, 1.0, -1.0, math.inf, -math.inf, math.nan, 1e-45, -1e-45, 3e38, -3e38, 1e-38], np.float32)
