@@ -18,7 +18,7 @@
 // keeps, one barrier gives each its place, and the units are written in order. Long sets that
 // leave compute units idle are shared out over workgroups, in three launches.
 // Bound by its instructions (60 per round of 64 units and wave) on one compute unit
-// per set: 96 sets of 37440 tokens 26 us, with the keys in registers and code unrolled over them 31, with
+// per set: 96 sets of 37440 tokens 25 us, with the keys in registers and code unrolled over them 31, with
 // four digits of 8 bits read from memory each time 98.
 
 #include <hip/hip_runtime.h>
