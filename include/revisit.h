@@ -574,8 +574,9 @@ int rc_select_workspace_size(int32_t sets, int32_t heads, int32_t n_units, int32
  *   rope_t_pairs 0..D/2 (0 = plain copy); rope_theta > 0, frames_per_unit >= 0
  *                (read with rope_t_pairs > 0 only)
  *
- * Source and destination must not overlap (REVISIT_ERR_SHAPE); caches must be
- * 16-byte aligned. n_layers == 0 or keep == 0 is valid (nothing to do).
+ * No destination (dst_k, dst_v, dst_weight) may overlap a source (src_k, src_v,
+ * src_weight, sel, or src_pos where it is read) or another destination
+ * (REVISIT_ERR_SHAPE); caches must be 16-byte aligned. n_layers == 0 or keep == 0 is valid (nothing to do).
  */
 int compact_kv(const void* src_k, const void* src_v, int32_t src_rows,
                const int32_t* sel, int32_t sel_heads, int32_t keep, int32_t unit, int32_t n_units,

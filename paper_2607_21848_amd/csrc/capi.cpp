@@ -590,7 +590,9 @@ void band_quarters(double theta, int n, double* out) {
     for (int j = 0; j < n; ++j, q *= ratio) out[j] = (double)q;
 }
 
+// whether two ranges share a byte (an empty one shares none)
 bool overlap(const void* a, double a_bytes, const void* b, double b_bytes) {
+    if (a_bytes == 0.0 || b_bytes == 0.0) return false;
     const double x = (double)(uintptr_t)a, y = (double)(uintptr_t)b;
     return x < y + b_bytes && y < x + a_bytes;
 }
@@ -908,11 +910,25 @@ int compact_kv(const void* src_k, const void* src_v, int32_t src_rows, const int
     a.n_t = rope_t_pairs;
     a.inv_unit = 1.0 / unit;
     a.inv_kept = 1.0 / ((double)keep * unit);
-    // units move within no cache: a vector could be overwritten before another block has read it
-    const double src_bytes = (double)n_layers * src_rows * row, dst_bytes = (double)n_layers * dst_rows * row;
-    if (overlap(src_k, src_bytes * a.k_bytes, dst_k, dst_bytes * a.k_bytes) || overlap(src_v, src_bytes * a.v_bytes, dst_v, dst_bytes * a.v_bytes) ||
-        (src_weight && overlap(src_weight, 4.0 * n_layers * H * src_weight_cols, dst_weight, 4.0 * n_layers * H * dst_weight_cols)))
-        return fail(REVISIT_ERR_SHAPE, "%s: source and destination overlap", fn);
+    // no destination within a source or another destination: bytes could be overwritten before another
+    // block has read them, or written twice
+    struct Range {
+        const void* at;
+        double bytes;
+    };
+    const double src_rows_all = (double)n_layers * src_rows * row, dst_rows_all = (double)n_layers * dst_rows * row;
+    const Range dst[] = {{dst_k, dst_rows_all * a.k_bytes}, {dst_v, dst_rows_all * a.v_bytes},
+                         {dst_weight, dst_weight ? 4.0 * n_layers * H * dst_weight_cols : 0.0}};
+    const Range src[] = {{src_k, src_rows_all * a.k_bytes}, {src_v, src_rows_all * a.v_bytes},
+                         {src_weight, src_weight ? 4.0 * n_layers * H * src_weight_cols : 0.0},
+                         {sel, 4.0 * n_layers * sel_heads * keep},
+                         {src_pos, src_pos && rope_t_pairs > 0 ? 4.0 * n_units : 0.0}};
+    for (int i = 0; i < 3; ++i) {
+        for (const Range& r : src)
+            if (overlap(dst[i].at, dst[i].bytes, r.at, r.bytes)) return fail(REVISIT_ERR_SHAPE, "%s: source and destination overlap", fn);
+        for (int j = 0; j < i; ++j)
+            if (overlap(dst[i].at, dst[i].bytes, dst[j].at, dst[j].bytes)) return fail(REVISIT_ERR_SHAPE, "%s: destinations overlap", fn);
+    }
     if (revisit::compact_blocks(a) > (double)INT32_MAX) return fail(REVISIT_ERR_SHAPE, "%s: problem too large", fn);
     revisit::CompactFreq f;
     if (rope_t_pairs > 0) band_quarters((double)rope_theta, rope_t_pairs, f.quarter);

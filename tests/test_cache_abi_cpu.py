@@ -148,6 +148,28 @@ def test_compact_rejects(L, kw, status):
     assert "compact_kv" in _lib.last_error()
 
 
+# bytes of _compact's arrays: src_k and src_v 184320 each, dst_k and dst_v 92160, sel 40, weights 2 x 3 x 120 and x 60 words
+_APART = dict(sv=ctypes.c_void_p(0x100000), dv=ctypes.c_void_p(0x900100000), sel=ctypes.c_void_p(0x200000))
+_WEIGHTS = dict(sw=ctypes.c_void_p(0x300000), dw=ctypes.c_void_p(0x900300000), swc=120, dwc=60)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dv=FAKE), dict(dv=ctypes.c_void_p(0x10000 + 184320 - 16)), dict(sk=ctypes.c_void_p(0x500000), dv=ctypes.c_void_p(0x500000 - 92160 + 16)),  # dst_v in src_k
+    dict(dk=ctypes.c_void_p(0x100000 + 184320 - 16)), dict(dk=ctypes.c_void_p(0x100000)),                            # dst_k in src_v
+    dict(dv=FAR), dict(dv=ctypes.c_void_p(0x900000000 + 92160 - 16)), dict(dk=ctypes.c_void_p(0x900100000 + 16)),    # dst_k with dst_v
+    dict(sel=FAR), dict(sel=ctypes.c_void_p(0x900100000 + 92160 - 4)), dict(sel=ctypes.c_void_p(0x900000000 - 36)),  # over the selection
+    dict(pos=ctypes.c_void_p(0x900000000 + 400)), dict(pos=ctypes.c_void_p(0x900100000 - 44)),                       # over the positions
+    dict(_WEIGHTS, dw=ctypes.c_void_p(0x10000)), dict(_WEIGHTS, dw=ctypes.c_void_p(0x100000 + 4)),                   # weights over the caches
+    dict(_WEIGHTS, dw=ctypes.c_void_p(0x900000000 + 8)), dict(_WEIGHTS, dw=ctypes.c_void_p(0x900100000 - 4)),
+    dict(_WEIGHTS, dw=ctypes.c_void_p(0x200000 - 1436)), dict(_WEIGHTS, dw=ctypes.c_void_p(0x300000 + 2876)),
+    dict(_WEIGHTS, sw=ctypes.c_void_p(0x900000000 + 92160 - 4)), dict(_WEIGHTS, sw=ctypes.c_void_p(0x900100000 - 4)),
+])
+def test_compact_rejects_overlap(L, kw):
+    """Every destination against every source and every other destination: blocks would race. (Layers 2 x rows x 3 x 128 bf16.)"""
+    assert _compact(L, **dict(_APART, **kw)) == 2
+    assert "overlap" in _lib.last_error()
+
+
 def test_compact_nothing_to_do(L):
     assert _compact(L, layers=0, sk=NULL, sel=NULL, dk=NULL) == 0
     assert _compact(L, keep=0, row0=60, sk=NULL, sel=NULL, dk=NULL) == 0
