@@ -460,8 +460,8 @@ int pool_token_depth(const float* depth, int32_t n_frames, int32_t h, int32_t w,
  *                or NULL: token r stands at (t0 + r / (h w), r / w mod h, r mod w)
  *   theta > 0
  *
- * Angles are evaluated in double, their cos and sin to a few 1e-8, products
- * and sums in fp32, and the result is rounded once to the output's type.
+ * Angles are evaluated in double (within 2^-52 of themselves), their cos and sin within 4e-8
+ * of that angle's, products and sums in fp32, and the result is rounded once to the output's type.
  * Rows must start on 16 bytes (fp8 outputs on 8): pointers and row strides,
  * REVISIT_ERR_SHAPE otherwise. n_tokens == 0 is valid (nothing to do).
  */

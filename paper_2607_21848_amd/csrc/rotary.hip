@@ -6,13 +6,14 @@
 // bound by HBM: one 256-thread block moves 1024 vectors of 16 bytes, four per
 // thread with all loads in flight first, and while they are it computes the cos
 // and sin of its tokens' angles, one per (token, pair), into a table in LDS that
-// all heads of the token share. Angles are counted in double and reduced before
-// they are rounded to fp32 (rope.h); products and sums are fp32, rounded once to
-// the output's type.
+// all heads of the token share. Angles, cos and sin are evaluated in double and
+// rounded once to fp32 (rope.h); products and sums are fp32, rounded once to the
+// output's type.
 //
-// Measured: q and k of 10800 tokens, 40 heads, D 128, bf16 to e4m3 (332 MB): 60 us, 5.5 TB/s, a
-// plain copy of this card 4.9; 4680 tokens of 12 heads out of packed rows (58 MB) 10.8 us; one
-// token 3.3 us on the device, 9 a call.
+// Measured: q and k of 10800 tokens, 40 heads, D 128, bf16 to e4m3 (332 MB): 61.7 us, 5.4 TB/s, a
+// plain copy of this card 4.9; 4680 tokens of 12 heads out of packed rows (58 MB) 10.5 us (15.0 with
+// the 76 registers that the compiler takes by itself, six waves per SIMD); one token 3.3 us on the
+// device, 9 a call.
 
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -42,7 +43,7 @@ __device__ __forceinline__ uint32_t pack_bf16(floatx2 p) { return __builtin_bit_
 __device__ __forceinline__ float e4m3_range(float x) { return x > 448.0f ? 448.0f : (x < -448.0f ? -448.0f : x); }
 
 template <int kIn, bool kFp8>
-__global__ __launch_bounds__(kBlock) void rotary_kernel(RotaryArgs a, RotaryFreq f, unsigned blocks_q, unsigned blocks) {
+__global__ __launch_bounds__(kBlock, 8) void rotary_kernel(RotaryArgs a, RotaryFreq f, unsigned blocks_q, unsigned blocks) {
     extern __shared__ CosSin table[];  // [tokens of the block][pairs]
     const unsigned block = row_block();
     if (block >= blocks) return;  // grid padding (uniform)

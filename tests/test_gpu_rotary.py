@@ -1,9 +1,9 @@
 """rotary_embed against its fp64 oracle: types, head layouts, strided rows, bands that do not fill the head, given
 and grid positions, the way back, and values that rounding or saturation would lose.
 
-Tolerance. cos and sin: the reduced angle is rounded to fp32 twice and multiplied by a rounded pi / 2 (below 1e-7
-in all), and each Taylor sum ends in two roundings (below 1.2e-7): 4 units of 2^-24. A product pair adds up to two
-more, so the fp32 value is within 6 * 2^-24 (|x| + |y|) of the exact one. Rounding to bf16 adds half a step, 2^-8
+Tolerance. cos and sin: 2^-25 of rounding to fp32, 2e-9 of their Taylor sums, and 2^-52 of the angle; 4 units of 2^-24
+are allowed (test_cos_and_sin holds them to what they are, to the ends of the positions' range). A product pair adds up
+to two more, so the fp32 value is within 6 * 2^-24 (|x| + |y|) of the exact one. Rounding to bf16 adds half a step, 2^-8
 of the value, to e4m3 2^-4 of it (2^-10 below its smallest normal number)."""
 
 from __future__ import annotations
@@ -81,6 +81,32 @@ def test_given_positions_and_the_way_back(dtype):
     # q alone, without k
     alone, none = rv.rotary_embed(q, pairs=pairs, theta=THETA, pos=at, inverse=True)
     assert none is None and torch.equal(alone, qo)
+
+
+@pytest.mark.parametrize("theta", [10000.0, 256.0, 1.0])
+def test_cos_and_sin(theta):
+    """Pairs (1, 0) become (cos, sin) themselves. Near the origin, near frame counts, and to the ends of the positions'
+    range, against angles in 80 bits: the Taylor sums' remainder (2e-9), one rounding to fp32 (half a step below 1: 2^-25)
+    and 2^-52 of the angle (the rounded frequency and its product)."""
+    D, n = 256, 3000
+    pairs = (43, 43, 42)
+    rng = np.random.default_rng(11)
+    pos = np.concatenate([rng.integers(-200, 200, (n // 3, 3)), rng.integers(-2 ** 20, 2 ** 20, (n // 3, 3)),
+                          rng.integers(-2 ** 31, 2 ** 31, (n // 3, 3))]).astype(np.int32)
+    pos[-1], pos[-2] = 2 ** 31 - 1, -2 ** 31
+    x = torch.zeros(n, 1, D, device=DEV)
+    x[..., 0::2] = 1.0
+    for inverse in (False, True):
+        got = rv.rotary_embed(x, pairs=pairs, theta=theta, pos=torch.from_numpy(pos).to(DEV), inverse=inverse)[0].double().cpu().numpy()[:, 0]
+        at = 0
+        for axis, m in enumerate(pairs):
+            omega = np.longdouble(theta) ** (-np.arange(m).astype(np.longdouble) / m)
+            phi = pos[:, axis].astype(np.longdouble)[:, None] * omega
+            tol = 2.0 ** -25 + 2e-9 + 2.0 ** -52 * np.abs(phi)
+            si = -np.sin(phi) if inverse else np.sin(phi)
+            assert (np.abs(got[:, 2 * at:2 * (at + m):2] - np.cos(phi)) <= tol).all()
+            assert (np.abs(got[:, 2 * at + 1:2 * (at + m):2] - si) <= tol).all()
+            at += m
 
 
 def test_gradient_against_differences():
