@@ -491,7 +491,9 @@ int rotary_embed(const void* q, int64_t q_row, const void* k, int64_t k_row,
  *   out          [H][Lk] fp32
  *
  * Lq == 0 is valid (out = decay * prev, or 0). Exponentials and sums are fp32;
- * the result does not change between calls (no atomics).
+ * the result does not change between calls (no atomics). The bias of keys near a
+ * correspondence keeps fp32's accuracy: it is off by some 2^-24 of
+ * lambda / (2 sigma^2) (h + w + (h^2 + w^2) / 128) at most (bf16 / fp8), of itself (fp32).
  *
  *   query_parts  0 = chosen from the shape and the compute units of the current
  *                device (one below 256 queries, at most 16), or a fixed number in [1, 64] (clamped to the number of

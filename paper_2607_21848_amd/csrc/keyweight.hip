@@ -18,6 +18,7 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <numeric>
 #include <type_traits>
 
 #include "internal.h"
@@ -58,9 +59,9 @@ __device__ __forceinline__ int acc_row(int hh, int i) { return 8 * (i >> 2) + 4 
 // Bound by matrix cores and VALU together at the chip's power limit (1.86 GHz):
 // 12 heads of 4680 x 28080 without bias 391 us, 1032 TFLOP/s, where a large bf16 product
 // reaches 1350 to 1390; MFMA 50 to 55% and VALU 60 to 70% of the cycles. With a third of the frames
-// biased 413 us. On the way there: 32 keys per wave and queries from global memory
+// biased 440 us (the bias is two MFMAs per tile, and all its cost adds up). On the way there: 32 keys per wave and queries from global memory
 // 1458 (biased); 64 keys, LDS, no order of its own 536; products beside exponentials 470; query parts by
-// rounds 441; ring addresses as constants and one wave per frame for the bias 416.
+// rounds 441; ring addresses as constants and one wave per frame for the bias, one MFMA then, 416.
 // Block 0's products before block 1's, with sums, exponentials and exponents of three groups in one
 // slot so that nothing waits: 405 against 395 without bias, not kept.
 //
@@ -102,27 +103,81 @@ __device__ __forceinline__ u32x4 wide(uint32_t a, uint32_t b) {
     return u32x4{pair(a, std::false_type{}), pair(a, std::true_type{}), pair(b, std::false_type{}), pair(b, std::true_type{})};
 }
 
-// Bias products. With centred token coordinates a = u_k - c, u' = u^ - c:
-//     (lambda / scale) B = 2 gamma a.u' - gamma |a|^2 - gamma |u'|^2,
-// each fp32 factor as three bf16 pieces (the half-integers a are exact in one), x terms in the first
-// half of the contraction and y terms in the second:
-//     key side    [2 a (x3), -gamma a^2 (3 pieces), 1, 1 or 0]
-//     query side  [gamma u' (3 pieces), 1, 1, 1, -gamma |u'|^2 (2 pieces in the first half, the third in the second)]
-// A query without a correspondence (ok false) has zeros.
-__device__ __forceinline__ u32x4 key_side(float gamma, int t, int w, float cx, float cy, int hh) {
-    const int ky = t / w;
-    const float at = hh ? ((float)ky + 0.5f) - cy : ((float)(t - ky * w) + 0.5f) - cx;
-    const uint32_t twice = bf16_bits(2.0f * at);
-    uint32_t ph, pm, pl;
-    split3(-gamma * (at * at), ph, pm, pl);
-    return u32x4{pack2(twice, twice), pack2(twice, ph), pack2(pm, pl), hh ? kOne : pack2(kOne, kOne)};
+// Bias products. The matrix cores also make the bias gamma |a - u|^2, gamma = -lambda / (2 sigma^2 scale), a the token
+// centre of a key and u a query's correspondence, and the products q k are added to it. Written out in fp32 as gamma (|a|^2 -
+// 2 a.u + |u|^2) it would cancel where a key lies beside the correspondence and has the weight: logits off by
+// 2e-6 at 30 x 52 tokens, sigma 2, and 1.1e-4 at 256 x 256 (rms; largest 5e-4). So u is taken apart into the token centre g
+// next to it and the rest f, and gamma into a number c of 6 bits and the rest e: with T = 2 a, G = 2 g whole numbers
+// counted from the middle of the grid, and sums over both axes,
+//     gamma |a - u|^2 = c [sum T^2/4 - sum T G/2 + sum G^2/4]
+//                       + [sum e T^2/4 - sum T (e G/2 + gamma f) + sum (e G^2/4 + gamma f (G + f))].
+// On a grid of up to 256 tokens a side the terms of the first bracket and their partial sums are whole quarters of c's
+// last place, below 2^24 of them, so that one MFMA adds them up without rounding; the second one's are small
+// (n^2 / 256 + n / 2 times gamma on n tokens) and round like that: logits off by 2e-7 and less at 30 x 52 and 45 x 80, 1e-6 at
+// 256 x 256, of which the exponential's argument alone makes 1e-7. What has more bits than a bf16 holds is cut into pieces
+// that hold it. A lane has the x axis in the first half of the contraction (hh 0), the y axis in the second, and a sum
+// over both in one of them:
+//     key side    hh 0  [c sum T^2/4 (3 pieces), 0, T, T, T, *]    [T, T, T, e sum T^2/4 (3 pieces), 0, 0]
+//                 hh 1  [1, 1, 1, 0, T, T, T, *]                   [T, T, T, 1, 1, 1, 0, 0]
+//     query side  hh 0  [1, 1, 1, 0, -c G/2 (2 pieces), 0, 0]      [-(e G/2 + gamma f) (3 pieces), 1, 1, 1, 0, 0]
+//                 hh 1  [c sum G^2/4 (3), 0, -c G/2 (2), 0, 0]     [the same (3), the last sum (3), 0, 0]
+// A query without a correspondence has zeros. (With |a - u|^2 added up unscaled, u in 256ths first, and multiplied by gamma
+// in the registers, nothing is left of the error, but 18 biased frames take 5% longer.)
+struct BiasScale {
+    float gamma, c, e;
+};
+__device__ __forceinline__ BiasScale bias_scale(float gamma) {
+    // (to nearest; beyond the largest, down)
+    uint32_t c = (__float_as_uint(gamma) + 0x20000u) & 0xfffc0000u;
+    if ((c & 0x7f800000u) == 0x7f800000u) c = __float_as_uint(gamma) & 0xfffc0000u;
+    return BiasScale{gamma, __uint_as_float(c), gamma - __uint_as_float(c)};
 }
-__device__ __forceinline__ u32x4 query_side(float gamma, float ux, float uy, bool ok, int hh) {
-    uint32_t ah, am, al, zh, zm, zl;
-    split3(gamma * (hh ? uy : ux), ah, am, al);
-    split3(-gamma * (ux * ux + uy * uy), zh, zm, zl);
-    const uint32_t one = ok ? kOne : 0;
-    return u32x4{pack2(ah, am), pack2(al, one), pack2(one, one), hh ? zl : pack2(zh, zm)};
+typedef unsigned int u32x6 __attribute__((ext_vector_type(6)));
+struct KeySide {
+    u32x6 words;  // the first product's operand in words 0 to 3, the second's in 2 to 5
+};
+__device__ __forceinline__ KeySide key_side(BiasScale b, int t, int w, int h, int hh) {
+    const int ky = t / w;
+    const float x = (float)(2 * (t - ky * w) + 1 - w), y = (float)(2 * ky + 1 - h);
+    const float sq = 0.25f * (x * x + y * y);  // 17 bits
+    uint32_t ch = kOne, cm = kOne, cl = kOne, eh = kOne, em = kOne, el = kOne;
+    if (hh == 0) {
+        split3(b.c * sq, ch, cm, cl);
+        split3(b.e * sq, eh, em, el);
+    }
+    const uint32_t T = bf16_bits(hh ? y : x);
+    return KeySide{u32x6{pack2(ch, cm), cl, pack2(T, T), pack2(T, eh), pack2(em, el), 0}};
+}
+struct QuerySide {
+    u32x4 exact, rest;  // operands of the two products
+};
+// u: the correspondence's coordinate on this lane's axis of last + 1 tokens; ok: there is one (the same in both halves)
+__device__ __forceinline__ QuerySide query_side(BiasScale b, float u, float last, bool ok, int hh) {
+    auto both = [](float v) -> float {  // the sum over the axes
+        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    };
+    const float cell = fminf(fmaxf(floorf(u), 0.0f), last);
+    const float f = (u - cell) - 0.5f, G = 2.0f * cell - last, q = 0.25f * (G * G);
+    uint32_t ch = kOne, cm = kOne, cl = kOne, eh = kOne, em = kOne, el = kOne, lh, lm, ll;
+    const float c = b.c * both(q), e = both(fmaf(b.e, q, (b.gamma * f) * (G + f)));
+    if (hh) {
+        split3(c, ch, cm, cl);
+        split3(e, eh, em, el);
+    }
+    split3(-fmaf(b.gamma, f, b.e * (0.5f * G)), lh, lm, ll);
+    const float lin = -0.5f * b.c * G;  // 14 bits
+    const uint32_t lin_hi = bf16_bits(lin), lin_lo = bf16_bits(lin - __uint_as_float(lin_hi << 16));
+    QuerySide s;
+    s.exact = u32x4{pack2(ch, cm), cl, pack2(lin_hi, lin_lo), 0};
+    s.rest = u32x4{pack2(lh, lm), pack2(ll, eh), pack2(em, el), 0};
+    return ok ? s : QuerySide{u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}};
+}
+// a tile's bias
+__device__ __forceinline__ floatx16 bias_tile(const QuerySide& q, const KeySide& k) {
+    const u32x4 exact = __builtin_shufflevector(k.words, k.words, 0, 1, 2, 3), rest = __builtin_shufflevector(k.words, k.words, 2, 3, 4, 5);
+    const floatx16 d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(q.exact), as_bf16x8(exact), floatx16{0}, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(q.rest), as_bf16x8(rest), d, 0, 0, 0);
 }
 
 // A block of 32 keys: where it is, and what its bias goes by.
@@ -147,11 +202,15 @@ __device__ __forceinline__ KeyBlock key_block(const KeyWeightArgs& a, int kb, bo
     return b;
 }
 
-template <bool kFp8, bool kBias>
+// kFrames: frames that the blocks of a workgroup may lie in (2 or 4), 0: no bias.
+template <bool kFp8, int kFrames>
 __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeightArgs a, unsigned n_items) {
+    constexpr bool kBias = kFrames > 0;
     __shared__ __attribute__((aligned(256))) uint8_t lds_q[3 * kStepBytes];
     __shared__ floatx4 lds_row[3 * kStep / 4];  // -LSE log2 e of the step's queries
-    __shared__ u32x4 lds_bias[kBias ? 3 * kWaves : 1][2][kBias ? 64 : 1];  // [ring][frame][half of the step]
+    // query side of the bias products: [ring of two][frame][half of the step][lane]
+    __shared__ u32x4 lds_exact[kBias ? 2 * kFrames : 1][2][kBias ? 64 : 1];
+    __shared__ uint32_t lds_rest[kBias ? 2 * kFrames : 1][2][kBias ? 64 : 1][3];
 
     const int tid = threadIdx.x;
     const int lane = tid & 63;
@@ -221,8 +280,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
     // this wave's keys: two blocks of 32
     KeyBlock kb[2];
     bf16x8 kf[2][kD / 16];
-    bf16x8 kbias[2];  // key side of the bias products
-    const float cx = 0.5f * (float)a.w, cy = 0.5f * (float)a.h;
+    KeySide kside[2];
+    const BiasScale scale = bias_scale(-a.gamma);
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
         kb[b] = key_block(a, b < per_wave ? g * per_group + wave * per_wave + b : a.n_blocks, kBias);
@@ -236,51 +295,55 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
                 kf[b][j] = as_bf16x8(*reinterpret_cast<const u32x4*>(row + 32 * j + 16 * hh));
             }
         }
-        if constexpr (kBias) {
-            kbias[b] = as_bf16x8(key_side(a.gamma, kb[b].in0 + n, a.w, cx, cy, hh));
-        }
+        if constexpr (kBias) kside[b] = key_side(scale, kb[b].in0 + n, a.w, a.h, hh);
     }
-    // Bias products: the query side of each frame that the workgroup's blocks lie in (four
-    // at most, counted from its first block's) is made by one wave per frame, in
-    // LDS. A lane takes one of a step's 64 queries, evaluates both contraction halves
-    // (x terms for the first, y terms for the second), and one swap of wave halves
-    // hands each to the lanes of its half.
+    // The query side of the frames that the workgroup's blocks lie in (counted from its first
+    // block's): a wave makes that of half a step (32 queries) for every other frame, each lane one query's on its axis. What
+    // one step reads, its own second half and the next step's first, is made in the step before it (turn t: the
+    // sides that step t reads), so that two turns are held.
+    constexpr int kMade = kBias ? kFrames / 2 : 1;  // frames of a wave
     const int frame0 = g * per_group / a.frame_blocks;
     const int last_block = min((g + 1) * per_group, a.n_blocks) - 1;
-    int made = -1;  // retrieved frame whose side this wave makes
-    if (kBias && frame0 + wave <= last_block / a.frame_blocks) {
-        const int s = a.slot[frame0 + wave];
-        if (s >= 0 && s < a.S) made = __builtin_amdgcn_readfirstlane(s);
-    }
-    float2 corr_u;
-    int corr_i;
-    auto fetch_corr = [&](int q0) {
-        if (made < 0) return;
-        const int64_t o = (int64_t)made * a.Lq + base_of(q0) + my_query;
-        corr_u = reinterpret_cast<const float2*>(a.corr_uv)[o];
-        corr_i = a.corr_idx[o];
-    };
-    auto make_bias = [&](int ring) {
-        if (made < 0) return;
-        const bool ok = corr_i >= 0 && !__builtin_isnan(corr_u.x);
-        const float ux = ok ? corr_u.x - cx : 0.0f, uy = ok ? corr_u.y - cy : 0.0f;
-        uint32_t xh, xm, xl, yh, ym, yl, zh, zm, zl;
-        split3(a.gamma * ux, xh, xm, xl);
-        split3(a.gamma * uy, yh, ym, yl);
-        split3(-a.gamma * (ux * ux + uy * uy), zh, zm, zl);
-        const uint32_t one = ok ? kOne : 0;
-        const u32x4 x = {pack2(xh, xm), pack2(xl, one), pack2(one, one), pack2(zh, zm)}, y = {pack2(yh, ym), pack2(yl, one), pack2(one, one), zl};
-        u32x4 half0, half1;
+    const int half = wave & 1;
+    int made[kMade];  // retrieved frames whose side this wave makes, -1: none
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const auto s = __builtin_amdgcn_permlane32_swap(x[i], y[i], false, false);
-            half0[i] = s[0];
-            half1[i] = s[1];
+    for (int i = 0; i < kMade; ++i) {
+        made[i] = -1;
+        const int f = frame0 + 2 * i + (wave >> 1);
+        if (kBias && f <= last_block / a.frame_blocks) {
+            const int s = a.slot[f];
+            if (s >= 0 && s < a.S) made[i] = __builtin_amdgcn_readfirstlane(s);
         }
-        lds_bias[ring * kWaves + wave][0][lane] = half0;
-        lds_bias[ring * kWaves + wave][1][lane] = half1;
+    }
+    const uint32_t corr_at = 4u * (uint32_t)min(32 * half + n, a.Lq - 1);  // bytes of a correspondence's index
+    float corr_u[kMade];
+    int corr_i[kMade];
+    auto fetch_corr = [&](int turn) {
+#pragma unroll
+        for (int i = 0; i < kMade; ++i) {
+            if (made[i] < 0) continue;
+            const int64_t row = (int64_t)made[i] * a.Lq + base_of(t0 * 32 + max(turn + 1 - half, 0) * kStep);  // uniform
+            corr_u[i] = *reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(a.corr_uv + 2 * row) + (2u * corr_at + 4u * hh));
+            corr_i[i] = *reinterpret_cast<const int32_t*>(reinterpret_cast<const uint8_t*>(a.corr_idx + row) + corr_at);
+        }
     };
-    // this wave's blocks: whether they are biased, and by which wave's side
+    auto make_bias = [&](int turn) {
+        int w = a.w, h = a.h;
+        asm volatile("" : "+s"(w), "+s"(h));  // (no register for what is made of them here)
+        const float bias_last = (float)((hh ? h : w) - 1);
+#pragma unroll
+        for (int i = 0; i < kMade; ++i) {
+            if (made[i] < 0) continue;
+            // a correspondence whose x (the first half's) is NaN is none
+            const float x = __uint_as_float(__builtin_amdgcn_permlane32_swap(__float_as_uint(corr_u[i]), __float_as_uint(corr_u[i]), false, false)[0]);
+            const QuerySide q = query_side(scale, corr_u[i], bias_last, corr_i[i] >= 0 && !__builtin_isnan(x), hh);
+            const int at = (turn & 1) * kFrames + 2 * i + (wave >> 1);
+            lds_exact[at][half][lane] = q.exact;
+#pragma unroll
+            for (int k = 0; k < 3; ++k) lds_rest[at][half][lane][k] = q.rest[k];
+        }
+    };
+    // this wave's blocks: whether they are biased, and by which of the frames' sides
     const int bias0 = kb[0].slot < 0 ? -1 : kb[0].frame - frame0, bias1 = kb[1].slot < 0 ? -1 : kb[1].frame - frame0;
 
     const int n_steps = (t1 - t0 + 1) / 2;
@@ -291,60 +354,97 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
     floatx4 rc[2];   // row constants of the next eight exponentials
     int q_lane[kD / 16];  // chunk 2 j + hh of this lane's row
 #pragma unroll
-    for (int j = 0; j < kD / 16; ++j) q_lane[j] = chunk_at(n, 2 * j + hh);
+    for (int j = 0; j < kD / 16; ++j) {
+        q_lane[j] = chunk_at(n, 2 * j + hh);
+        asm volatile("" : "+v"(q_lane[j]));  // one register each: not put together anew for the last steps
+    }
     auto read_q = [&](int rows, int j) { qf[j & 3] = *reinterpret_cast<const u32x4*>(lds_q + q_lane[j] + rows); };
     auto read_rc = [&](int row, int i) { rc[i & 1] = lds_row[hh + row + 2 * i]; };
     constexpr int kHalf = 32 * kRowBytes, kRow = kStep / 4;  // half a step's rows; a step's row constants, in quads
+
+    // two exponentials of block b's tile `from`: weights 2 e and 2 e + 1 of a lane, added to s
+    auto exps = [&](const floatx16* from, int b, int e, float& s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 2 * e; i < 2 * e + 2; ++i) {
+            // a probability: at most 1, and 0 where the row has no LSE whatever its logits are
+            const float x = __builtin_amdgcn_exp2f(fmaf(from[b][i], a.c_log2, rc[(i >> 2) & 1][i & 3]));
+            s += fminf(fmaxf(x, 0.0f), 1.0f);
+        }
+        asm volatile("" : "+v"(s));  // keeps the exponentials here
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto product = [&](floatx16* to, int b, int j) __attribute__((always_inline)) {
+        to[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qf[j & 3]), kf[b][j], to[b], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // The first products of a half (qf[0]), on top of the bias where a block has one. `meanwhile` is called with 0 while
+    // the bias's operands are read and with 1 beside the first block's matrix instructions. (Branches are uniform per wave.)
+    auto first_products = [&](floatx16* to, int turn, int which, auto meanwhile) __attribute__((always_inline)) {
+        const int frame[2] = {bias0, bias1};
+        QuerySide side[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            if (frame[b] < 0) continue;
+            const int at = (turn & 1) * kFrames + frame[b];
+            const uint32_t* rest = lds_rest[at][which][lane];
+            side[b] = QuerySide{lds_exact[at][which][lane], u32x4{rest[0], rest[1], rest[2], 0}};
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        meanwhile(0);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            if (frame[b] >= 0) {
+                to[b] = bias_tile(side[b], kside[b]);
+                product(to, b, 0);
+            } else {
+                to[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qf[0]), kf[b][0], floatx16{0}, 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (b == 0) meanwhile(1);
+        }
+    };
 
     // Half of a step: the products of the next half (rows) beside the exponentials of
     // this one (row constants row), one MFMA to two of them. Operands are read four
     // products, row constants eight exponentials ahead: past the end, those of the half after.
     auto do_half = [&](auto last_tag, floatx16* cur, floatx16* next, auto rows, auto rows_after, auto row, auto row_after,
-                       auto bias_ring, auto bias_half) __attribute__((always_inline)) {
+                       int turn, auto turn_half) __attribute__((always_inline)) {
         constexpr bool kLast = decltype(last_tag)::value;
-        if constexpr (!kLast) next[0] = next[1] = floatx16{0};
-        u32x4 qb[2];
         float s0 = 0.0f, s1 = 0.0f;
+        auto exps_read = [&](int e) __attribute__((always_inline)) {  // row constants after their last use
+            if (e & 1) {
+                if (e < 4) read_rc(row, (e >> 1) + 2);
+                else if constexpr (!kLast) read_rc(row_after, (e >> 1) - 2);
+            }
+        };
+        if constexpr (kLast || !kBias) {
+            if constexpr (!kLast) next[0] = next[1] = floatx16{0};
 #pragma unroll
-        for (int j = 0; j < kD / 16; ++j) {
-            if constexpr (!kLast) {
-                next[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qf[j & 3]), kf[0][j], next[0], 0, 0, 0);
+            for (int j = 0; j < kD / 16; ++j) {
+                if constexpr (!kLast) product(next, 0, j);
+                exps(cur, 0, j, s0);
+                if constexpr (!kLast) product(next, 1, j);
+                exps(cur, 1, j, s1);
+                if constexpr (!kLast) read_q(j < 4 ? rows : rows_after, (j + 4) & 7);
+                exps_read(j);
                 __builtin_amdgcn_sched_barrier(0);
             }
+        } else {
+            first_products(next, turn, turn_half, [&](int b) __attribute__((always_inline)) {
+                if (b == 0) exps(cur, 0, 0, s0);
+                else exps(cur, 1, 0, s1);
+            });
+            read_q(rows, 4);
 #pragma unroll
-            for (int i = 2 * j; i < 2 * j + 2; ++i) {
-                // a probability: at most 1, and 0 where the row has no LSE whatever its logits are
-                const float e = __builtin_amdgcn_exp2f(fmaf(cur[0][i], a.c_log2, rc[(i >> 2) & 1][i & 3]));
-                s0 += fminf(fmaxf(e, 0.0f), 1.0f);
-            }
-            asm volatile("" : "+v"(s0));  // keeps the exponentials here
-            __builtin_amdgcn_sched_barrier(0);
-            if constexpr (!kLast) {
-                next[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qf[j & 3]), kf[1][j], next[1], 0, 0, 0);
+            for (int j = 1; j < kD / 16; ++j) {
+                product(next, 0, j);
+                exps(cur, 0, j, s0);
+                product(next, 1, j);
+                exps(cur, 1, j, s1);
+                read_q(j < 4 ? rows : rows_after, (j + 4) & 7);
+                exps_read(j);
                 __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int i = 2 * j; i < 2 * j + 2; ++i) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(cur[1][i], a.c_log2, rc[(i >> 2) & 1][i & 3]));
-                s1 += fminf(fmaxf(e, 0.0f), 1.0f);
-            }
-            asm volatile("" : "+v"(s1));
-            if constexpr (!kLast) read_q(j < 4 ? rows : rows_after, (j + 4) & 7);
-            if constexpr (kBias && !kLast) {
-                if (j == 0) {
-                    if (bias0 >= 0) qb[0] = lds_bias[bias_ring * kWaves + bias0][bias_half][lane];  // uniform per wave
-                    if (bias1 >= 0) qb[1] = lds_bias[bias_ring * kWaves + bias1][bias_half][lane];
-                }
-                if (j == 4) {
-                    if (bias0 >= 0) next[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qb[0]), kbias[0], next[0], 0, 0, 0);
-                    if (bias1 >= 0) next[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qb[1]), kbias[1], next[1], 0, 0, 0);
-                }
-            }
-            if (j & 1) {
-                if (j < 4) read_rc(row, (j >> 1) + 2);
-                else if constexpr (!kLast) read_rc(row_after, (j >> 1) - 2);
-            }
-            __builtin_amdgcn_sched_barrier(0);
         }
         sum[0] += s0;
         sum[1] += s1;
@@ -353,11 +453,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
     if (n_steps > 0) {
         put(q_begin, 0, 0);
         if constexpr (kBias) {
-            fetch_corr(q_begin);
-            make_bias(0);
+            fetch_corr(-1);
+            make_bias(-1);
         }
         fetch(q_begin + kStep);
-        if constexpr (kBias) fetch_corr(q_begin + kStep);
+        if constexpr (kBias) fetch_corr(0);
         // the keys are waited for here: at their first use below the wait would drain the
         // next step's query loads too, every time round the loop
 #pragma unroll
@@ -367,15 +467,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < 4; ++j) read_q(0, j);
-        accA[0] = accA[1] = floatx16{0};
-        if constexpr (kBias) {
-            if (bias0 >= 0) accA[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(lds_bias[bias0][0][lane]), kbias[0], accA[0], 0, 0, 0);
-            if (bias1 >= 0) accA[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(lds_bias[bias1][0][lane]), kbias[1], accA[1], 0, 0, 0);
-        }
+        if constexpr (kBias) first_products(accA, -1, 0, [](int) {});
+        else accA[0] = accA[1] = floatx16{0};
 #pragma unroll
         for (int j = 0; j < kD / 16; ++j) {
+            if (!kBias || j > 0) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b) accA[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qf[j & 3]), kf[b][j], accA[b], 0, 0, 0);
+                for (int b = 0; b < 2; ++b) accA[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qf[j & 3]), kf[b][j], accA[b], 0, 0, 0);
+            }
             read_q(j < 4 ? 0 : kHalf, (j + 4) & 7);
         }
         read_rc(0, 0);
@@ -383,8 +482,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
         put(q_begin + kStep, kStepBytes, kRow);
         fetch(q_begin + 2 * kStep);
         if constexpr (kBias) {
-            make_bias(1);
-            fetch_corr(q_begin + 2 * kStep);
+            make_bias(0);
+            fetch_corr(1);
         }
         __syncthreads();
         // At the top of step s: accA holds the logits of its first half, qf the first queries of
@@ -392,16 +491,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
         // (buffers s mod 3).
         // (ring: s mod 3, and the two behind it)
         auto step = [&](int s, auto ring0, auto ring1, auto ring2) __attribute__((always_inline)) {
-            do_half(std::false_type{}, accA, accB, ring0 * kStepBytes + kHalf, ring1 * kStepBytes, ring0 * kRow, ring0 * kRow + kRow / 2, ring0, 1);
+            do_half(std::false_type{}, accA, accB, ring0 * kStepBytes + kHalf, ring1 * kStepBytes, ring0 * kRow, ring0 * kRow + kRow / 2, s, 1);
             if (s + 2 < n_steps) {
                 put(q_begin + (s + 2) * kStep, ring2 * kStepBytes, ring2 * kRow);
                 fetch(q_begin + (s + 3) * kStep);  // past the last step: in bounds, for nothing
-                if constexpr (kBias) {
-                    make_bias(ring2);
-                    fetch_corr(q_begin + (s + 3) * kStep);
-                }
             }
-            do_half(std::false_type{}, accB, accA, ring1 * kStepBytes, ring1 * kStepBytes + kHalf, ring0 * kRow + kRow / 2, ring1 * kRow, ring1, 0);
+            if constexpr (kBias) {
+                make_bias(s + 1);
+                fetch_corr(s + 2);
+            }
+            do_half(std::false_type{}, accB, accA, ring1 * kStepBytes, ring1 * kStepBytes + kHalf, ring0 * kRow + kRow / 2, ring1 * kRow, s, 0);
             __syncthreads();
         };
         // three steps at a time, so that the ring's addresses are constants
@@ -413,7 +512,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
         }
         for (int r = 0; s + 1 < n_steps; ++s, ++r) step(s, r, r == 2 ? 0 : r + 1, r == 0 ? 2 : r - 1);
         const int ring = s % 3, q0 = ring * kStepBytes, r0 = ring * kRow;
-        do_half(std::false_type{}, accA, accB, q0 + kHalf, q0, r0, r0 + kRow / 2, ring, 1);
+        do_half(std::false_type{}, accA, accB, q0 + kHalf, q0, r0, r0 + kRow / 2, s, 1);
         do_half(std::true_type{}, accB, accA, 0, 0, r0 + kRow / 2, 0, 0, 0);
     }
 #pragma unroll
@@ -457,6 +556,15 @@ __global__ __launch_bounds__(64 * kWaves) void key_weight_few_kernel(KeyWeightAr
     const int64_t row_bytes = (int64_t)a.H * kD * kSize;
     const uint8_t* kr = static_cast<const uint8_t*>(a.k) + (kb.key0 + min(n, kb.keys - 1)) * row_bytes + (int64_t)hd * kD * kSize + 16 * hh;
     const uint8_t* Qg = static_cast<const uint8_t*>(a.q) + (int64_t)hd * kD * kSize + 16 * hh;
+    // the correspondence first: its bias is made while the keys are on their way
+    const int q = max(min(n, a.Lq - 1), 0);
+    float corr_u = 0.0f;
+    int corr_i = -1;
+    if (kBias && kb.slot >= 0 && a.Lq > 0) {
+        const int64_t o = (int64_t)kb.slot * a.Lq + q;
+        corr_u = a.corr_uv[2 * o + hh];
+        corr_i = a.corr_idx[o];
+    }
     u32x4 kraw[kLoads];
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) kraw[j] = *reinterpret_cast<const u32x4*>(kr + 32 * j);
@@ -464,12 +572,8 @@ __global__ __launch_bounds__(64 * kWaves) void key_weight_few_kernel(KeyWeightAr
         if constexpr (kFp8) return as_bf16x8(wide(raw[step >> 1][2 * (step & 1)], raw[step >> 1][2 * (step & 1) + 1]));
         else return as_bf16x8(raw[step]);
     };
-    bf16x8 kbias = as_bf16x8(u32x4{0, 0, 0, 0});
-    const float cx = 0.5f * (float)a.w, cy = 0.5f * (float)a.h;
-    if (kBias && kb.slot >= 0) kbias = as_bf16x8(key_side(a.gamma, kb.in0 + n, a.w, cx, cy, hh));
     float sum = 0.0f;
     if (a.Lq > 0) {
-        const int q = min(n, a.Lq - 1);
         const uint8_t* qr = Qg + q * row_bytes;
         u32x4 qraw[kLoads];
 #pragma unroll
@@ -478,11 +582,11 @@ __global__ __launch_bounds__(64 * kWaves) void key_weight_few_kernel(KeyWeightAr
         __builtin_amdgcn_sched_barrier(0);  // all loads leave before the first is waited for
         floatx16 acc = floatx16{0};
         if (kBias && kb.slot >= 0) {
-            const int64_t o = (int64_t)kb.slot * a.Lq + q;
-            const float2 u = reinterpret_cast<const float2*>(a.corr_uv)[o];
-            const bool ok = a.corr_idx[o] >= 0 && !__builtin_isnan(u.x);
-            const float ux = ok ? u.x - cx : 0.0f, uy = ok ? u.y - cy : 0.0f;
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(query_side(a.gamma, ux, uy, ok, hh)), kbias, acc, 0, 0, 0);
+            // a correspondence whose x (the first half's) is NaN is none
+            const float x = __uint_as_float(__builtin_amdgcn_permlane32_swap(__float_as_uint(corr_u), __float_as_uint(corr_u), false, false)[0]);
+            const BiasScale scale = bias_scale(-a.gamma);
+            const QuerySide side = query_side(scale, corr_u, (float)((hh ? a.h : a.w) - 1), corr_i >= 0 && !__builtin_isnan(x), hh);
+            acc = bias_tile(side, key_side(scale, kb.in0 + n, a.w, a.h, hh));
         }
         // a query past the end, or one without an LSE, has no weight to give; both halves write the same
         reinterpret_cast<float*>(lds_row[wave])[n] = n < a.Lq && __builtin_isfinite(lse) ? -lse * kLog2e : -INFINITY;
@@ -663,6 +767,13 @@ __global__ __launch_bounds__(256) void key_weight_merge(const float* partial, co
     out[i] = prev ? fmaf(decay, prev[i], sum) : sum;
 }
 
+// Frames that the blocks of a workgroup lie in, at most: workgroups start at multiples of
+// gcd(their blocks, a frame's blocks) within a frame. 2 for frames of 4 and 6 and of 7 blocks and more, else 3 or 4.
+int group_frames(const KeyWeightArgs& a) {
+    const int group = a.wave_blocks * kWaves, step = std::gcd(group, a.frame_blocks);
+    return 1 + (group - step + a.frame_blocks - 1) / a.frame_blocks;
+}
+
 bool few_queries(const KeyWeightArgs& a) { return a.Lq <= kFewQueries; }
 
 }  // namespace
@@ -675,7 +786,7 @@ void key_weight_plan(KeyWeightArgs& a) {
     }
     a.frame_blocks = (a.hw + kKeys - 1) / kKeys;
     a.n_blocks = a.frame_blocks * (a.Lk / a.hw);
-    // a wave takes two blocks; where frames are single blocks, one, so that a workgroup meets four biased frames at most
+    // a wave takes two blocks; where frames are single blocks, one, so that a workgroup meets four at most
     a.wave_blocks = a.type == kTypeF32 || few_queries(a) || (a.S > 0 && a.frame_blocks == 1) ? 1 : 2;
 }
 
@@ -721,9 +832,11 @@ hipError_t launch_key_weight(const KeyWeightArgs& a, hipStream_t stream) {
         if (a.type == kTypeFp8) bias ? go(key_weight_few_kernel<true, true>) : go(key_weight_few_kernel<true, false>);
         else bias ? go(key_weight_few_kernel<false, true>) : go(key_weight_few_kernel<false, false>);
     } else if (a.type == kTypeFp8) {
-        bias ? go(key_weight_bf16_kernel<true, true>) : go(key_weight_bf16_kernel<true, false>);
+        if (!bias) go(key_weight_bf16_kernel<true, 0>);
+        else group_frames(a) <= 2 ? go(key_weight_bf16_kernel<true, 2>) : go(key_weight_bf16_kernel<true, 4>);
     } else {
-        bias ? go(key_weight_bf16_kernel<false, true>) : go(key_weight_bf16_kernel<false, false>);
+        if (!bias) go(key_weight_bf16_kernel<false, 0>);
+        else group_frames(a) <= 2 ? go(key_weight_bf16_kernel<false, 2>) : go(key_weight_bf16_kernel<false, 4>);
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.parts > 1) {

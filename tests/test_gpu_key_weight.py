@@ -176,6 +176,80 @@ def test_a_part_of_the_keys_under_the_whole_lse(dtype, D, Lq):
     assert (off <= tol[:, rows]).all(), (off / tol[:, rows]).max()
 
 
+def _distances(uv, h, w):
+    """Squared distances [S, Lq, h * w] of the token centres from the correspondences, float64."""
+    t = np.arange(h * w)
+    u = uv.cpu().numpy().astype(np.float64)
+    return (u[..., :1] - (t % w + 0.5)) ** 2 + (u[..., 1:] - (t // w + 0.5)) ** 2
+
+
+def _bias_bound(uv, d2, h, w, lam, sigma):
+    """How far a bias of squared distance d2 may be off on the matrix cores, uv [..., 2] the correspondences. Its whole part,
+    the distance of token centres times a factor of 6 bits, is added without rounding. On an axis of n tokens the other terms
+    are, for a factor of 1, n (f + n / 128), n^2 / 256 and n^2 / 256 + n f + f^2 at most, f what uv is away from its token centre
+    and 1/64 what the factor may be off from 6 bits; S is their sum. They cancel to no more than d2, so that no partial
+    sum passes S / 2 + d2: 16 additions and the terms' own rounding. The factor and the product are off by 5 * 2^-24 of the
+    bias. (Against |a|^2 - 2 a.u + |u|^2 in fp32, whose terms are n^2 / 4 each.)"""
+    S = 0.0
+    for axis, n in ((0, w), (1, h)):
+        u = uv[..., axis].cpu().numpy().astype(np.float64)
+        f = np.abs(u - np.clip(np.floor(u), 0, n - 1) - 0.5)
+        S = S + 2 * n * f + n * n / 64 + f * f
+    return U * abs(lam) / (2 * sigma * sigma) * (9 * S[..., None] + 21 * d2)
+
+
+@pytest.mark.parametrize("dtype,Lq", [(torch.bfloat16, 7), (torch.bfloat16, 100), (torch.float8_e4m3fn, 5), (torch.float8_e4m3fn, 70)])
+@pytest.mark.parametrize("h,w,nf", [(256, 256, 1), (45, 80, 2), (30, 52, 3), (1, 256, 2), (256, 1, 2), (255, 256, 1), (256, 253, 1), (2, 3, 9), (5, 13, 7), (8, 16, 4), (11, 14, 5), (7, 9, 6)])
+def test_bias_beside_the_correspondence(dtype, Lq, h, w, nf):
+    """Queries of zeros one at a time (the others have no LSE): a weight is exp of its bias alone. Frames of one, two, three
+    and five blocks of keys put up to four of them into a workgroup."""
+    H, D, lam, sigma = 2, 128, 1.0, 2.0
+    g = torch.Generator(device=DEV).manual_seed(h * w)
+    q, k = torch.zeros(Lq, H, D, device=DEV).to(dtype), torch.randn(nf * h * w, H, D, generator=g, device=DEV).to(dtype)
+    S = nf
+    slot = torch.arange(S, dtype=torch.int32, device=DEV).flip(0).contiguous()
+    uv = torch.rand(S, Lq, 2, generator=g, device=DEV) * torch.tensor([float(w), float(h)], device=DEV)
+    uv[:, 0] = torch.tensor([0.0, 0.0])
+    uv[:, 1] = torch.tensor([w - 2.0 ** -16, h - 2.0 ** -16])
+    uv[:, 2] = torch.tensor([1e-6, h / 2])
+    uv[:, 3] = torch.tensor([w / 2 + 0.5, 0.3])
+    uv[:, 4] = torch.tensor([-1.7, h + 2.3])  # beside the grid
+    idx = torch.zeros(S, Lq, dtype=torch.int32, device=DEV)
+    by_key = lambda x: x[slot.cpu().numpy()].transpose(1, 0, 2).reshape(Lq, nf * h * w)  # noqa: E731
+    d2 = _distances(uv, h, w)
+    bound, d2 = by_key(_bias_bound(uv, d2, h, w, lam, sigma)), by_key(d2)
+    B = -lam / (2 * sigma * sigma) * d2
+    for p in sorted({0, 1, 2, 3, 4, Lq // 2, Lq - 1}):
+        lse = torch.full((H, Lq), math.inf, device=DEV)
+        lse[:, p] = 0.0
+        got = rv.attention_key_weight(q, k, lse, slot, uv, idx, h=h, w=w, softmax_scale=D ** -0.5, lam=lam, sigma=sigma)
+        tol = np.exp(B[p]) * (np.expm1(bound[p] + 4 * U * np.abs(B[p])) + 2.0 ** -22) + 2.0 ** -126
+        off = np.abs(got.double().cpu().numpy() - np.exp(B[p]))
+        assert (off <= tol).all(), (p, (off / tol).max())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float8_e4m3fn])
+@pytest.mark.parametrize("Lq,nf,h,w,S", [(90, 2, 45, 80, 1), (200, 1, 100, 120, 1), (20, 2, 60, 90, 2), (130, 30, 3, 5, 20), (130, 6, 12, 13, 5)])
+def test_biased_weights_of_large_grids(dtype, Lq, nf, h, w, S):
+    """As test_weights, with the bound on the bias of above; the products are added to the bias, so that their D + 4
+    roundings also count its size."""
+    H, D, lam, sigma = 2, 128, 1.3, 2.0
+    q, k, slot, uv, idx = _case(h + w, dtype, Lq, nf, h, w, H, D, S)
+    uv = uv.nan_to_num(0.0)
+    A, lse = _oracle(q, k, slot, uv, idx, h, w, D ** -0.5, lam, sigma)
+    plain = _tolerance(q, k, A, lse, h, w, D ** -0.5, lam, sigma, D, False)
+    of = slot.cpu().numpy()
+    there = (idx >= 0).cpu().numpy()[..., None]
+    d2 = np.where(there, _distances(uv, h, w), 0.0)
+    bound = np.where(there, _bias_bound(uv, d2, h, w, lam, sigma), 0.0) + (D + 4) * U * lam / (2 * sigma * sigma) * d2
+    rel = np.where((of >= 0)[:, None, None], bound[of], 0.0).transpose(1, 0, 2).reshape(Lq, nf * h * w)
+    p = np.exp(A - lse.astype(np.float64)[:, :, None])
+    tol = plain + (p * np.expm1(rel)[None]).sum(axis=1)
+    got = rv.attention_key_weight(q, k, torch.from_numpy(lse).to(DEV), slot, uv, idx, h=h, w=w, softmax_scale=D ** -0.5, lam=lam, sigma=sigma)
+    off = np.abs(got.double().cpu().numpy() - OC.key_weight(A, lse))
+    assert (off <= tol).all(), (off / tol).max()
+
+
 def test_refusals_of_the_binding():
     q, k, slot, uv, idx = _case(13, torch.bfloat16, 40, 4, 4, 5, 2, 128, 2)
     lse = torch.zeros(2, 40, device=DEV)
