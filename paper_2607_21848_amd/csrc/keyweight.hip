@@ -6,7 +6,8 @@
 // with 32x32 MFMAs: queries are the M dimension, its keys the N dimension (held in
 // registers), so a lane holds one key and 16 queries of each tile and a key's
 // sum stays in its lane until the end, where the two wave halves meet: 16 weights
-// of a tile are added first, then the tile to the key's sum, all in fp32. No
+// of a tile are added first, then 16 or 18 tiles, then those sums, all in fp32 (n tiles
+// one after the other would round n times at the sum's own size, up to n 2^-24 in all). No
 // atomics: the same call gives the same bits. Blocks of 32 keys never cross a frame,
 // so one retrieved frame's correspondences serve the whole block.
 //
@@ -77,6 +78,7 @@ constexpr int kD = 128;
 constexpr int kStep = 64;                    // queries of a step
 constexpr int kRowBytes = kD * 2;
 constexpr int kStepBytes = kStep * kRowBytes;
+constexpr int kSumSteps = 9;                 // steps whose weights are added up by themselves
 
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 
@@ -208,6 +210,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
     constexpr bool kBias = kFrames > 0;
     __shared__ __attribute__((aligned(256))) uint8_t lds_q[3 * kStepBytes];
     __shared__ floatx4 lds_row[3 * kStep / 4];  // -LSE log2 e of the step's queries
+    __shared__ float lds_total[2][kWaves][64];  // each lane's two sums
     // query side of the bias products: [ring of two][frame][half of the step][lane]
     __shared__ u32x4 lds_exact[kBias ? 2 * kFrames : 1][2][kBias ? 64 : 1];
     __shared__ uint32_t lds_rest[kBias ? 2 * kFrames : 1][2][kBias ? 64 : 1][3];
@@ -315,10 +318,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
             if (s >= 0 && s < a.S) made[i] = __builtin_amdgcn_readfirstlane(s);
         }
     }
-    const uint32_t corr_at = 4u * (uint32_t)min(32 * half + n, a.Lq - 1);  // bytes of a correspondence's index
     float corr_u[kMade];
     int corr_i[kMade];
     auto fetch_corr = [&](int turn) {
+        int last = a.Lq - 1;
+        asm volatile("" : "+s"(last));  // (no register for what is made of it here)
+        const uint32_t corr_at = 4u * (uint32_t)min(32 * half + n, last);  // bytes of a correspondence's index
 #pragma unroll
         for (int i = 0; i < kMade; ++i) {
             if (made[i] < 0) continue;
@@ -329,7 +334,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
     };
     auto make_bias = [&](int turn) {
         int w = a.w, h = a.h;
-        asm volatile("" : "+s"(w), "+s"(h));  // (no register for what is made of them here)
+        asm volatile("" : "+s"(w), "+s"(h));  // (nor here)
         const float bias_last = (float)((hh ? h : w) - 1);
 #pragma unroll
         for (int i = 0; i < kMade; ++i) {
@@ -349,6 +354,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
     const int n_steps = (t1 - t0 + 1) / 2;
     const int q_begin = t0 * 32;
     float sum[2] = {0.0f, 0.0f};
+    lds_total[0][wave][lane] = lds_total[1][wave][lane] = 0.0f;
     floatx16 accA[2], accB[2];
     u32x4 qf[4];     // queries of the next four products
     floatx4 rc[2];   // row constants of the next eight exponentials
@@ -509,6 +515,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
             step(s, Int<0>{}, Int<1>{}, Int<2>{});
             step(s + 1, Int<1>{}, Int<2>{}, Int<0>{});
             step(s + 2, Int<2>{}, Int<0>{}, Int<1>{});
+            if (s % kSumSteps == kSumSteps - 3) {  // (s is a multiple of 3)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    lds_total[b][wave][lane] += sum[b];
+                    sum[b] = 0.0f;
+                }
+            }
         }
         for (int r = 0; s + 1 < n_steps; ++s, ++r) step(s, r, r == 2 ? 0 : r + 1, r == 0 ? 2 : r - 1);
         const int ring = s % 3, q0 = ring * kStepBytes, r0 = ring * kRow;
@@ -517,6 +530,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
     }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
+        sum[b] += lds_total[b][wave][lane];
         const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum[b]), __float_as_uint(sum[b]), false, false);
         const float s = __uint_as_float(p[0]) + __uint_as_float(p[1]);
         if (hh == 0 && n < kb[b].keys) {
@@ -677,7 +691,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_f32_kernel(KeyWeigh
         }
         return r;
     };
-    float sum = 0.0f, part_sum = 0.0f;
+    float sum = 0.0f, group = 0.0f, part_sum = 0.0f;  // of all tiles, of up to 16 of them, of one
     // the weight of logit i of a tile whose rows lie in `rows`; the next one's row is read meanwhile
     float4 ahead;
     auto unit = [&](const floatx16& acc, const float4* rows, int i) {
@@ -721,7 +735,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_f32_kernel(KeyWeigh
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        sum += part_sum;
+        group += part_sum;
     };
     if (t0 < t1) {
         floatx16 accA, accB;
@@ -737,6 +751,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_f32_kernel(KeyWeigh
         for (; t + 1 < t1; t += 2) {
             tile(std::false_type{}, t, accB, accA);
             tile(std::false_type{}, t + 1, accA, accB);
+            if (((t - t0) & 15) == 15) {
+                sum += group;
+                group = 0.0f;
+            }
         }
         if (t < t1) {
             tile(std::false_type{}, t, accB, accA);
@@ -746,7 +764,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_f32_kernel(KeyWeigh
         ahead = lds_row[wave][(t1 - 1) & 1][acc_row(hh, 0)];
 #pragma unroll
         for (int i = 0; i < 16; ++i) unit(accA, lds_row[wave][(t1 - 1) & 1], i);
-        sum += part_sum;
+        sum += group + part_sum;
     }
     const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
     sum = __uint_as_float(p[0]) + __uint_as_float(p[1]);

@@ -176,6 +176,27 @@ def test_a_part_of_the_keys_under_the_whole_lse(dtype, D, Lq):
     assert (off <= tol[:, rows]).all(), (off / tol[:, rows]).max()
 
 
+@pytest.mark.parametrize("dtype,D", [(torch.bfloat16, 128), (torch.float8_e4m3fn, 128), (torch.float32, 64), (torch.float32, 128)])
+def test_long_sums_of_one_value(dtype, D):
+    """9600 queries that all give a key the same weight, in one part: 300 tiles of 32. A lane's sum, half of them, may round
+    at each of 16 weights, at each of up to 18 tiles that are added up by themselves and at each of up to 19 such
+    groups, then once with the other half: within 54 * 2^-24. Tile after tile it would round 300 times, near its end always the
+    same way, for some of these values by nearly half a step each time: about 73 * 2^-24 in all."""
+    H, Lq, h, w = 64, 9600, 5, 8
+    q = torch.zeros(Lq, H, D, device=DEV).to(dtype)
+    k = torch.zeros(h * w, H, D, device=DEV).to(dtype)
+    kw = dict(h=h, w=w, softmax_scale=D ** -0.5, lam=0.0, sigma=1.0, query_parts=1)
+    at = np.float32(-math.log(2.0 ** -12 * 1.7))
+    values = at + np.arange(H, dtype=np.float32) * np.spacing(at)  # one for each head: their last bits run through all places
+    lse = torch.full((H, Lq), math.inf, device=DEV)
+    lse[:, 7] = torch.from_numpy(values).to(DEV)
+    one = rv.attention_key_weight(q, k, lse, None, None, None, **kw).double()  # a single query's weight
+    assert (one[:, :1] == one).all() and ((one[:, 0] * 2 ** 12 / 1.7 - 1).abs() < 1e-4).all()
+    lse[:] = lse[:, 7:8].clone()
+    got = rv.attention_key_weight(q, k, lse, None, None, None, **kw).double()
+    assert ((got / (Lq * one) - 1).abs() <= 54 * U).all(), float((got / (Lq * one) - 1).abs().max() / U)
+
+
 def _distances(uv, h, w):
     """Squared distances [S, Lq, h * w] of the token centres from the correspondences, float64."""
     t = np.arange(h * w)
