@@ -33,7 +33,12 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr float kLog2e = 1.4426950408889634f;
+// -LSE log2 e, rounded once: log2 e alone in fp32 is 1.9e-8 off, which would make every weight too large by 1.3e-8 of the LSE
+__device__ __forceinline__ float row_constant(float lse) {
+    constexpr double kLog2e = 1.4426950408889634;
+    constexpr float kHi = (float)kLog2e, kLo = (float)(kLog2e - (double)kHi);
+    return -fmaf(lse, kHi, lse * kLo);
+}
 constexpr int kWaves = 4;
 constexpr int kFewQueries = 32;
 constexpr int kKeys = 32;  // keys of a block
@@ -276,7 +281,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_bf16_kernel(KeyWeig
         // a query past the end, or one without an LSE, has no weight to give
         const int q = base_of(q0) + lane;
         __builtin_amdgcn_sched_barrier(0);  // the registers are loaded again only after this
-        if (wave == 0) reinterpret_cast<float*>(lds_row + to_row)[lane] = q >= q0 && q < q_end && __builtin_isfinite(stage_lse) ? -stage_lse * kLog2e : -INFINITY;
+        if (wave == 0) reinterpret_cast<float*>(lds_row + to_row)[lane] = q >= q0 && q < q_end && __builtin_isfinite(stage_lse) ? row_constant(stage_lse) : -INFINITY;
     };
     if (t0 < t1) fetch(t0 * 32);
 
@@ -603,7 +608,7 @@ __global__ __launch_bounds__(64 * kWaves) void key_weight_few_kernel(KeyWeightAr
             acc = bias_tile(side, key_side(scale, kb.in0 + n, a.w, a.h, hh));
         }
         // a query past the end, or one without an LSE, has no weight to give; both halves write the same
-        reinterpret_cast<float*>(lds_row[wave])[n] = n < a.Lq && __builtin_isfinite(lse) ? -lse * kLog2e : -INFINITY;
+        reinterpret_cast<float*>(lds_row[wave])[n] = n < a.Lq && __builtin_isfinite(lse) ? row_constant(lse) : -INFINITY;
 #pragma unroll
         for (int j = 0; j < kD / 16; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(qraw, j), operand(kraw, j), acc, 0, 0, 0);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -683,7 +688,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void key_weight_f32_kernel(KeyWeigh
     auto make_row = [&](int t) -> float4 {
         float4 r = {0.0f, 0.0f, 0.0f, -INFINITY};
         // a query past the end, or one without an LSE, has no weight to give
-        if (t * 32 + n < a.Lq && __builtin_isfinite(row_lse)) r.w = -row_lse * kLog2e;
+        if (t * 32 + n < a.Lq && __builtin_isfinite(row_lse)) r.w = row_constant(row_lse);
         if (kBias && row_i >= 0 && !__builtin_isnan(row_u.x)) {
             r.x = row_u.x;
             r.y = row_u.y;

@@ -197,6 +197,23 @@ def test_long_sums_of_one_value(dtype, D):
     assert ((got / (Lq * one) - 1).abs() <= 54 * U).all(), float((got / (Lq * one) - 1).abs().max() / U)
 
 
+@pytest.mark.parametrize("Lq", [32, 9600])
+@pytest.mark.parametrize("dtype,D", [(torch.bfloat16, 128), (torch.float8_e4m3fn, 128), (torch.float32, 64), (torch.float32, 128)])
+def test_no_common_error_of_the_exponent(dtype, D, Lq):
+    """Logits of 0 under LSEs around 80: the mean of many sums shows what all weights have in common. A query's exponent,
+    115 in units of log 2, may round by 2^-18, which is 2.7e-6 of its weight and as often up as down: over 64 heads of
+    Lq queries the mean is within 6 of its standard deviations (2.7e-6 / sqrt(3) / sqrt(64 Lq)), and 8 * 2^-24 for the exponentials' and
+    the sums' own. A log2 e that is rounded to fp32 makes it 1.1e-6 throughout."""
+    H, h, w = 64, 5, 8
+    g = torch.Generator(device=DEV).manual_seed(3)
+    q, k = torch.zeros(Lq, H, D, device=DEV).to(dtype), torch.zeros(h * w, H, D, device=DEV).to(dtype)
+    lse = 79.0 + 2.0 * torch.rand(H, Lq, generator=g, device=DEV)
+    got = rv.attention_key_weight(q, k, lse, None, None, None, h=h, w=w, softmax_scale=D ** -0.5, lam=0.0, sigma=1.0).double()
+    want = (-lse.double()).exp().sum(1)
+    off = (got[:, 0] / want - 1).mean().abs()
+    assert off <= 6 * 2.7e-6 / math.sqrt(3 * 64 * Lq) + 8 * U, float(off)
+
+
 def _distances(uv, h, w):
     """Squared distances [S, Lq, h * w] of the token centres from the correspondences, float64."""
     t = np.arange(h * w)
