@@ -818,22 +818,31 @@ int64_t key_weight_items(const KeyWeightArgs& a) {
     return ((int64_t)a.n_blocks + per_group - 1) / per_group * a.H * a.parts;
 }
 
+// Workgroups that a compute unit has room for, by the kernels' registers: fp32 at D 64, at D 128, bf16 / fp8.
+constexpr int kPlacesF32D64 = 4, kPlacesF32D128 = 2, kPlacesBf16 = 2;
+
 int32_t key_weight_parts(const KeyWeightArgs& a, int32_t cus) {
     if (a.Lq < 256) return 1;  // a part's own start (its keys, its first queries) would cost more than it saves
     KeyWeightArgs b = a;
     b.parts = 1;
     const int64_t items = key_weight_items(b), tiles = (a.Lq + 31) / 32;
-    // Estimated time in steps of 64 queries: the rounds that the workgroups make on the chip's
-    // places, each as long as a part plus its start; a last round that leaves every
-    // compute unit at most one workgroup runs faster. With parts, the merge.
+    // Estimated time in steps of 64 queries: the rounds that the workgroups make on the chip's places,
+    // each as long as a part plus its start. The last round leaves k workgroups on a compute unit, which share it and take
+    // about k / places of a full one. Workgroups with a bias take a quarter longer than those without, and
+    // which come last is chance: a fifth of a part more. With parts, the merge. Chosen against the best of 1 to 16
+    // parts, us: fp32, D 128, 3 heads of 1560 x 28080 309, 309; 12 of 1170 x 4680 167, 167; D 64, 2 of 3321 x 9963 90, 90;
+    // 3 of 1560 x 28080 167, 165 (places and step time of one size for both D chose 325, 180, 103 and 181); bf16, half of
+    // 6 frames of 3600 biased, 12 heads of 10800 queries 810, 803 (without the fifth 860).
     const bool f32 = a.type == kTypeF32;
-    const int64_t slots = (int64_t)cus * (f32 ? 3 : 2);
-    const double start = f32 ? 1.0 : 2.3, step_us = f32 ? 8.0 : (a.S > 0 ? 2.1 : 1.8);
+    const int64_t places = !f32 ? kPlacesBf16 : (a.D == 64 ? kPlacesF32D64 : kPlacesF32D128), slots = cus * places;
+    const double start = f32 ? 1.0 : 2.3, step_us = f32 ? (a.D == 64 ? 9.0 : 8.0) : (a.S > 0 ? 2.1 : 1.8);
+    const int64_t least = f32 ? 1 : 4;  // tiles of a part: an fp32 one takes 4 us, as long as a whole start
     double best = 0.0;
     int32_t parts = 1;
-    for (int32_t p = 1; p <= 16 && tiles / p >= 4; ++p) {
-        const int64_t n = items * p, full = n / slots, rest = n % slots;
-        double t = ((double)full + (rest == 0 ? 0.0 : (rest <= cus ? 0.55 : 1.0))) * (start + (double)((tiles + p - 1) / p) / 2);
+    for (int32_t p = 1; p <= 16 && (p == 1 || tiles / p >= least); ++p) {
+        const int64_t n = items * p, last = (n % slots + cus - 1) / cus;
+        const double rounds = (double)(n / slots) + (last > 0 ? ((double)last + 0.2) / ((double)places + 0.2) : 0.0);
+        double t = (rounds + (!f32 && a.S > 0 ? 0.2 : 0.0)) * (start + (double)((tiles + p - 1) / p) / 2);
         if (p > 1) t += (3.0 + (double)p * a.H * a.Lk * 4 / 4e6) / step_us;
         if (p == 1 || t < best) {
             best = t;
