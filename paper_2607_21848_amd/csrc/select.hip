@@ -377,7 +377,7 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectArgs a) {
 constexpr int kWideRounds = 4;
 constexpr int kWideUnits = kSelThreads * kWideRounds;
 constexpr int kWideGroups = 256;          // workgroups of a launch: one per compute unit
-constexpr int64_t kWideFrom = 1 << 18;    // (wide_shares)
+constexpr int64_t kWideFrom = 31000, kWideFromTwo = 50000;  // (wide_shares)
 // where a workgroup is, and its set's part of the workspace: per share the histogram, its sums over
 // 64 bins and the range of the listed keys, and the list
 struct Wide {
@@ -773,17 +773,21 @@ int32_t select_splits(const SelectArgs& a) {
     return (int32_t)(want < a.heads ? want : a.heads);
 }
 
-// Shares of a long set, 0 where one workgroup chooses from all of it. That one takes 0.65 ns per unit,
-// the three launches 20 us and a share of that, so they pay from n (1 - 1 / shares) = 31000 on; shares * n >
-// 2^18 is near that between 2 and 8 shares, and keeps off sets whose keys one workgroup holds in
-// LDS. One workgroup against shares, us: 30 sets of 37440 25.2, 22.7; 32 of 40000 32.6, 25.6; 60 of 70000
-// 54.6, 37.9; 128 of 140000 118, 98; one of 280800 181, 31, of 1000000 657, 52. On the other side of
-// the rule: one of 17000 16.2, 19.8; 96 of 37440 26.9, 59 (with eight shares each).
+// Shares of a long set, 0 where one workgroup chooses from all of it. Where its keys do not lie in LDS, that one takes 8 us and
+// 0.5 to 0.6 ns per unit, the three launches 17 us and 4.3 per block of a share: up to one block each 21. They
+// pay from n (1 - 1 / shares) = 31000 on, with two shares, whose blocks fill only half of the chip's time, from n = 100000. One
+// workgroup against shares, us (spread scores; a tenth and a twentieth of the units protected): one or eight sets
+// of 36000 22.5, 20.9; 51 of 42000 29.5, 26.1; 64 of 52000 35.3, 30.7; 85 of 52000 36.0, 34.7; 100 of 120000 90.0,
+// 74.3; one of 140000 84, 24; of 1000000 657, 38. On the other side of the rule: one of 32700 21.5, 20.5; 51 of
+// 36000 23.7, 25.7; 64 of 36000 23.9, 26.0; 85 of 42000 30.5, 30.8; 100 of 90000 57.8, 59.5.
+// Scores that nearly all lie in one bin of the first digit (within an eighth of each other, but not equal) are all listed, and each
+// workgroup searches the whole list: 30 sets of 40000 34.5, 48.3; 128 of 140000 118, 160; one of 131072 91, 71, of 1000000
+// 700, 443. Equal scores are quicker than spread ones (one of 1000000 820, 26).
 static int32_t wide_shares(const SelectArgs& a) {
     if (a.sets < 1 || a.sets > kWideGroups / 2) return 0;
-    const int64_t most = ((int64_t)a.n_units + kWideUnits - 1) / kWideUnits;
+    const int64_t n = a.n_units, most = (n + kWideUnits - 1) / kWideUnits;
     const int64_t shares = most < kWideGroups / a.sets ? most : kWideGroups / a.sets;
-    return shares * a.n_units > kWideFrom ? (int32_t)shares : 0;
+    return n * (shares - 1) > (shares == 2 ? kWideFromTwo : kWideFrom) * shares ? (int32_t)shares : 0;
 }
 
 // the workspace: unit sums in double, then what the workgroups of a long set share

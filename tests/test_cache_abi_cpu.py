@@ -120,6 +120,21 @@ def test_select_workspace(L):
     assert L.rc_select_workspace_size(1, 1, 1, 1, None) == 1
 
 
+def test_select_shares(L):
+    """Which long sets are shared out over workgroups, as the workspace shows: from n (1 - 1 / shares) = 31000 units on, where
+    there are two shares from 50000 on."""
+    n = ctypes.c_size_t(7)
+
+    def size(sets, units):
+        assert L.rc_select_workspace_size(sets, 1, units, 1, ctypes.byref(n)) == 0
+        return n.value
+
+    for sets, shares, least in ((1, 9, 34875), (32, 8, 35428), (51, 5, 38750), (64, 4, 41333), (85, 3, 46500), (100, 2, 100000), (128, 2, 100000)):
+        assert size(sets, least) == 0, (sets, least)
+        assert size(sets, least + 1) == 4 * (sets * shares * (4096 + 64 + 2) + sets * (least + 1)), (sets, least + 1)
+    assert size(129, 1 << 23) == 0
+
+
 def test_select_nothing_to_do(L):
     assert _select(L, sets=0, weight=NULL, idx=NULL) == 0
     assert _select(L, keep=0, first=0, last=0, weight=NULL, idx=NULL) == 0
