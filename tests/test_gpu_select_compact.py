@@ -201,6 +201,31 @@ def test_move_with_turned_keys(dtype, H, D, unit, units, keep, by_head, n_t, fpu
         assert np.array_equal(got[0, :unit, 0], plain[0, :unit, 0])  # did not move: copied
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("H,D,unit,n_t", [(12, 96, 30, 17), (12, 40, 47, 7), (5, 80, 60, 40), (3, 112, 73, 1), (1, 24, 1500, 5), (2, 8, 2100, 3), (7, 512, 9, 100)])
+def test_move_of_large_units_with_turned_keys(dtype, H, D, unit, n_t):
+    """Units of whole blocks that all heads share, at head sizes whose vectors do not divide a block: a thread's vectors lie in
+    different places of a head; the last turned pair lies inside a vector."""
+    rng = np.random.default_rng(D)
+    L, units, keep, theta, fpu, dst_pos = 2, 5, 3, 10000.0, 1, 9
+    assert unit * H * D * (2 if dtype == torch.bfloat16 else 4) // 16 >= 1024
+    src, dst = _kv(8, dtype, L, unit * units, H, D), _kv(9, dtype, L, unit * keep + 1, H, D)
+    after = [d[:, unit * keep:].clone() for d in dst]
+    sel = np.stack([[np.sort(rng.choice(units, keep, replace=False))] for _ in range(L)]).astype(np.int32)
+    delta = dst_pos + np.arange(keep) * fpu - sel.astype(np.int64) * fpu
+    x = _host(src[0])
+    want = OC.compact(x, sel, unit, _host(dst[0]), 0, delta, n_t, theta)
+    plain = OC.compact(x, sel, unit, _host(dst[0]), 0)
+    rv.compact_kv(*src, torch.from_numpy(sel).to(DEV), *dst, unit=unit, dst_pos=dst_pos, frames_per_unit=fpu, rope_t_pairs=n_t, rope_theta=theta)
+    got = _host(dst[0])
+    mag = np.repeat(np.abs(plain[..., 0::2]) + np.abs(plain[..., 1::2]), 2, axis=-1)
+    tol = 6 * 2.0 ** -24 * mag + (np.abs(want) * 2.0 ** -8 if dtype == torch.bfloat16 else 0.0)
+    assert (np.abs(got - want)[:, :unit * keep] <= tol[:, :unit * keep]).all()
+    assert np.array_equal(got[..., 2 * n_t:], plain[..., 2 * n_t:])
+    assert np.array_equal(_host(dst[1])[:, :unit * keep], OC.compact(_host(src[1]), sel, unit, _host(dst[1]), 0)[:, :unit * keep])
+    assert all(torch.equal(d[:, unit * keep:], a) for d, a in zip(dst, after))
+
+
 def test_move_of_infinite_keys_that_stay():
     k, v = _kv(5, torch.bfloat16, 1, 4, 1, 128)
     k[0, 1] = math.inf
