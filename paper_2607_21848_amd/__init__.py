@@ -420,9 +420,10 @@ def rotary_embed(q: torch.Tensor, k: Optional[torch.Tensor] = None, *, pairs: Se
     of a packed projection do). pairs = (time, row, column) pairs of the bands.
     Token r stands at (t0 + r // (h*w), r // w % h, r % w), or at pos[r] with pos
     [n, 3] i32. inverse=True turns back, which is also the gradient with respect
-    to q and k. out_dtype: q's, or float8_e4m3fn for bf16 (values times
-    fp8_scale = (q's, k's)). out = (q_out, k_out), which may be q and k themselves
-    where the type stays. Returns (q_out, k_out); k_out is None without k."""
+    to q and k: no autograd graph is recorded. out_dtype: q's, or float8_e4m3fn for
+    bf16 (values times fp8_scale = (q's, k's)). out = (q_out, k_out), which may be
+    q and k themselves where the type stays; else no output may overlap an input
+    or the other output. Returns (q_out, k_out); k_out is None without k."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor [n, heads, D]")
     dtype, index = q.dtype, q.get_device()
@@ -574,7 +575,7 @@ def compact_kv(src_k: torch.Tensor, src_v: torch.Tensor, sel: torch.Tensor, dst_
     src_k, src_v [L, rows, H, D], dst_k, dst_v [L, dst_rows, H, D] (bf16 or fp32,
     or fp8 keys with bf16 values); sel [L, 1 or H, keep] i32 units of `unit` rows
     (entries outside the source leave their rows as they are), going to rows
-    dst_row0 + i*unit. weight [L, H, >= rows of the units] and out_weight [L, H, >=
+    dst_row0 + i*unit. No destination may overlap a source or another destination. weight [L, H, >= rows of the units] and out_weight [L, H, >=
     dst_row0 + keep*unit] f32 move alike. With rope_t_pairs > 0 keys are turned from
     their unit's frame position (src_pos [units] i32, else u*frames_per_unit) to
     dst_pos + i*frames_per_unit."""
