@@ -30,6 +30,13 @@
  *   select_kept               -- which units of the cache to keep, by weight
  *   compact_kv                -- move of the kept units into a smaller cache
  *
+ * The paged cache, which many streams share:
+ *
+ *   append_paged_kv           -- new keys and values into their pages, keys
+ *                                with their rotary position, in 8 bits if
+ *                                wanted
+ *   paged_chunk_attention     -- biased_chunk_attention over the pages
+ *
  * and a streaming driver (rc_stream_*) that runs the paper's cache layout
  * chunk by chunk on the device.
  *
@@ -88,6 +95,9 @@ enum {
  * with bias 7, 3 mantissa bits, no infinities, 0x7f / 0xff NaN), v and o in
  * bf16. */
 enum { REVISIT_BF16 = 1, REVISIT_F32 = 2, REVISIT_FP8_QK = 3 };
+/* Pages of a paged cache in fp8 e4m3 with scales (append_paged_kv,
+ * paged_chunk_attention); q, k, v and o in bf16. */
+enum { REVISIT_FP8_KV = 4 };
 
 /* Correspondence reason codes written to out_idx by reproject_correspondence
  * and reproject_rotation (the rejection causes of Sec. 4.3, design choice
@@ -588,6 +598,131 @@ int compact_kv(const void* src_k, const void* src_v, int32_t src_rows,
                int32_t n_layers, int32_t dtype, int32_t H, int32_t D,
                const int32_t* src_pos, int32_t dst_pos, int32_t frames_per_unit,
                int32_t rope_t_pairs, float rope_theta, hipStream_t stream);
+
+/*
+ * The paged cache -- one pool of pages for the keys and values of many streams.
+ *
+ *   cache_k, cache_v  [n_pages][H][page][D] in the cache's type: a page holds
+ *                 `page` consecutive positions of one stream, head by head.
+ *                 page is a power of two in [32, 4096]; 16-byte aligned
+ *   page_table    [B][max_pages] int32: entry i of stream s is the page of its
+ *                 positions [i page, (i + 1) page). Pages may lie in any order.
+ *                 An entry outside [0, n_pages) is no page: what would be
+ *                 stored there is dropped, its keys are left out. Two entries
+ *                 may name one page for reading; for writing they must not
+ *                 (which of them is stored is undefined then)
+ *   kv_len        [B] int32: positions that stream s holds. Below 0 counts as
+ *                 0, beyond max_pages page as that
+ *   cu_tokens     nullable [B + 1] int32, ascending from 0: of the call's n_tokens
+ *                 tokens, stream s has cu_tokens[s] .. cu_tokens[s + 1] - 1 (none is
+ *                 valid). NULL: n_tokens / B each, which must be whole. Tokens
+ *                 behind cu_tokens[B] belong to nobody: they are not stored, and their
+ *                 rows of the outputs are left as they are. Values outside
+ *                 [0, n_tokens] count as its ends; where the list is not
+ *                 ascending it is undefined which tokens are processed
+ *   dtype         REVISIT_BF16, REVISIT_F32 (pages, q, k, v and o in this type) or
+ *                 REVISIT_FP8_KV: pages in e4m3, q, k, v and o in bf16. D = 64
+ *                 or 128
+ *   scale_k, scale_v  REVISIT_FP8_KV only: [n_pages][H][page / 32] bytes. The 32
+ *                 positions of a block share one scale per head, 2^(byte - 127); a
+ *                 stored value is its code times that, a bf16 value exactly. Byte 0
+ *                 counts as 1, and 255 is NaN.
+ */
+
+/*
+ * append_paged_kv -- new keys and values into the pages.
+ *
+ * Token i of stream s goes to position c = kv_len[s] + i - cu_tokens[s]: its value
+ * v[i] as it is, its key k[i] with the rotary embedding of rotary_embed at the
+ * position (time, row, column) given by pos[i], or with pos NULL at
+ * (t0 + c / (h w), c / w mod h, c mod w). Both are evaluated in fp32 with
+ * rotary_embed's precision and rounded once to the pages' type, to nearest
+ * even (values in their own type, and pairs behind the bands, are copied).
+ * Positions at and beyond max_pages page are dropped.
+ *
+ * Scales of REVISIT_FP8_KV, for keys and values each: where a block of 32
+ * positions holds nothing of the stream yet, its exponent is the least e >= -100
+ * with |x| <= 448 2^e for the finite values x of its new rows (e4m3 is a floating format, so
+ * a power of two leaves its normal values' precision as it is). Where it holds
+ * positions, the exponent is that or the stored one, whichever is larger; if
+ * it grows, the codes that are there are rounded to it again, to nearest even.
+ * What is not finite is stored as NaN.
+ *
+ *   k, v          [n_tokens] rows of [H][D] elements, row r starting k_row / v_row
+ *                 elements after row r - 1 (both may be views into the rows of one
+ *                 projection); rows start on 16 bytes
+ *   out_len       nullable [B] int32: the streams' new lengths, kv_len[s] plus its
+ *                 tokens, at most max_pages page. Not kv_len itself
+ *   pairs_t, pairs_y, pairs_x, theta, pos, t0, h, w  as for rotary_embed; all three 0:
+ *                 keys are copied
+ *
+ * No output (caches, scales, out_len) may overlap an input or another output
+ * (REVISIT_ERR_SHAPE). Rows of the pages that no token goes to are left as they are, but for
+ * the codes of a block whose scale grows. B == 0, and n_tokens == 0 without out_len, is
+ * valid (nothing to do). Two calls that may overlap in time must not write the
+ * same 32 positions.
+ */
+int append_paged_kv(const void* k, int64_t k_row, const void* v, int64_t v_row, int32_t dtype, int32_t n_tokens,
+                    const int32_t* cu_tokens, int32_t B, const int32_t* kv_len, int32_t* out_len,
+                    void* cache_k, void* cache_v, uint8_t* scale_k, uint8_t* scale_v,
+                    const int32_t* page_table, int32_t n_pages, int32_t page, int32_t max_pages,
+                    int32_t H, int32_t D, const int32_t* pos, int32_t t0, int32_t h, int32_t w,
+                    int32_t pairs_t, int32_t pairs_y, int32_t pairs_x, float theta, hipStream_t stream);
+
+/*
+ * paged_chunk_attention -- biased_chunk_attention over the pages, for the queries
+ * of many streams: a chunk of each, prompts of uneven lengths, single tokens.
+ *
+ * Query p of stream s attends to the keys at positions j < min(kv_len[s],
+ * visible[p]) of its stream that have a page, with the logits of
+ * biased_chunk_attention (kv_len counts the queries' own positions where they
+ * have been appended before):
+ *     A_pj = softmax_scale * q_p . k_j + lambda * B(p, j)
+ * Position j is token j mod (h w) of frame j / (h w) of the stream; the bias
+ * applies in frames whose slot is a retrieved frame, as there. Query head i
+ * reads key head i / (Hq / Hk). A query without a key has o = 0 and lse = -inf; keys that it does
+ * not see change nothing of it, whatever they and their values hold, NaN and
+ * infinities included.
+ *
+ *   q             [n_tokens] rows of [Hq][D], row r starting q_row elements after row
+ *                 r - 1, each on 16 bytes; o [n_tokens][Hq][D]; lse nullable
+ *                 [Hq][n_tokens] fp32
+ *   visible       nullable [n_tokens] int32: the first keys of its stream that a query
+ *                 sees (below 0 counts as 0); NULL: all of them. Causal: the
+ *                 query's own position plus one
+ *   kv_frame_slot [B][max_frames] int32: s in [0, S) for a retrieved frame, any
+ *                 other value = unbiased; frames from max_frames on are unbiased
+ *   corr_uv [S][n_tokens][2] fp32, corr_idx [S][n_tokens] int32, S, lambda, sigma, softmax_scale
+ *                 as for biased_chunk_attention; S == 0 or lambda == 0: no bias (h, w and
+ *                 the pointers are then not read). With the bias on, bf16 and 8 bits
+ *                 take token grids of at most 256 x 256
+ *   max_keys      0, or the longest stream's length if the caller knows it: the key
+ *                 split is chosen for it instead of max_pages page. No other meaning
+ *   key_parts     0 = chosen from the shape and the compute units of the current
+ *                 device, or a fixed number in [1, 64] of parts into which the
+ *                 keys of every tile of queries are cut; a second kernel joins them
+ *   workspace, workspace_bytes  device scratch of at least the size
+ *                 rc_paged_attention_workspace_size() returns for the same arguments on the
+ *                 same device (ragged: whether cu_tokens is given), 16-byte aligned; may be NULL / 0 when that size is 0.
+ *                 Too small: REVISIT_ERR_SHAPE; NULL while needed: REVISIT_ERR_NULL
+ *
+ * Hq is a multiple of Hk; n_tokens Hq / Hk <= 2^30. q must not overlap o; outputs
+ * must not overlap inputs (REVISIT_ERR_SHAPE). Sums, maxima and logits are fp32,
+ * probabilities are rounded to bf16 for the product with the values (fp32 pages: not at all), outputs once.
+ * n_tokens == 0 or B == 0 is valid (nothing to do). Results do not change between calls (no atomics).
+ */
+int paged_chunk_attention(const void* q, int64_t q_row, const void* cache_k, const void* cache_v,
+                          const uint8_t* scale_k, const uint8_t* scale_v, void* o, float* lse, int32_t dtype,
+                          int32_t n_tokens, const int32_t* cu_tokens, int32_t B, const int32_t* kv_len, const int32_t* visible,
+                          const int32_t* page_table, int32_t n_pages, int32_t page, int32_t max_pages,
+                          int32_t Hq, int32_t Hk, int32_t D, int32_t h, int32_t w,
+                          const int32_t* kv_frame_slot, int32_t max_frames,
+                          const float* corr_uv, const int32_t* corr_idx, int32_t S,
+                          float softmax_scale, float lambda, float sigma,
+                          int32_t max_keys, int32_t key_parts, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+int rc_paged_attention_workspace_size(int32_t dtype, int32_t n_tokens, int32_t ragged, int32_t B, int32_t Hq, int32_t Hk, int32_t D,
+                                      int32_t page, int32_t max_pages, int32_t max_keys, int32_t key_parts, size_t* bytes);
 
 /*
  * Streaming driver -- Sec. 4.2 (cache layout, loop-closure retrieval, cache

@@ -16,12 +16,15 @@ current HIP stream. The entry points mirror include/revisit.h:
 * ``attention_key_weight``     -- the weight of every cached key in the attention
 * ``select_kept``              -- which units of the cache to keep, by weight
 * ``compact_kv``               -- move of the kept units into a smaller cache
+* ``append_paged_kv``          -- new keys and values of many streams into the
+                                  pages of their cache, keys turned to their positions
+* ``paged_chunk_attention``    -- the attention over those pages, in the queries' type or 8 bits
 
 Each accepts optional preallocated outputs (``out=``) and, where a kernel
 needs scratch memory, a preallocated ``workspace=`` (a uint8 GPU tensor of at
 least ``attention_workspace_size(...)`` / ``retrieve_workspace_size(...)`` /
-``key_weight_workspace_size(...)`` / ``select_workspace_size(...)`` bytes), so
-a caller can run the path without allocating; without one the binding
+``key_weight_workspace_size(...)`` / ``select_workspace_size(...)`` /
+``paged_attention_workspace_size(...)`` bytes), so a caller can run the path without allocating; without one the binding
 allocates the workspace with torch on the current stream.
 """
 
@@ -33,12 +36,13 @@ from typing import Optional, Sequence
 import torch
 
 from . import _lib
-from ._lib import BF16, F32, FP8_QK, MAX_K, RevisitError, last_error, lib, status_string  # noqa: F401
+from ._lib import BF16, F32, FP8_KV, FP8_QK, MAX_K, RevisitError, last_error, lib, status_string  # noqa: F401
 
 __all__ = ["retrieve_chunks", "reproject_correspondence", "reproject_rotation", "biased_chunk_attention", "pack_retrieved_kv",
-           "pool_token_depth", "rotary_embed", "attention_key_weight", "select_kept", "compact_kv", "StreamDriver",
+           "pool_token_depth", "rotary_embed", "attention_key_weight", "select_kept", "compact_kv", "append_paged_kv", "paged_chunk_attention",
+           "StreamDriver",
            "attention_workspace_size", "retrieve_workspace_size", "key_weight_workspace_size", "select_workspace_size",
-           "RevisitError", "lib"]
+           "paged_attention_workspace_size", "RevisitError", "lib"]
 
 
 # The small calls are as long as their marshalling (a launch itself is 4 us):
@@ -615,6 +619,154 @@ def compact_kv(src_k: torch.Tensor, src_v: torch.Tensor, sel: torch.Tensor, dst_
     _call(dev.index, "compact_kv", _ptr(src_k), _ptr(src_v), rows, _ptr(sel), sel.shape[1], sel.shape[2], unit, n_units, _ptr(dst_k),
           _ptr(dst_v), dst_rows, dst_row0, _ptr(weight), cols, _ptr(out_weight), dst_cols, L, dt, H, D, _ptr(src_pos), dst_pos,
           frames_per_unit, rope_t_pairs, rope_theta)
+
+
+# type of a paged cache by that of its pages, and the type of q, k, v and o beside it
+_PAGED_DTYPES = {torch.bfloat16: (BF16, torch.bfloat16), torch.float32: (F32, torch.float32), torch.float8_e4m3fn: (FP8_KV, torch.bfloat16)}
+
+
+def _pages(cache_k, cache_v, scale_k, scale_v, page_table, kv_len, cu, n, dev):
+    """Checks a paged cache's tensors; (type, type of q, k, v and o, n_pages, H, page, D, B, max_pages)."""
+    if not isinstance(cache_k, torch.Tensor) or cache_k.dim() != 4:
+        raise ValueError("cache_k must be a tensor [pages, heads, page, D]")
+    dt, idt = _PAGED_DTYPES.get(cache_k.dtype, (None, None))
+    if dt is None:
+        raise TypeError(f"cache_k must be bfloat16, float32 or float8_e4m3fn (got {cache_k.dtype})")
+    if not cache_k.is_cuda:
+        raise ValueError(f"cache_k must be a GPU tensor (got {cache_k.device}); there is no CPU path")
+    n_pages, H, page, D = cache_k.shape
+    _need(cache_k, "cache_k", cache_k.dtype, None, dev)
+    _need(cache_v, "cache_v", cache_k.dtype, (n_pages, H, page, D), dev)
+    if dt == FP8_KV:
+        _need(scale_k, "scale_k", torch.float8_e8m0fnu, (n_pages, H, page // 32), dev)
+        _need(scale_v, "scale_v", torch.float8_e8m0fnu, (n_pages, H, page // 32), dev)
+    elif scale_k is not None or scale_v is not None:
+        raise ValueError("scale_k and scale_v belong to float8_e4m3fn pages")
+    _need(page_table, "page_table", torch.int32, None, dev)
+    if page_table.dim() != 2:
+        raise ValueError(f"page_table has shape {tuple(page_table.shape)}, expected (streams, pages of a stream)")
+    B, max_pages = page_table.shape
+    _need(kv_len, "kv_len", torch.int32, (B,), dev)
+    if cu is not None:
+        _need(cu, "cu", torch.int32, (B + 1,), dev)
+    elif n % B if B else n:
+        raise ValueError(f"{n} tokens are not shared evenly by {B} streams: give cu")
+    return dt, idt, n_pages, H, page, D, B, max_pages
+
+
+def append_paged_kv(k: torch.Tensor, v: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tensor, page_table: torch.Tensor,
+                    kv_len: torch.Tensor, *, pairs: Sequence[int], theta: float, cu: Optional[torch.Tensor] = None,
+                    scale_k: Optional[torch.Tensor] = None, scale_v: Optional[torch.Tensor] = None, h: int = 0, w: int = 0, t0: int = 0,
+                    pos: Optional[torch.Tensor] = None, out_len: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """New keys and values of many streams into the pages of their cache, in place.
+
+    k, v [n, H, D] (rows may lie apart, as views of a packed projection do); cache_k,
+    cache_v [pages, H, page, D] in the type of k and v (bf16, fp32), or
+    float8_e4m3fn for bf16 k and v, with scale_k, scale_v [pages, H, page // 32]
+    float8_e8m0fnu: a power of two for each 32 positions of a head. page_table
+    [B, pages of a stream] i32, kv_len [B] i32 the positions that the streams hold.
+    Stream s has tokens cu[s] .. cu[s+1]-1 of the n (cu [B+1] i32; None: n // B
+    each); they go to its positions kv_len[s] on. Keys get the rotary position of
+    rotary_embed (pairs, theta): position c stands at (t0 + c // (h*w), c // w % h,
+    c % w), or a token at pos[i] with pos [n, 3] i32. Returns the new lengths [B]
+    i32 (out_len, which must not be kv_len)."""
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError("k must be a tensor [n, heads, D]")
+    n = k.shape[0]
+    dev = k.device
+    dt, idt, n_pages, H, page, D, B, max_pages = _pages(cache_k, cache_v, scale_k, scale_v, page_table, kv_len, cu, n, dev)
+    Hk, k_row = _rows(k, "k", idt, n, D, dev.index)
+    Hv, v_row = _rows(v, "v", idt, n, D, dev.index)
+    if Hk != H or Hv != H:
+        raise ValueError(f"k and v have {Hk} and {Hv} heads, expected {H}")
+    if pos is not None:
+        _need(pos, "pos", torch.int32, (n, 3), dev)
+    if out_len is None:
+        out_len = torch.empty((B,), dtype=torch.int32, device=dev)
+    else:
+        _need(out_len, "out_len", torch.int32, (B,), dev)
+    nt, ny, nx = pairs
+    _call(dev.index, "append_paged_kv", k.data_ptr(), k_row, v.data_ptr(), v_row, dt, n, _ptr(cu), B, kv_len.data_ptr(), out_len.data_ptr(),
+          cache_k.data_ptr(), cache_v.data_ptr(), _ptr(scale_k), _ptr(scale_v), page_table.data_ptr(), n_pages, page, max_pages, H, D,
+          _ptr(pos), t0, h, w, nt, ny, nx, theta)
+    return out_len
+
+
+def paged_attention_workspace_size(dtype: torch.dtype, n: int, ragged: bool, B: int, Hq: int, Hk: int, D: int, page: int, max_pages: int,
+                                   max_keys: int = 0, key_parts: int = 0) -> int:
+    """Bytes of workspace paged_chunk_attention needs on the current device (dtype: of the pages; ragged: with cu)."""
+    dt = _PAGED_DTYPES.get(dtype, (None,))[0]
+    if dt is None:
+        raise TypeError(f"pages must be bfloat16, float32 or float8_e4m3fn (got {dtype})")
+    size = ctypes.c_size_t(0)
+    st = (_lib._LIB or lib()).rc_paged_attention_workspace_size(dt, n, 1 if ragged else 0, B, Hq, Hk, D, page, max_pages, max_keys, key_parts,
+                                                               ctypes.byref(size))
+    if st:
+        _lib.check("rc_paged_attention_workspace_size", st)
+    return size.value
+
+
+def paged_chunk_attention(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tensor, page_table: torch.Tensor, kv_len: torch.Tensor, *,
+                          softmax_scale: float, cu: Optional[torch.Tensor] = None, scale_k: Optional[torch.Tensor] = None,
+                          scale_v: Optional[torch.Tensor] = None, visible: Optional[torch.Tensor] = None,
+                          kv_frame_slot: Optional[torch.Tensor] = None, corr_uv: Optional[torch.Tensor] = None,
+                          corr_idx: Optional[torch.Tensor] = None, h: int = 0, w: int = 0, lam: float = 0.0, sigma: float = 1.0,
+                          max_keys: int = 0, key_parts: int = 0, return_lse: bool = True, out=None,
+                          workspace: Optional[torch.Tensor] = None):
+    """biased_chunk_attention over the pages of a cache, for the queries of many streams.
+
+    q [n, Hq, D] (rows may lie apart), the pages, page_table, kv_len, cu and scales
+    as for append_paged_kv; Hq is a multiple of the pages' heads. kv_len counts all
+    keys of a stream, those appended for these queries included. visible None or
+    [n] i32: the first keys of its stream that a query sees (causal: its own
+    position + 1); a query without a key has o = 0 and lse = -inf. The bias, where
+    corr_uv [S, n, 2] f32 and corr_idx [S, n] i32 are given: kv_frame_slot [B, frames]
+    i32, position j of a stream being token j % (h*w) of its frame j // (h*w).
+    max_keys: the longest stream's length if it is known, for the choice of the key
+    split only. Returns (o [n, Hq, D], lse [Hq, n] f32 or None)."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a tensor [n, heads, D]")
+    n, _, D = q.shape
+    dev = q.device
+    dt, idt, n_pages, Hk, page, Dk, B, max_pages = _pages(cache_k, cache_v, scale_k, scale_v, page_table, kv_len, cu, n, dev)
+    Hq, q_row = _rows(q, "q", idt, n, Dk, dev.index)
+    if Hq % Hk:
+        raise ValueError(f"{Hq} query heads are not a multiple of {Hk} key heads")
+    if visible is not None:
+        _need(visible, "visible", torch.int32, (n,), dev)
+    S = frames = 0
+    if corr_uv is not None:
+        S = corr_uv.shape[0]
+        _need(corr_uv, "corr_uv", torch.float32, (S, n, 2), dev)
+        _need(corr_idx, "corr_idx", torch.int32, (S, n), dev)
+        _need(kv_frame_slot, "kv_frame_slot", torch.int32, None, dev)
+        if kv_frame_slot.dim() != 2 or kv_frame_slot.shape[0] != B:
+            raise ValueError(f"kv_frame_slot has shape {tuple(kv_frame_slot.shape)}, expected ({B}, frames)")
+        frames = kv_frame_slot.shape[1]
+    if out is None:
+        o = torch.empty((n, Hq, D), dtype=idt, device=dev)
+        lse = torch.empty((Hq, n), dtype=torch.float32, device=dev) if return_lse else None
+    else:
+        o, lse = out
+        _need(o, "o", idt, (n, Hq, D), dev)
+        if lse is not None:
+            _need(lse, "lse", torch.float32, (Hq, n), dev)
+    if workspace is not None:
+        _need(workspace, "workspace", torch.uint8, None, dev)
+    else:
+        size = (cache_k.dtype, n, cu is not None, B, Hq, Hk, D, page, max_pages, max_keys, key_parts)
+        if _current_device() == dev.index:
+            nbytes = paged_attention_workspace_size(*size)
+        else:
+            with torch.cuda.device(dev):
+                nbytes = paged_attention_workspace_size(*size)
+        if nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _call(dev.index, "paged_chunk_attention", q.data_ptr(), q_row, cache_k.data_ptr(), cache_v.data_ptr(), _ptr(scale_k), _ptr(scale_v),
+          o.data_ptr(), _ptr(lse), dt, n, _ptr(cu), B, kv_len.data_ptr(), _ptr(visible), page_table.data_ptr(), n_pages, page, max_pages,
+          Hq, Hk, D, h, w, _ptr(kv_frame_slot), frames, _ptr(corr_uv), _ptr(corr_idx), S, softmax_scale, lam, sigma, max_keys, key_parts,
+          _ptr(workspace), workspace.numel() if workspace is not None else 0)
+    return o, lse
 
 
 class StreamDriver:

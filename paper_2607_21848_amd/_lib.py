@@ -14,14 +14,14 @@ _LIB = None
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "librevisit.so")
 
 OK, ERR_NULL, ERR_SHAPE, ERR_UNSUPPORTED, ERR_PARAM, ERR_LAUNCH, ERR_MEMORY = 0, 1, 2, 3, 4, 5, 6
-BF16, F32, FP8_QK = 1, 2, 3
+BF16, F32, FP8_QK, FP8_KV = 1, 2, 3, 4
 MAX_K = 32
 EXPORTED = ("rc_status_string", "rc_last_error", "retrieve_chunks", "reproject_correspondence",
             "reproject_rotation", "biased_chunk_attention", "biased_chunk_attention_noalloc", "rc_retrieve_workspace_size",
             "rc_attention_workspace_size",
             "pack_retrieved_kv", "pool_token_depth", "rc_stream_create", "rc_stream_step", "rc_stream_view",
             "rc_stream_destroy", "rotary_embed", "attention_key_weight", "rc_key_weight_workspace_size", "select_kept",
-            "rc_select_workspace_size", "compact_kv")
+            "rc_select_workspace_size", "compact_kv", "append_paged_kv", "paged_chunk_attention", "rc_paged_attention_workspace_size")
 
 _p = ctypes.c_void_p
 _i = ctypes.c_int32
@@ -110,6 +110,14 @@ def lib() -> ctypes.CDLL:
         L.compact_kv.restype = ctypes.c_int
         L.compact_kv.argtypes = [_p, _p, _i, _p, _i, _i, _i, _i, _p, _p, _i, _i, _p, _i, _p, _i, _i, _i, _i, _i, _p, _i, _i,
                                  _i, _f, _p]
+        L.append_paged_kv.restype = ctypes.c_int
+        L.append_paged_kv.argtypes = [_p, _l, _p, _l, _i, _i, _p, _i, _p, _p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _p, _i, _i,
+                                      _i, _i, _i, _i, _f, _p]
+        L.paged_chunk_attention.restype = ctypes.c_int
+        L.paged_chunk_attention.argtypes = [_p, _l, _p, _p, _p, _p, _p, _p, _i, _i, _p, _i, _p, _p, _p, _i, _i, _i, _i, _i, _i, _i,
+                                            _i, _p, _i, _p, _p, _i, _f, _f, _f, _i, _i, _p, _z, _p]
+        L.rc_paged_attention_workspace_size.restype = ctypes.c_int
+        L.rc_paged_attention_workspace_size.argtypes = [_i] * 11 + [ctypes.POINTER(ctypes.c_size_t)]
         _LIB = L
     return _LIB
 

@@ -936,3 +936,264 @@ int compact_kv(const void* src_k, const void* src_v, int32_t src_rows, const int
 }
 
 }  // extern "C"
+
+namespace {
+
+// What append_paged_kv and paged_chunk_attention check alike; fills `q`.
+int check_paged(const char* fn, int32_t dtype, int32_t n_tokens, const int32_t* cu_tokens, int32_t B, const int32_t* kv_len,
+                const int32_t* page_table, int32_t n_pages, int32_t page, int32_t max_pages, int32_t H, int32_t D,
+                revisit::PagedSeqs& q) {
+    if (dtype != REVISIT_BF16 && dtype != REVISIT_F32 && dtype != REVISIT_FP8_KV)
+        return fail(REVISIT_ERR_UNSUPPORTED, "%s: dtype %d not supported", fn, dtype);
+    if (D != 64 && D != 128) return fail(REVISIT_ERR_UNSUPPORTED, "%s: D = 64 or 128 (got %d)", fn, D);
+    if (H < 1 || H > 65535) return fail(REVISIT_ERR_SHAPE, "%s: need 1 to 65535 heads", fn);
+    if (n_tokens < 0 || n_tokens > (1 << 30) || B < 0 || B > (1 << 20) || n_pages < 0 || max_pages < 0)
+        return fail(REVISIT_ERR_SHAPE, "%s: need 0 <= n_tokens <= 2^30, 0 <= B <= 2^20, n_pages, max_pages >= 0", fn);
+    if (page < 32 || page > 4096 || (page & (page - 1)) != 0)
+        return fail(REVISIT_ERR_SHAPE, "%s: page=%d is not a power of two in [32, 4096]", fn, page);
+    if ((int64_t)max_pages * page > (1 << 30)) return fail(REVISIT_ERR_SHAPE, "%s: more than 2^30 positions in a stream", fn);
+    if ((double)n_pages * page * H * D > (double)kMaxElems) return fail(REVISIT_ERR_SHAPE, "%s: cache too large", fn);
+    if (!cu_tokens && (B ? n_tokens % B : n_tokens) != 0)
+        return fail(REVISIT_ERR_SHAPE, "%s: %d tokens are not shared evenly by %d streams (cu_tokens is NULL)", fn, n_tokens, B);
+    if (!aligned(cu_tokens, 4) || !aligned(kv_len, 4) || !aligned(page_table, 4))
+        return fail(REVISIT_ERR_SHAPE, "%s: cu_tokens, kv_len and page_table must be 4-byte aligned", fn);
+    q.cu = cu_tokens;
+    q.kv_len = kv_len;
+    q.page_table = page_table;
+    q.n_tokens = n_tokens;
+    q.B = B;
+    q.per = B ? n_tokens / B : 0;
+    q.n_pages = n_pages;
+    q.max_pages = max_pages;
+    q.page_log2 = __builtin_ctz((unsigned)page);
+    return REVISIT_OK;
+}
+
+int check_paged_pointers(const char* fn, const revisit::PagedSeqs& q, int32_t dtype, const void* cache_k, const void* cache_v,
+                         const uint8_t* scale_k, const uint8_t* scale_v) {
+    if (!q.kv_len) return fail(REVISIT_ERR_NULL, "%s: kv_len is required", fn);
+    if (q.max_pages > 0 && !q.page_table) return fail(REVISIT_ERR_NULL, "%s: page_table is required", fn);
+    if (q.n_pages > 0 && (!cache_k || !cache_v)) return fail(REVISIT_ERR_NULL, "%s: cache_k and cache_v are required", fn);
+    if (q.n_pages > 0 && dtype == REVISIT_FP8_KV && (!scale_k || !scale_v))
+        return fail(REVISIT_ERR_NULL, "%s: pages of 8 bits need scale_k and scale_v", fn);
+    if (!aligned(cache_k, 16) || !aligned(cache_v, 16)) return fail(REVISIT_ERR_SHAPE, "%s: cache_k and cache_v must be 16-byte aligned", fn);
+    return REVISIT_OK;
+}
+
+// A range of memory that a call reads or writes.
+struct Range {
+    const char* name;
+    const void* at;
+    double bytes;
+};
+
+// Refuses a written range that shares a byte with a read one or with another written one.
+int check_apart(const char* fn, const Range* written, int n_written, const Range* read, int n_read) {
+    for (int i = 0; i < n_written; ++i) {
+        if (!written[i].at) continue;
+        for (int j = i + 1; j < n_written; ++j)
+            if (written[j].at && overlap(written[i].at, written[i].bytes, written[j].at, written[j].bytes))
+                return fail(REVISIT_ERR_SHAPE, "%s: %s and %s overlap", fn, written[i].name, written[j].name);
+        for (int j = 0; j < n_read; ++j)
+            if (read[j].at && overlap(written[i].at, written[i].bytes, read[j].at, read[j].bytes))
+                return fail(REVISIT_ERR_SHAPE, "%s: %s overlaps %s", fn, written[i].name, read[j].name);
+    }
+    return REVISIT_OK;
+}
+
+// Shape checks and plan shared by paged_chunk_attention and its workspace query (H is Hk).
+int plan_paged_attention(const char* fn, int32_t Hq, int32_t max_keys, int32_t key_parts, revisit::PagedAttentionArgs& a, size_t* bytes) {
+    *bytes = 0;
+    if (Hq < 1 || Hq > 65535 || Hq % a.Hk != 0)
+        return fail(REVISIT_ERR_SHAPE, "%s: Hq=%d is not a multiple of Hk=%d in [1, 65535]", fn, Hq, a.Hk);
+    a.Hq = Hq;
+    a.G = Hq / a.Hk;
+    if ((int64_t)a.seqs.n_tokens * a.G > (1 << 30) || (double)a.seqs.n_tokens * Hq * a.D > (double)kMaxElems)
+        return fail(REVISIT_ERR_SHAPE, "%s: problem too large", fn);
+    if (max_keys < 0) return fail(REVISIT_ERR_PARAM, "%s: max_keys=%d", fn, max_keys);
+    if (key_parts < 0 || key_parts > revisit::kPagedMaxParts)
+        return fail(REVISIT_ERR_PARAM, "%s: key_parts=%d outside [0, %d]", fn, key_parts, revisit::kPagedMaxParts);
+    if (a.seqs.n_tokens == 0 || a.seqs.B == 0) return REVISIT_OK;
+    int cus = 256;
+    const hipError_t e = device_compute_units(&cus);
+    if (e != hipSuccess) {
+        // without a device only a fixed split has a size
+        if (key_parts == 0) return fail(REVISIT_ERR_LAUNCH, "%s: device query failed: %s", fn, hipGetErrorString(e));
+        (void)hipGetLastError();
+    }
+    *bytes = revisit::paged_plan(a, key_parts, max_keys ? max_keys : INT32_MAX, cus);
+    if (revisit::paged_units(a) > (double)(1 << 30)) return fail(REVISIT_ERR_SHAPE, "%s: problem too large", fn);
+    return REVISIT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int append_paged_kv(const void* k, int64_t k_row, const void* v, int64_t v_row, int32_t dtype, int32_t n_tokens,
+                    const int32_t* cu_tokens, int32_t B, const int32_t* kv_len, int32_t* out_len, void* cache_k, void* cache_v,
+                    uint8_t* scale_k, uint8_t* scale_v, const int32_t* page_table, int32_t n_pages, int32_t page, int32_t max_pages,
+                    int32_t H, int32_t D, const int32_t* pos, int32_t t0, int32_t h, int32_t w, int32_t pairs_t, int32_t pairs_y,
+                    int32_t pairs_x, float theta, hipStream_t stream) {
+    const char* fn = "append_paged_kv";
+    revisit::PagedAppendArgs a{};
+    int st = check_paged(fn, dtype, n_tokens, cu_tokens, B, kv_len, page_table, n_pages, page, max_pages, H, D, a.seqs);
+    if (st != REVISIT_OK) return st;
+    if (pairs_t < 0 || pairs_y < 0 || pairs_x < 0 || (int64_t)pairs_t + pairs_y + pairs_x > D / 2)
+        return fail(REVISIT_ERR_PARAM, "%s: bands of %d + %d + %d pairs in a head of %d", fn, pairs_t, pairs_y, pairs_x, D / 2);
+    if (!(finite(theta) && theta > 0.0f)) return fail(REVISIT_ERR_PARAM, "%s: theta must be finite and > 0", fn);
+    if (!pos && (h < 1 || w < 1 || (int64_t)h * w > INT32_MAX))
+        return fail(REVISIT_ERR_SHAPE, "%s: without positions the token grid is needed: h, w >= 1", fn);
+    const int esize = dtype == REVISIT_F32 ? 4 : 2, osize = dtype == REVISIT_FP8_KV ? 1 : esize;
+    const int64_t row = (int64_t)H * D, most = kMaxElems / (n_tokens > 1 ? n_tokens : 1);
+    if (k_row < row || v_row < row || k_row > most || v_row > most)
+        return fail(REVISIT_ERR_SHAPE, "%s: a row stride is below the row's %lld elements or too large", fn, (long long)row);
+    if (k_row * esize % 16 != 0 || v_row * esize % 16 != 0) return fail(REVISIT_ERR_SHAPE, "%s: rows of k and v must start on 16 bytes", fn);
+    if (B == 0 || (n_tokens == 0 && !out_len)) return REVISIT_OK;
+    if (n_tokens > 0 && (!k || !v)) return fail(REVISIT_ERR_NULL, "%s: k and v are required", fn);
+    st = check_paged_pointers(fn, a.seqs, dtype, cache_k, cache_v, scale_k, scale_v);
+    if (st != REVISIT_OK) return st;
+    if (!aligned(k, 16) || !aligned(v, 16)) return fail(REVISIT_ERR_SHAPE, "%s: k and v must be 16-byte aligned", fn);
+    if (!aligned(out_len, 4) || !aligned(pos, 4)) return fail(REVISIT_ERR_SHAPE, "%s: out_len and pos must be 4-byte aligned", fn);
+    const bool fp8 = dtype == REVISIT_FP8_KV;
+    const double positions = (double)n_pages * page * H, in_k = n_tokens ? ((double)(n_tokens - 1) * k_row + row) * esize : 0.0,
+                 in_v = n_tokens ? ((double)(n_tokens - 1) * v_row + row) * esize : 0.0;
+    const Range written[] = {{"cache_k", cache_k, positions * D * osize},
+                             {"cache_v", cache_v, positions * D * osize},
+                             {"scale_k", fp8 ? scale_k : nullptr, positions / 32},
+                             {"scale_v", fp8 ? scale_v : nullptr, positions / 32},
+                             {"out_len", out_len, 4.0 * B}};
+    const Range read[] = {{"k", k, in_k},
+                          {"v", v, in_v},
+                          {"cu_tokens", cu_tokens, 4.0 * (B + 1.0)},
+                          {"kv_len", kv_len, 4.0 * B},
+                          {"page_table", page_table, 4.0 * B * max_pages},
+                          {"pos", pos, 12.0 * n_tokens}};
+    st = check_apart(fn, written, 5, read, 6);
+    if (st != REVISIT_OK) return st;
+    a.k = k;
+    a.v = v;
+    a.k_row_bytes = k_row * esize;
+    a.v_row_bytes = v_row * esize;
+    a.cache_k = cache_k;
+    a.cache_v = cache_v;
+    a.scale_k = scale_k;
+    a.scale_v = scale_v;
+    a.out_len = out_len;
+    a.dtype = dtype;
+    a.H = H;
+    a.D = D;
+    a.pos = pos;
+    a.t0 = t0;
+    a.hw = pos ? 1 : h * w;
+    a.w = pos ? 1 : w;
+    a.n_t = pairs_t;
+    a.n_y = pairs_y;
+    a.n_x = pairs_x;
+    const int pairs = pairs_t + pairs_y + pairs_x;
+    a.inv_pairs = pairs > 0 ? 1.0f / (float)pairs : 0.0f;
+    if (revisit::paged_append_blocks(a) > (1 << 30)) return fail(REVISIT_ERR_SHAPE, "%s: problem too large", fn);
+    revisit::PagedFreq f;
+    band_quarters((double)theta, pairs_t, f.quarter);
+    band_quarters((double)theta, pairs_y, f.quarter + pairs_t);
+    band_quarters((double)theta, pairs_x, f.quarter + pairs_t + pairs_y);
+    return launched(revisit::launch_paged_append(a, f, stream), fn);
+}
+
+int rc_paged_attention_workspace_size(int32_t dtype, int32_t n_tokens, int32_t ragged, int32_t B, int32_t Hq, int32_t Hk, int32_t D,
+                                      int32_t page, int32_t max_pages, int32_t max_keys, int32_t key_parts, size_t* bytes) {
+    const char* fn = "rc_paged_attention_workspace_size";
+    if (!bytes) return fail(REVISIT_ERR_NULL, "%s: bytes is NULL", fn);
+    *bytes = 0;
+    static const int32_t list = 0;  // stands for a list; never read
+    revisit::PagedAttentionArgs a{};
+    const int st = check_paged(fn, dtype, n_tokens, ragged ? &list : nullptr, B, nullptr, nullptr, 0, page, max_pages, Hk, D, a.seqs);
+    if (st != REVISIT_OK) return st;
+    a.dtype = dtype;
+    a.Hk = Hk;
+    a.D = D;
+    return plan_paged_attention(fn, Hq, max_keys, key_parts, a, bytes);
+}
+
+int paged_chunk_attention(const void* q, int64_t q_row, const void* cache_k, const void* cache_v, const uint8_t* scale_k,
+                          const uint8_t* scale_v, void* o, float* lse, int32_t dtype, int32_t n_tokens, const int32_t* cu_tokens, int32_t B,
+                          const int32_t* kv_len, const int32_t* visible, const int32_t* page_table, int32_t n_pages, int32_t page,
+                          int32_t max_pages, int32_t Hq, int32_t Hk, int32_t D, int32_t h, int32_t w, const int32_t* kv_frame_slot,
+                          int32_t max_frames, const float* corr_uv, const int32_t* corr_idx, int32_t S, float softmax_scale, float lambda,
+                          float sigma, int32_t max_keys, int32_t key_parts, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    const char* fn = "paged_chunk_attention";
+    revisit::PagedAttentionArgs a{};
+    int st = check_paged(fn, dtype, n_tokens, cu_tokens, B, kv_len, page_table, n_pages, page, max_pages, Hk, D, a.seqs);
+    if (st != REVISIT_OK) return st;
+    a.dtype = dtype;
+    a.Hk = Hk;
+    a.D = D;
+    size_t need = 0;
+    st = plan_paged_attention(fn, Hq, max_keys, key_parts, a, &need);
+    if (st != REVISIT_OK) return st;
+    if (!(finite(softmax_scale) && softmax_scale > 0.0f)) return fail(REVISIT_ERR_PARAM, "%s: softmax_scale must be finite and > 0", fn);
+    if (S < 0) return fail(REVISIT_ERR_SHAPE, "%s: S=%d", fn, S);
+    const bool bias = S > 0 && lambda != 0.0f;
+    if (S > 0 && !finite(lambda)) return fail(REVISIT_ERR_PARAM, "%s: lambda must be finite", fn);
+    if (bias) {
+        if (!(finite(sigma) && sigma > 0.0f)) return fail(REVISIT_ERR_PARAM, "%s: sigma must be finite and > 0", fn);
+        a.gamma = lambda / (2.0f * sigma * sigma * softmax_scale);
+        if (!finite(a.gamma)) return fail(REVISIT_ERR_PARAM, "%s: lambda / (2 sigma^2 softmax_scale) is not finite", fn);
+        if (h < 1 || w < 1 || (int64_t)h * w > INT32_MAX) return fail(REVISIT_ERR_SHAPE, "%s: the bias needs a token grid: h, w >= 1", fn);
+        if (dtype != REVISIT_F32 && (h > kMaxGridSide || w > kMaxGridSide))
+            return fail(REVISIT_ERR_SHAPE, "%s: bf16 / 8 bits with bias needs h, w <= %d (got %d x %d)", fn, kMaxGridSide, h, w);
+        if (max_frames < 0 || (double)S * n_tokens > (double)kMaxElems) return fail(REVISIT_ERR_SHAPE, "%s: max_frames=%d, S=%d", fn, max_frames, S);
+    }
+    const int64_t row = (int64_t)Hq * D, most = kMaxElems / (n_tokens > 1 ? n_tokens : 1);
+    const int esize = dtype == REVISIT_F32 ? 4 : 2;
+    if (q_row < row || q_row > most) return fail(REVISIT_ERR_SHAPE, "%s: q_row is below the row's %lld elements or too large", fn, (long long)row);
+    if (q_row * esize % 16 != 0) return fail(REVISIT_ERR_SHAPE, "%s: rows of q must start on 16 bytes", fn);
+    if (n_tokens == 0 || B == 0) return REVISIT_OK;
+    if (!q || !o) return fail(REVISIT_ERR_NULL, "%s: q and o are required", fn);
+    st = check_paged_pointers(fn, a.seqs, dtype, cache_k, cache_v, scale_k, scale_v);
+    if (st != REVISIT_OK) return st;
+    if (bias && ((max_frames > 0 && !kv_frame_slot) || !corr_uv || !corr_idx))
+        return fail(REVISIT_ERR_NULL, "%s: the bias needs kv_frame_slot, corr_uv and corr_idx", fn);
+    if (!aligned(q, 16) || !aligned(o, 16)) return fail(REVISIT_ERR_SHAPE, "%s: q and o must be 16-byte aligned", fn);
+    if (!aligned(lse, 4) || !aligned(visible, 4) || (bias && (!aligned(kv_frame_slot, 4) || !aligned(corr_uv, 8) || !aligned(corr_idx, 4))))
+        return fail(REVISIT_ERR_SHAPE, "%s: lse, visible, kv_frame_slot and corr_idx must be 4-byte, corr_uv 8-byte aligned", fn);
+    const double out = (double)n_tokens * row * esize, cache = (double)n_pages * page * Hk * D * (dtype == REVISIT_FP8_KV ? 1 : esize);
+    const Range written[] = {{"o", o, out}, {"lse", lse, 4.0 * Hq * n_tokens}, {"workspace", need ? workspace : nullptr, (double)need}};
+    const Range read[] = {{"q", q, ((double)(n_tokens - 1) * q_row + row) * esize},
+                          {"cache_k", cache_k, cache},
+                          {"cache_v", cache_v, cache},
+                          {"scale_k", dtype == REVISIT_FP8_KV ? scale_k : nullptr, (double)n_pages * page / 32 * Hk},
+                          {"scale_v", dtype == REVISIT_FP8_KV ? scale_v : nullptr, (double)n_pages * page / 32 * Hk},
+                          {"cu_tokens", cu_tokens, 4.0 * (B + 1.0)},
+                          {"kv_len", kv_len, 4.0 * B},
+                          {"visible", visible, 4.0 * n_tokens},
+                          {"page_table", page_table, 4.0 * B * max_pages},
+                          {"kv_frame_slot", bias ? kv_frame_slot : nullptr, 4.0 * B * max_frames},
+                          {"corr_uv", bias ? corr_uv : nullptr, 8.0 * S * n_tokens},
+                          {"corr_idx", bias ? corr_idx : nullptr, 4.0 * S * n_tokens}};
+    st = check_apart(fn, written, 3, read, 12);
+    if (st != REVISIT_OK) return st;
+    st = check_workspace(fn, need, workspace, workspace_bytes);
+    if (st != REVISIT_OK) return st;
+    a.q = q;
+    a.q_row = q_row;
+    a.cache_k = cache_k;
+    a.cache_v = cache_v;
+    a.scale_k = scale_k;
+    a.scale_v = scale_v;
+    a.o = o;
+    a.lse = lse;
+    a.visible = visible;
+    a.h = h;
+    a.w = w;
+    a.slot = kv_frame_slot;
+    a.max_frames = max_frames;
+    a.corr_uv = corr_uv;
+    a.corr_idx = corr_idx;
+    a.S = bias ? S : 0;
+    a.softmax_scale = softmax_scale;
+    a.partial = static_cast<float*>(workspace);
+    return launched(revisit::launch_paged_attention(a, stream), fn);
+}
+
+}  // extern "C"

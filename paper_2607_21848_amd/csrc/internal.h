@@ -322,6 +322,70 @@ struct CompactFreq {
 double compact_blocks(const CompactArgs& a);
 hipError_t launch_compact(const CompactArgs& a, const CompactFreq& f, hipStream_t stream);
 
+// The streams of a paged cache (paged.h) and their tokens among a call's.
+constexpr int kPagedBf16 = 1, kPagedF32 = 2, kPagedFp8 = 4;  // REVISIT_BF16, REVISIT_F32, REVISIT_FP8_KV
+struct PagedSeqs {
+    const int32_t* cu;          // nullable [B + 1]: stream s has tokens cu[s] .. cu[s + 1] - 1; else `per` each
+    const int32_t* kv_len;      // [B]
+    const int32_t* page_table;  // [B][max_pages]
+    int32_t n_tokens, B, per;
+    int32_t n_pages, max_pages, page_log2;
+};
+
+// New keys and values into the pages (paged_append.hip).
+struct PagedAppendArgs {
+    PagedSeqs seqs;
+    const void* k;
+    const void* v;
+    int64_t k_row_bytes, v_row_bytes;
+    void* cache_k;
+    void* cache_v;
+    uint8_t* scale_k;  // 8-bit pages
+    uint8_t* scale_v;
+    int32_t* out_len;  // nullable [B]
+    int32_t dtype, H, D;
+    const int32_t* pos;     // nullable [n_tokens][3]: time, row, column
+    int32_t t0, hw, w;      // pos NULL: position c of a stream stands at (t0 + c / hw, c / w mod h, c mod w)
+    int32_t n_t, n_y, n_x;  // pairs of each band
+    float inv_pairs;        // 1 / (n_t + n_y + n_x)
+};
+struct PagedFreq {
+    double quarter[64];  // quarter turns per position, of every pair (D <= 128)
+};
+int64_t paged_append_blocks(const PagedAppendArgs& a);
+hipError_t launch_paged_append(const PagedAppendArgs& a, const PagedFreq& f, hipStream_t stream);
+
+// Attention over the pages (paged_attention.hip). paged_plan fills rows, tiles and parts, and returns the
+// workspace's bytes.
+struct PagedAttentionArgs {
+    PagedSeqs seqs;
+    const void* q;
+    int64_t q_row;  // elements between tokens
+    const void* cache_k;
+    const void* cache_v;
+    const uint8_t* scale_k;
+    const uint8_t* scale_v;
+    void* o;
+    float* lse;              // nullable [Hq][n_tokens]
+    const int32_t* visible;  // nullable [n_tokens]
+    int32_t dtype, Hq, Hk, D, G;  // G = Hq / Hk
+    int32_t h, w;
+    const int32_t* slot;  // [B][max_frames]
+    int32_t max_frames;
+    const float* corr_uv;      // [S][n_tokens][2]
+    const int32_t* corr_idx;   // [S][n_tokens]
+    int32_t S;                 // 0 = bias off
+    float softmax_scale, gamma;  // gamma = lambda / (2 sigma^2 softmax_scale)
+    int32_t rows;   // (query, head of a key head's group) rows of a tile
+    int32_t tiles;  // of a key head, over all streams, at most
+    int32_t parts;  // of the keys
+    float* partial;  // parts > 1: [tile][key head][part] results
+};
+constexpr int32_t kPagedMaxParts = 64;
+size_t paged_plan(PagedAttentionArgs& a, int32_t key_parts, int32_t max_keys, int32_t cus);
+double paged_units(const PagedAttentionArgs& a);
+hipError_t launch_paged_attention(const PagedAttentionArgs& a, hipStream_t stream);
+
 // Sets the calling thread's last-error string and returns status (capi.cpp).
 int fail_status(int status, const char* fmt, ...);
 

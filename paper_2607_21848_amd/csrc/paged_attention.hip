@@ -1,0 +1,699 @@
+// Attention over a paged cache (paged_chunk_attention).
+//
+// Per stream and head, O = softmax(scale Q K^T + lambda B) V over the keys that a query sees, with one pass over
+// keys and values: a running maximum and sum, the sums rescaled where the maximum grows. Rows of a tile are
+// (query, head of the group that shares a key head) pairs, so a key is read once for the whole group.
+//
+// Keys and values of 8 bits are widened to bf16 with their scale, which is a power of two: exactly. The 8-bit
+// matrix cores would not give an fp32 sum of products (they drop what lies 13 bits below a group's largest).
+//
+// The wave kernel. Tiles of 16, 32 or 64 rows against 32 keys; a wave works by itself, without a barrier until the
+// end, and loads its operands straight from the pages into registers in the matrix cores' layout: with 16x16
+// MFMAs a lane of S^T = K Q^T supplies 8 head dims of a key, of O^T = V^T P^T one head dim of 8 keys. Both
+// contractions may number their index at will as long as both operands agree, so a lane's head dims are
+// consecutive bytes of the key's row, the 8 keys of a lane are those whose probabilities its own accumulators
+// hold (no exchange between lanes), and the head dim of row m and block db is (D / 16) m + db, so that a lane's value
+// bytes are consecutive too; two keys' bytes are interleaved by byte permutes before they are widened. For few
+// queries it is bound by HBM: a wave has the next tile's keys and values in flight while it works on this one's.
+
+#include <float.h>
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "internal.h"
+#include "paged.h"
+
+namespace revisit {
+namespace {
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kTK = 32;               // keys of a tile: those that share a scale
+constexpr float kRescaleSlack = 8.0f;  // a maximum may grow by 2^8 before the sums are rescaled
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{a, b}, bf16x2));
+}
+__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
+
+// 2^(byte - 127) of a scale: byte 0 counts as 1, 255 is NaN
+__device__ __forceinline__ float scale_value(int byte) { return byte == 255 ? NAN : __uint_as_float((uint32_t)max(byte, 1) << 23); }
+
+// two e4m3 values (the low or high half of x) times a power of two, as bf16: exact
+template <bool kHigh>
+__device__ __forceinline__ uint32_t widen2(uint32_t x, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, kHigh));
+}
+
+// Which values of a word are not finite, by their top bits: e4m3 with all seven bits set, bf16 and fp32 with an exponent
+// of ones. spread: all bits of those values.
+template <int T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t x) {
+    if constexpr (T == kPagedFp8) return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    else if constexpr (T == kPagedBf16) return ((x & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
+    else return ((x & 0x7fffffffu) + 0x00800000u) & 0x80000000u;
+}
+template <int T>
+__device__ __forceinline__ uint32_t spread(uint32_t top) {
+    if constexpr (T == kPagedFp8) return (top >> 7) * 0xffu;
+    else if constexpr (T == kPagedBf16) return (top >> 15) * 0xffffu;
+    else return top ? ~0u : 0u;
+}
+// Element d of a stored row (8 bits: without its scale).
+template <int T>
+__device__ __forceinline__ float stored(const uint8_t* row, int d) {
+    if constexpr (T == kPagedFp8) return __builtin_amdgcn_cvt_f32_fp8(row[d], 0);
+    else if constexpr (T == kPagedBf16) return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(row)[d] << 16);
+    else return reinterpret_cast<const float*>(row)[d];
+}
+
+// Sizes of a tile's loads, by element type and head size.
+template <int D, int T>
+struct Shape {
+    static constexpr int kES = T == kPagedFp8 ? 1 : (T == kPagedBf16 ? 2 : 4);
+    static constexpr int kRowBytes = D * kES;
+    static constexpr int kDb = D / 16;                // blocks of 16 head dims
+    static constexpr int kKLoads = kRowBytes / 64;    // 16-byte loads of a lane per 16 keys
+    static constexpr int kVBytes = kDb * kES;         // of a lane and key
+    static constexpr int kVWords = kVBytes / 4;
+};
+
+template <int N>
+struct Words;
+template <>
+struct Words<1> {
+    typedef uint32_t type;
+};
+template <>
+struct Words<2> {
+    typedef u32x2 type;
+};
+template <>
+struct Words<4> {
+    typedef u32x4 type;
+};
+
+// bias of a query beside the frame at hand
+struct Corr {
+    float ng;  // -gamma, or 0 where the frame is not retrieved or the correspondence not accepted
+    float ux, uy;
+};
+
+struct PagedBias {
+    const int32_t* slot;  // of the stream's frames
+    const float* corr_uv;
+    const int32_t* corr_idx;
+    int max_frames, S, n_tokens;
+    float ng;
+};
+
+constexpr int part_floats(int rows, int D) { return rows * (D + 2); }
+
+template <int D, int T, int NQ, bool kBias>
+__global__ __launch_bounds__(256, NQ > 1 || (T == kPagedF32 && D == 128) ? 1 : (T == kPagedFp8 ? 3 : 2)) void paged_wave_kernel(PagedAttentionArgs a, float c_log2) {
+    using Sh = Shape<D, T>;
+    constexpr int kRows = 16 * NQ;
+    constexpr int kDb = Sh::kDb;
+    constexpr int kW = 4;  // waves
+    constexpr bool kF32 = T == kPagedF32;
+    __shared__ float lds_o[kW / 2][NQ * kDb * 4 * 64];
+    __shared__ float lds_m[kW][kRows], lds_l[kW][kRows];
+    __shared__ floatx4 lds_q[kF32 ? NQ * D / 16 : 1][64];  // fp32 queries: the lane's vector of four steps
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int m = lane & 15, grp = lane >> 4;
+    const PagedSeqs& sq = a.seqs;
+    const int G = a.G;
+
+    // unit = (key head, part, tile), tiles fastest: the tiles that read the same keys run on one XCD
+    const unsigned n_units = (unsigned)a.tiles * (unsigned)a.Hk * (unsigned)a.parts;
+    const unsigned block = row_block();
+    const unsigned unit = xcd_item(block, n_units);
+    if (block >= xcd_grid(n_units) || unit >= n_units) return;  // grid padding (uniform, before any barrier)
+    const int tile = (int)(unit % (unsigned)a.tiles);
+    const int hp = (int)(unit / (unsigned)a.tiles);
+    const int hk = hp / a.parts, part = hp - hk * a.parts;
+    StreamItem it;
+    if (sq.cu) {
+        it = find_item(sq.B, tile, [&](int s) { return (tokens_of(sq, s).y * G + kRows - 1) / kRows; });
+        if (it.s < 0) return;
+    } else {
+        const int each = (sq.per * G + kRows - 1) / kRows;
+        it.s = tile / each;
+        it.in = tile - it.s * each;
+    }
+    const int s = it.s;
+    const int2 tok = tokens_of(sq, s);
+    const int held = held_of(sq, s);
+    const int n_rows = tok.y * G;  // at most 2^30
+
+    // the lane's query rows (column m of block nq), and how many keys each sees
+    int token[NQ], head[NQ], vis[NQ];
+    int seen = 0, seen_min = INT32_MAX;
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+        const int r = it.in * kRows + 16 * nq + m, t = r / G;
+        token[nq] = r < n_rows ? tok.x + t : -1;
+        head[nq] = hk * G + r - t * G;
+        vis[nq] = held;
+        if (token[nq] >= 0 && a.visible) vis[nq] = min(held, max(a.visible[token[nq]], 0));
+        if (token[nq] >= 0) {
+            seen = max(seen, vis[nq]);
+            seen_min = min(seen_min, vis[nq]);
+        }
+    }
+#pragma unroll
+    for (int off = 1; off < 16; off *= 2) {
+        seen = max(seen, __shfl_xor(seen, off));
+        seen_min = min(seen_min, __shfl_xor(seen_min, off));
+    }
+    seen = __builtin_amdgcn_readfirstlane(seen);
+    seen_min = __builtin_amdgcn_readfirstlane(seen_min);
+
+    const int n_tiles = (seen + kTK - 1) / kTK;
+    const int t_begin = (int)((int64_t)part * n_tiles / a.parts), t_end = (int)((int64_t)(part + 1) * n_tiles / a.parts);
+
+    // queries: step (u, v) of a lane takes the head dims that its key vector u holds in elements 8 v .. (fp32: 4 v ..)
+    constexpr int kSteps = kF32 ? 1 : D / 32;
+    bf16x8 qf[kF32 ? 1 : NQ][kSteps];
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+        const int64_t row = (int64_t)max(token[nq], 0) * a.q_row + (int64_t)head[nq] * D;
+        if constexpr (kF32) {
+            for (int u = wave; u < D / 16; u += kW) {
+                floatx4 v = floatx4{0, 0, 0, 0};
+                if (token[nq] >= 0) v = *reinterpret_cast<const floatx4*>(static_cast<const float*>(a.q) + row + 16 * u + 4 * grp);
+                lds_q[nq * (D / 16) + u][lane] = v;
+            }
+        } else {
+#pragma unroll
+            for (int st = 0; st < kSteps; ++st) {
+                const int d = T == kPagedFp8 ? 64 * (st >> 1) + 16 * grp + 8 * (st & 1) : 32 * st + 8 * grp;
+                u32x4 v = u32x4{0, 0, 0, 0};
+                if (token[nq] >= 0) v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) + row + d);
+                qf[nq][st] = as_bf16x8(v);
+            }
+        }
+    }
+    if constexpr (kF32) __syncthreads();
+
+    // a tile's page (-1: none) and the operands of its keys and values
+    auto page_at = [&](int t) -> int { return __builtin_amdgcn_readfirstlane(page_of(sq, s, (t * kTK) >> sq.page_log2)); };
+    using VVec = typename Words<(Sh::kVWords > 4 ? 4 : Sh::kVWords)>::type;
+    constexpr int kVHalves = Sh::kVWords > 4 ? 2 : 1;
+    u32x4 kr[2][Sh::kKLoads];
+    VVec vr[8][kVHalves];
+    float k_scale = 1.0f, v_scale = 1.0f;
+    const int in_page = (1 << sq.page_log2) - 1;
+    auto tile_row = [&](int t, int page) -> size_t { return (((size_t)page * a.Hk + hk) << sq.page_log2) + ((t * kTK) & in_page); };
+    auto load_k = [&](int t, int page) {
+        const size_t row = tile_row(t, page);
+        const uint8_t* base = static_cast<const uint8_t*>(a.cache_k) + row * Sh::kRowBytes;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int u = 0; u < Sh::kKLoads; ++u)
+                kr[b][u] = *reinterpret_cast<const u32x4*>(base + (16 * b + m) * Sh::kRowBytes + 64 * u + 16 * grp);
+        if constexpr (T == kPagedFp8) k_scale = scale_value(a.scale_k[row / kScaleBlock]);
+    };
+    // key of the lane's element j
+    auto key_of = [&](int j) -> int { return 16 * (j >> 2) + 4 * grp + (j & 3); };
+    auto load_v = [&](int t, int page) {
+        const size_t row = tile_row(t, page);
+        const uint8_t* base = static_cast<const uint8_t*>(a.cache_v) + row * Sh::kRowBytes;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int u = 0; u < kVHalves; ++u) {
+                // fp32 at D 128: head dims 64 u + 4 m .., else kDb m ..
+                const int off = kVHalves == 2 ? 256 * u + 16 * m : Sh::kVBytes * m;
+                vr[j][u] = *reinterpret_cast<const VVec*>(base + key_of(j) * Sh::kRowBytes + off);
+            }
+        if constexpr (T == kPagedFp8) v_scale = scale_value(a.scale_v[row / kScaleBlock]);
+    };
+
+    // head dim of row 4 grp + i, block db
+    auto dim = [&](int i, int db) -> int { return kVHalves == 2 ? 64 * (db >> 2) + 4 * (4 * grp + i) + (db & 3) : kDb * (4 * grp + i) + db; };
+    auto value_word = [&](int j, int u, int w) -> uint32_t {
+        if constexpr (Sh::kVWords == 1) return vr[j][0];
+        else return vr[j][u][w];
+    };
+
+    floatx4 O[NQ][kDb];
+    float m_run[NQ], l_run[NQ], m_thr[NQ];
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+#pragma unroll
+        for (int db = 0; db < kDb; ++db) O[nq][db] = floatx4{0, 0, 0, 0};
+        m_run[nq] = -FLT_MAX;
+        m_thr[nq] = -INFINITY;
+        l_run[nq] = 0.0f;
+    }
+
+    const int hw = a.h * a.w;
+    // (p + 1/2) / w truncates to p / w exactly below 2^20 tokens of a frame: its error is under p 2^-22 / w, its
+    // distance from a whole number at least 1 / (2 w)
+    const float inv_w = 1.0f / (float)a.w;
+    auto grid_row = [&](int p) -> int { return kF32 && hw > (1 << 20) ? p / a.w : (int)(((float)p + 0.5f) * inv_w); };
+    Corr corr[NQ];
+    int corr_f = -1;
+    // what a new frame needs waits in LDS: as kernel arguments in scalar registers it made the compiler spill some
+    __shared__ PagedBias lds_b;
+    if constexpr (kBias) {
+        if (threadIdx.x == 0) lds_b = PagedBias{a.slot + (int64_t)s * a.max_frames, a.corr_uv, a.corr_idx, a.max_frames, a.S, sq.n_tokens, -a.gamma};
+        __syncthreads();
+    }
+    auto frame_corr = [&](int f) {
+        corr_f = f;
+        const PagedBias c = lds_b;
+        const int slot = f < c.max_frames ? c.slot[f] : -1;
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            corr[nq] = Corr{0.0f, 0.0f, 0.0f};
+            if (slot >= 0 && slot < c.S && token[nq] >= 0) {
+                const int64_t o = (int64_t)slot * c.n_tokens + token[nq];
+                const float2 u = reinterpret_cast<const float2*>(c.corr_uv)[o];
+                if (c.corr_idx[o] >= 0) corr[nq] = Corr{c.ng, u.x, u.y};
+            }
+        }
+    };
+
+    // next tile of this wave from t on whose page is there
+    int page = -1;
+    auto next_tile = [&](int t) -> int {
+        for (; t < t_end; t += kW) {
+            const int p = page_at(t);
+            if (p >= 0) {
+                page = p;
+                break;
+            }
+        }
+        return t;
+    };
+
+    int t = next_tile(t_begin + wave);
+    if (!kF32 && t < t_end) {
+        load_k(t, page);
+        load_v(t, page);
+    }
+    while (t < t_end) {
+        const int k0 = t * kTK;
+        const bool masked = k0 + kTK > seen_min;  // some query does not see all of the tile's keys
+        const int page_now = page;
+        if constexpr (kF32) load_k(t, page);
+        const int t_next = next_tile(t + kW);
+        const int t_load = t_next < t_end ? t_next : t;  // past the last one it is loaded again and not used
+
+        // S^T = K Q^T, the bias as the accumulators' start
+        floatx4 S[NQ][2];
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) S[nq][b] = floatx4{0, 0, 0, 0};
+        if constexpr (kBias) {
+            const int span = min(kTK, seen - k0);
+            int f = k0 / hw, first = k0 - f * hw;  // frame, and the tile's first key within it
+            for (;;) {
+                if (f != corr_f) frame_corr(f);
+                bool any = false;
+#pragma unroll
+                for (int nq = 0; nq < NQ; ++nq) any = any || corr[nq].ng != 0.0f;
+                if (__any(any)) {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int p = first + 16 * b + 4 * grp + i;
+                            const bool in = p >= 0 && p < hw;
+                            const int ky = grid_row(p);
+                            const float x = (float)(p - ky * a.w) + 0.5f, y = (float)ky + 0.5f;
+#pragma unroll
+                            for (int nq = 0; nq < NQ; ++nq) {
+                                const float dx = x - corr[nq].ux, dy = y - corr[nq].uy;
+                                S[nq][b][i] = in ? corr[nq].ng * (dx * dx + dy * dy) : S[nq][b][i];
+                            }
+                            __builtin_amdgcn_sched_barrier(0);  // one mask at a time
+                        }
+                }
+                if (first + span <= hw) break;  // the frame holds the tile's last key
+                ++f;
+                first -= hw;
+            }
+        }
+        if constexpr (kF32) {
+#pragma unroll
+            for (int u = 0; u < D / 16; ++u)
+#pragma unroll
+                for (int nq = 0; nq < NQ; ++nq) {
+                    const floatx4 qv = lds_q[nq * (D / 16) + u][lane];
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const floatx4 kv = __builtin_bit_cast(floatx4, kr[b][u]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) S[nq][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[i], qv[i], S[nq][b], 0, 0, 0);
+                    }
+                }
+        } else {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int st = 0; st < kSteps; ++st) {
+                    u32x4 w;
+                    if constexpr (T == kPagedFp8) {
+                        const uint32_t x = kr[b][st >> 1][2 * (st & 1)], y = kr[b][st >> 1][2 * (st & 1) + 1];
+                        w = u32x4{widen2<false>(x, k_scale), widen2<true>(x, k_scale), widen2<false>(y, k_scale), widen2<true>(y, k_scale)};
+                    } else {
+                        w = kr[b][st];
+                    }
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq)
+                        S[nq][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), qf[nq][st], S[nq][b], 0, 0, 0);
+                }
+        }
+        if constexpr (kF32) load_v(t, page_now);
+        else load_k(t_load, page);
+
+        // softmax: the lane's eight logits of each of its columns
+        u32x4 pf[NQ];
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (masked && k0 + key_of(j) >= vis[nq]) S[nq][j >> 2][j & 3] = -INFINITY;
+                mx = fmaxf(mx, S[nq][j >> 2][j & 3]);
+            }
+            if (__any(mx > m_thr[nq])) {
+                mx = fmaxf(mx, __shfl_xor(mx, 16));
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                const float m_new = fmaxf(m_run[nq], mx * c_log2);
+                const float alpha = __builtin_amdgcn_exp2f(m_run[nq] - m_new);
+                l_run[nq] *= alpha;
+#pragma unroll
+                for (int db = 0; db < kDb; ++db) O[nq][db] *= alpha;
+                m_run[nq] = m_new;
+                m_thr[nq] = (m_new + kRescaleSlack) / c_log2;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(S[nq][j >> 2][j & 3], c_log2, -m_run[nq]));
+                S[nq][j >> 2][j & 3] = p;
+                l_run[nq] += p;
+            }
+            if constexpr (!kF32)
+                pf[nq] = u32x4{pack_bf16(S[nq][0][0], S[nq][0][1]), pack_bf16(S[nq][0][2], S[nq][0][3]),
+                               pack_bf16(S[nq][1][0], S[nq][1][1]), pack_bf16(S[nq][1][2], S[nq][1][3])};
+        }
+
+        // values behind the stream's last key may be anything: none of them
+        if (k0 + kTK > held) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int u = 0; u < kVHalves; ++u)
+                    if (k0 + key_of(j) >= held) vr[j][u] = VVec{};
+        }
+        // A query's weight of a key that it does not see is 0, and 0 times a value that is not finite would be NaN. Where
+        // a masked tile holds such values, they are taken out of the operands, and the queries that see their
+        // keys get them one by one.
+        if (masked) {
+            uint32_t bad = v_scale != v_scale ? ~0u : 0u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int u = 0; u < kVHalves; ++u)
+#pragma unroll
+                    for (int w = 0; w < Sh::kVWords / kVHalves; ++w) bad |= not_finite<T>(value_word(j, u, w));
+            if (__builtin_expect(__any(bad != 0), 0)) {
+                const size_t row = tile_row(t, page_now);
+                const uint8_t* base = static_cast<const uint8_t*>(a.cache_v) + row * Sh::kRowBytes;
+#pragma unroll 1
+                for (int key = 0; key < min(kTK, held - k0); ++key) {
+                    const int j = 4 * (key >> 4) + (key & 3), from = 16 * ((key >> 2) & 3) + m;
+                    float p[NQ];
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq) {
+                        p[nq] = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) p[nq] = i == j ? S[nq][i >> 2][i & 3] : p[nq];
+                        p[nq] = __shfl(p[nq], from);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int db = 0; db < kDb; ++db) {
+                            const float x = stored<T>(base + key * Sh::kRowBytes, dim(i, db)) * v_scale;
+#pragma unroll
+                            for (int nq = 0; nq < NQ; ++nq)
+                                if (!(fabsf(x) < INFINITY) && k0 + key < vis[nq]) O[nq][db][i] += p[nq] * x;
+                            __builtin_amdgcn_sched_barrier(0);  // one mask at a time
+                        }
+                }
+                const uint32_t none = v_scale != v_scale ? 0u : ~0u;
+                v_scale = none ? v_scale : 1.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int u = 0; u < kVHalves; ++u) {
+                        if constexpr (Sh::kVWords == 1) {
+                            vr[j][0] &= none & ~spread<T>(not_finite<T>(vr[j][0]));
+                        } else {
+#pragma unroll
+                            for (int w = 0; w < Sh::kVWords / kVHalves; ++w) vr[j][u][w] &= none & ~spread<T>(not_finite<T>(vr[j][u][w]));
+                        }
+                    }
+            }
+        }
+        // O^T += V^T P^T
+        if constexpr (kF32) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                    for (int db = 0; db < kDb; ++db)
+                        O[nq][db] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(value_word(j, db / 4, db % 4)), S[nq][j >> 2][j & 3], O[nq][db], 0, 0, 0);
+        } else {
+            constexpr int kPer = 4 / Sh::kES;  // blocks of head dims that a word of the lane's value bytes holds
+#pragma unroll
+            for (int w = 0; w < Sh::kVWords; ++w) {
+                u32x4 vf[kPer];  // their operands, keys in pairs
+#pragma unroll
+                for (int jp = 0; jp < 4; ++jp) {
+                    const uint32_t x = value_word(2 * jp, 0, w), y = value_word(2 * jp + 1, 0, w);
+                    if constexpr (T == kPagedFp8) {
+                        // bytes of the two keys side by side: (x0 y0 x1 y1), (x2 y2 x3 y3)
+                        const uint32_t lo = __builtin_amdgcn_perm(y, x, 0x05010400), hi = __builtin_amdgcn_perm(y, x, 0x07030602);
+                        vf[0][jp] = widen2<false>(lo, v_scale);
+                        vf[1][jp] = widen2<true>(lo, v_scale);
+                        vf[2][jp] = widen2<false>(hi, v_scale);
+                        vf[3][jp] = widen2<true>(hi, v_scale);
+                    } else {
+                        vf[0][jp] = __builtin_amdgcn_perm(y, x, 0x05040100);
+                        vf[1][jp] = __builtin_amdgcn_perm(y, x, 0x07060302);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq)
+                        O[nq][kPer * w + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[i]), as_bf16x8(pf[nq]), O[nq][kPer * w + i], 0, 0, 0);
+            }
+        }
+        if constexpr (!kF32) load_v(t_load, page);
+        t = t_next;
+    }
+
+    // the waves' sums at the columns' common maximum; the upper half of the remaining waves hands its sums to the lower half
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+        l_run[nq] += __shfl_xor(l_run[nq], 16);
+        l_run[nq] += __shfl_xor(l_run[nq], 32);
+        if (grp == 0) {
+            lds_m[wave][16 * nq + m] = m_run[nq];
+            lds_l[wave][16 * nq + m] = l_run[nq];
+        }
+    }
+    __syncthreads();
+    float M[NQ], L[NQ];
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+        M[nq] = -FLT_MAX;
+        L[nq] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kW; ++w) M[nq] = fmaxf(M[nq], lds_m[w][16 * nq + m]);
+#pragma unroll
+        for (int w = 0; w < kW; ++w) L[nq] += lds_l[w][16 * nq + m] * __builtin_amdgcn_exp2f(lds_m[w][16 * nq + m] - M[nq]);
+        const float mine = __builtin_amdgcn_exp2f(m_run[nq] - M[nq]);
+#pragma unroll
+        for (int db = 0; db < kDb; ++db) O[nq][db] *= mine;
+    }
+#pragma unroll
+    for (int half = kW / 2; half >= 1; half /= 2) {
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                for (int db = 0; db < kDb; ++db)
+                    *reinterpret_cast<floatx4*>(&lds_o[wave - half][((nq * kDb + db) * 64 + lane) * 4]) = O[nq][db];
+        }
+        __syncthreads();
+        if (wave < half) {
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                for (int db = 0; db < kDb; ++db)
+                    O[nq][db] += *reinterpret_cast<const floatx4*>(&lds_o[wave][((nq * kDb + db) * 64 + lane) * 4]);
+        }
+        __syncthreads();
+    }
+    if (wave != 0) return;
+
+    if (a.parts > 1) {
+        float* base = a.partial + ((size_t)((size_t)tile * a.Hk + hk) * a.parts + part) * part_floats(kRows, D);
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            if (grp == 0) {
+                base[kRows * D + 16 * nq + m] = t_begin < t_end ? M[nq] : -INFINITY;
+                base[kRows * D + kRows + 16 * nq + m] = L[nq];
+            }
+            if (t_begin < t_end && token[nq] >= 0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int b4 = 0; b4 < kDb / 4; ++b4)
+                        *reinterpret_cast<floatx4*>(base + (16 * nq + m) * D + dim(i, 4 * b4)) =
+                            floatx4{O[nq][4 * b4][i], O[nq][4 * b4 + 1][i], O[nq][4 * b4 + 2][i], O[nq][4 * b4 + 3][i]};
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+        if (token[nq] < 0) continue;
+        // a query that sees no key: nothing, and an LSE of -inf
+        const float inv = L[nq] == 0.0f ? 0.0f : 1.0f / L[nq];
+        const size_t row = ((size_t)token[nq] * a.Hq + head[nq]) * D;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int b4 = 0; b4 < kDb / 4; ++b4) {
+                const floatx4 x = floatx4{O[nq][4 * b4][i], O[nq][4 * b4 + 1][i], O[nq][4 * b4 + 2][i], O[nq][4 * b4 + 3][i]} * inv;
+                if constexpr (kF32) *reinterpret_cast<floatx4*>(static_cast<float*>(a.o) + row + dim(i, 4 * b4)) = x;
+                else
+                    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.o) + row + dim(i, 4 * b4)) =
+                        u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+            }
+        if (a.lse && grp == 0) a.lse[(size_t)head[nq] * sq.n_tokens + token[nq]] = (M[nq] + log2f(L[nq])) * kLn2;
+    }
+}
+
+// O = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p over the key parts of a tile: thread t of a row's D / 4 takes head
+// dims 4 t ..; a part without keys has m = -inf and is not read.
+template <int D, bool kF32>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttentionArgs a, unsigned blocks) {
+    constexpr int kLanes = D / 4, kRowsPer = 256 / kLanes;
+    const unsigned block = row_block();
+    if (block >= blocks) return;
+    const unsigned per = (unsigned)(a.rows / kRowsPer);
+    const unsigned item = block / per;  // (tile, key head)
+    const int r = (int)(block - item * per) * kRowsPer + (int)threadIdx.x / kLanes;
+    const int d = 4 * ((int)threadIdx.x % kLanes);
+    const int tile = (int)(item / (unsigned)a.Hk), hk = (int)(item - (unsigned)tile * (unsigned)a.Hk);
+    const PagedSeqs& sq = a.seqs;
+    StreamItem it;
+    if (sq.cu) {
+        it = find_item(sq.B, tile, [&](int s) { return (tokens_of(sq, s).y * a.G + a.rows - 1) / a.rows; });
+        if (it.s < 0) return;
+    } else {
+        const int each = (sq.per * a.G + a.rows - 1) / a.rows;
+        it.s = tile / each;
+        it.in = tile - it.s * each;
+    }
+    const int2 tok = tokens_of(sq, it.s);
+    const int row = it.in * a.rows + r;
+    if (row >= tok.y * a.G) return;
+    const int token = tok.x + row / a.G, head = hk * a.G + row % a.G;
+    const float* base = a.partial + (size_t)item * a.parts * part_floats(a.rows, D);
+    const size_t step = part_floats(a.rows, D);
+    float M = -INFINITY;
+    for (int p = 0; p < a.parts; ++p) M = fmaxf(M, base[p * step + a.rows * D + r]);
+    float L = 0.0f;
+    floatx4 x = floatx4{0, 0, 0, 0};
+    for (int p = 0; p < a.parts; ++p) {
+        const float mp = base[p * step + a.rows * D + r];
+        if (mp == -INFINITY) continue;
+        const float c = __builtin_amdgcn_exp2f(mp - M);
+        L = fmaf(c, base[p * step + a.rows * D + a.rows + r], L);
+        x += c * *reinterpret_cast<const floatx4*>(base + p * step + r * D + d);
+    }
+    x *= L == 0.0f ? 0.0f : 1.0f / L;
+    const size_t out = ((size_t)token * a.Hq + head) * D + d;
+    if constexpr (kF32) *reinterpret_cast<floatx4*>(static_cast<float*>(a.o) + out) = x;
+    else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.o) + out) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+    if (a.lse && d == 0) a.lse[(size_t)head * sq.n_tokens + token] = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
+}
+
+}  // namespace
+
+size_t paged_plan(PagedAttentionArgs& a, int32_t key_parts, int32_t max_keys, int32_t cus) {
+    const PagedSeqs& q = a.seqs;
+    const int64_t streams = q.B < q.n_tokens ? q.B : q.n_tokens;
+    const int64_t rows = streams ? (int64_t)q.n_tokens * a.G / streams : 0;  // of a stream and key head, on average
+    a.rows = rows <= 16 ? 16 : (rows <= 32 || a.dtype != kPagedFp8 ? 32 : 64);
+    const int64_t tiles = q.cu ? (int64_t)q.n_tokens * a.G / a.rows + streams : q.B * (((int64_t)q.per * a.G + a.rows - 1) / a.rows);
+    a.tiles = (int32_t)std::min<int64_t>(tiles, INT32_MAX);
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(max_keys, (int64_t)q.max_pages << q.page_log2));
+    const int64_t key_tiles = (most + kTK - 1) / kTK;
+    int64_t parts = key_parts;
+    if (parts == 0) {
+        const int64_t units = std::max<int64_t>(1, tiles * a.Hk);
+        parts = std::min<int64_t>((4 * (int64_t)cus + units - 1) / units, key_tiles / 16);
+    }
+    a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(parts, kPagedMaxParts), key_tiles));
+    return a.parts > 1 ? (size_t)tiles * a.Hk * a.parts * part_floats(a.rows, a.D) * sizeof(float) : 0;
+}
+
+double paged_units(const PagedAttentionArgs& a) { return (double)a.tiles * a.Hk * a.parts; }
+
+hipError_t launch_paged_attention(const PagedAttentionArgs& a, hipStream_t stream) {
+    if (a.seqs.n_tokens == 0 || a.tiles == 0) return hipSuccess;
+    const float c = a.softmax_scale * kLog2e;
+    const dim3 grid = grid_rows(xcd_grid((unsigned)a.tiles * (unsigned)a.Hk * (unsigned)a.parts));
+    auto wave = [&](auto d_tag, auto t_tag) {
+        constexpr int D = decltype(d_tag)::value, T = decltype(t_tag)::value;
+        auto rows = [&](auto bias_tag) {
+            constexpr bool B = decltype(bias_tag)::value;
+            if (a.rows == 16) hipLaunchKernelGGL((paged_wave_kernel<D, T, 1, B>), grid, dim3(256), 0, stream, a, c);
+            else if (a.rows == 32 || T != kPagedFp8) hipLaunchKernelGGL((paged_wave_kernel<D, T, 2, B>), grid, dim3(256), 0, stream, a, c);
+            else hipLaunchKernelGGL((paged_wave_kernel<D, T, T == kPagedFp8 ? 4 : 2, B>), grid, dim3(256), 0, stream, a, c);
+        };
+        if (a.S > 0) rows(std::true_type{});
+        else rows(std::false_type{});
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || a.parts == 1) return e;
+        const unsigned blocks = (unsigned)a.tiles * (unsigned)a.Hk * (unsigned)(a.rows / (1024 / D));
+        hipLaunchKernelGGL((paged_merge_kernel<D, T == kPagedF32>), grid_rows(blocks), dim3(256), 0, stream, a, blocks);
+        return hipGetLastError();
+    };
+    auto by_type = [&](auto d_tag) {
+        if (a.dtype == kPagedFp8) return wave(d_tag, std::integral_constant<int, kPagedFp8>{});
+        if (a.dtype == kPagedBf16) return wave(d_tag, std::integral_constant<int, kPagedBf16>{});
+        return wave(d_tag, std::integral_constant<int, kPagedF32>{});
+    };
+    return a.D == 128 ? by_type(std::integral_constant<int, 128>{}) : by_type(std::integral_constant<int, 64>{});
+}
+
+}  // namespace revisit
