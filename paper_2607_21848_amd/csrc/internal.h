@@ -379,6 +379,7 @@ struct PagedAttentionArgs {
     int32_t rows;   // (query, head of a key head's group) rows of a tile
     int32_t tiles;  // of a key head, over all streams, at most
     int32_t parts;  // of the keys
+    int32_t many;   // workgroups of many waves
     float* partial;  // parts > 1: [tile][key head][part] results
 };
 constexpr int32_t kPagedMaxParts = 64;
