@@ -1192,6 +1192,7 @@ int paged_chunk_attention(const void* q, int64_t q_row, const void* cache_k, con
     a.corr_idx = corr_idx;
     a.S = bias ? S : 0;
     a.softmax_scale = softmax_scale;
+    if (n_pages == 0) a.seqs.max_pages = 0;  // nobody has a key; the kernels take page 0 to be there
     a.partial = static_cast<float*>(workspace);
     return launched(revisit::launch_paged_attention(a, stream), fn);
 }

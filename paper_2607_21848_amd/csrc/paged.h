@@ -62,4 +62,58 @@ __device__ __forceinline__ StreamItem find_item(int B, int unit, Count count) {
     return StreamItem{-1, 0};
 }
 
+// Stream and tile of `rows` (query, head of the group) rows that number `tile` of a key head's tiles stands for. A stream's
+// tiles come in falling order: the last queries of a causal prompt have the most keys, and start first.
+__device__ __forceinline__ StreamItem row_tile(const PagedAttentionArgs& a, int rows, int tile) {
+    const PagedSeqs& q = a.seqs;
+    auto count = [&](int s) { return (tokens_of(q, s).y * a.G + rows - 1) / rows; };
+    StreamItem it;
+    if (q.cu) {
+        it = find_item(q.B, tile, count);
+        if (it.s < 0) return it;
+    } else {
+        const int each = (q.per * a.G + rows - 1) / rows;
+        it.s = tile / each;
+        it.in = tile - it.s * each;
+    }
+    it.in = count(it.s) - 1 - it.in;
+    return it;
+}
+
+// floats of a part's result of a tile: O [rows][D], maxima [rows], sums [rows]
+__host__ __device__ constexpr int paged_part_floats(int rows, int D) { return rows * (D + 2); }
+
+typedef __attribute__((address_space(4))) int32_t const_i32;  // memory that does not change while the kernel runs
+
+// 2^(byte - 127) of a scale: byte 0 counts as 1, 255 is NaN
+__device__ __forceinline__ float scale_value(int byte) { return byte == 255 ? NAN : __uint_as_float((uint32_t)max(byte, 1) << 23); }
+
+// two e4m3 values (the low or high half of x) times a power of two, as bf16: exact
+template <bool kHigh>
+__device__ __forceinline__ uint32_t widen2(uint32_t x, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, kHigh));
+}
+
+// Which values of a word are not finite, by their top bits: e4m3 with all seven bits set, bf16 and fp32 with an exponent
+// of ones. spread: all bits of those values.
+template <int T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t x) {
+    if constexpr (T == kPagedFp8) return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    else if constexpr (T == kPagedBf16) return ((x & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
+    else return ((x & 0x7fffffffu) + 0x00800000u) & 0x80000000u;
+}
+template <int T>
+__device__ __forceinline__ uint32_t spread(uint32_t top) {
+    if constexpr (T == kPagedFp8) return (top >> 7) * 0xffu;
+    else if constexpr (T == kPagedBf16) return (top >> 15) * 0xffffu;
+    else return top ? ~0u : 0u;
+}
+// Element d of a stored row (8 bits: without its scale).
+template <int T>
+__device__ __forceinline__ float stored(const uint8_t* row, int d) {
+    if constexpr (T == kPagedFp8) return __builtin_amdgcn_cvt_f32_fp8(row[d], 0);
+    else if constexpr (T == kPagedBf16) return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(row)[d] << 16);
+    else return reinterpret_cast<const float*>(row)[d];
+}
+
 }  // namespace revisit

@@ -47,37 +47,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 }
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 
-// 2^(byte - 127) of a scale: byte 0 counts as 1, 255 is NaN
-__device__ __forceinline__ float scale_value(int byte) { return byte == 255 ? NAN : __uint_as_float((uint32_t)max(byte, 1) << 23); }
-
-// two e4m3 values (the low or high half of x) times a power of two, as bf16: exact
-template <bool kHigh>
-__device__ __forceinline__ uint32_t widen2(uint32_t x, float scale) {
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, kHigh));
-}
-
-// Which values of a word are not finite, by their top bits: e4m3 with all seven bits set, bf16 and fp32 with an exponent
-// of ones. spread: all bits of those values.
-template <int T>
-__device__ __forceinline__ uint32_t not_finite(uint32_t x) {
-    if constexpr (T == kPagedFp8) return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-    else if constexpr (T == kPagedBf16) return ((x & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
-    else return ((x & 0x7fffffffu) + 0x00800000u) & 0x80000000u;
-}
-template <int T>
-__device__ __forceinline__ uint32_t spread(uint32_t top) {
-    if constexpr (T == kPagedFp8) return (top >> 7) * 0xffu;
-    else if constexpr (T == kPagedBf16) return (top >> 15) * 0xffffu;
-    else return top ? ~0u : 0u;
-}
-// Element d of a stored row (8 bits: without its scale).
-template <int T>
-__device__ __forceinline__ float stored(const uint8_t* row, int d) {
-    if constexpr (T == kPagedFp8) return __builtin_amdgcn_cvt_f32_fp8(row[d], 0);
-    else if constexpr (T == kPagedBf16) return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(row)[d] << 16);
-    else return reinterpret_cast<const float*>(row)[d];
-}
-
 // Sizes of a tile's loads, by element type and head size.
 template <int D, int T>
 struct Shape {
@@ -104,8 +73,6 @@ struct Words<4> {
     typedef u32x4 type;
 };
 
-typedef __attribute__((address_space(4))) int32_t const_i32;  // memory that does not change while the kernel runs
-
 // bias of a query beside the frame at hand
 struct Corr {
     float ng;  // -gamma, or 0 where the frame is not retrieved or the correspondence not accepted
@@ -119,8 +86,6 @@ struct PagedBias {
     int max_frames, S, n_tokens;
     float ng;
 };
-
-constexpr int part_floats(int rows, int D) { return rows * (D + 2); }
 
 constexpr int kManyWaves = 8;  // of a workgroup where there are few
 
@@ -152,15 +117,8 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (NQ == 1 && (T != kPagedF32 || D
     const int tile = (int)(unit % (unsigned)a.tiles);
     const int hp = (int)(unit / (unsigned)a.tiles);
     const int hk = hp / a.parts, part = hp - hk * a.parts;
-    StreamItem it;
-    if (sq.cu) {
-        it = find_item(sq.B, tile, [&](int s) { return (tokens_of(sq, s).y * G + kRows - 1) / kRows; });
-        if (it.s < 0) return;
-    } else {
-        const int each = (sq.per * G + kRows - 1) / kRows;
-        it.s = tile / each;
-        it.in = tile - it.s * each;
-    }
+    const StreamItem it = row_tile(a, kRows, tile);
+    if (it.s < 0) return;
     const int s = it.s;
     const int2 tok = tokens_of(sq, s);
     const int n_rows = tok.y * G;  // at most 2^30
@@ -607,7 +565,7 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (NQ == 1 && (T != kPagedF32 || D
         // its head dims: blocks 4 b .. 4 b + 3 from first[b] on
         auto first = [&](int b) -> int { return kVHalves == 2 ? 64 * b + 4 * (4 * (l >> 4) + i) : kDb * (4 * (l >> 4) + i) + 4 * b; };
         if (a.parts > 1) {
-            float* base = a.partial + ((size_t)((size_t)tile * a.Hk + hk) * a.parts + part) * part_floats(kRows, D);
+            float* base = a.partial + ((size_t)((size_t)tile * a.Hk + hk) * a.parts + part) * paged_part_floats(kRows, D);
             if (l < 16 && i == 0) {
                 base[kRows * D + col] = t_begin < t_end ? M : -INFINITY;
                 base[kRows * D + kRows + col] = L;
@@ -649,21 +607,14 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttentionArgs a, 
     const int g = (int)threadIdx.x % kThreads / kLanes, d = 4 * ((int)threadIdx.x % kLanes);
     const int tile = (int)(item / (unsigned)a.Hk), hk = (int)(item - (unsigned)tile * (unsigned)a.Hk);
     const PagedSeqs& sq = a.seqs;
-    StreamItem it;
-    if (sq.cu) {
-        it = find_item(sq.B, tile, [&](int s) { return (tokens_of(sq, s).y * a.G + a.rows - 1) / a.rows; });
-        if (it.s < 0) return;
-    } else {
-        const int each = (sq.per * a.G + a.rows - 1) / a.rows;
-        it.s = tile / each;
-        it.in = tile - it.s * each;
-    }
+    const StreamItem it = row_tile(a, a.rows, tile);
+    if (it.s < 0) return;
     const int2 tok = tokens_of(sq, it.s);
     const int row = it.in * a.rows + r;
     const bool ok = row < tok.y * a.G;
     if (kRowsPer == 1 && !ok) return;  // uniform
     const int token = tok.x + row / a.G, head = hk * a.G + row % a.G;
-    const size_t step = part_floats(a.rows, D);
+    const size_t step = paged_part_floats(a.rows, D);
     const float* base = a.partial + (size_t)item * a.parts * step + r * D + d;
     const float* stat = a.partial + (size_t)item * a.parts * step + a.rows * D + r;
     float M = -INFINITY, L = 0.0f;
@@ -707,7 +658,7 @@ size_t paged_plan(PagedAttentionArgs& a, int32_t key_parts, int32_t max_keys, in
     const PagedSeqs& q = a.seqs;
     const int64_t streams = q.B < q.n_tokens ? q.B : q.n_tokens;
     const int64_t rows = streams ? (int64_t)q.n_tokens * a.G / streams : 0;  // of a stream and key head, on average
-    a.rows = rows <= 16 ? 16 : 32;
+    a.rows = rows <= 16 ? 16 : (rows > 64 && a.dtype != kPagedF32 ? kPagedTileRows : 32);  // the tile kernel has no fp32 form
     const int64_t tiles = q.cu ? (int64_t)q.n_tokens * a.G / a.rows + streams : q.B * (((int64_t)q.per * a.G + a.rows - 1) / a.rows);
     a.tiles = (int32_t)std::min<int64_t>(tiles, INT32_MAX);
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(max_keys, (int64_t)q.max_pages << q.page_log2));
@@ -716,11 +667,18 @@ size_t paged_plan(PagedAttentionArgs& a, int32_t key_parts, int32_t max_keys, in
     // workgroups of many waves where there are fewer units than compute units
     a.many = a.rows == 16 && units < cus;
     int64_t parts = key_parts;
-    if (parts == 0) {
+    if (parts == 0 && a.rows == kPagedTileRows) {
+        AttentionArgs like{};  // its split is that of as many items of biased_chunk_attention
+        like.Lq = (int32_t)std::min<int64_t>(128 * tiles, INT32_MAX);
+        like.Lk = (int32_t)most;
+        like.H = a.Hk;
+        like.layers = 1;
+        parts = attention_bf16_key_parts(like, cus);
+    } else if (parts == 0) {
         parts = a.many ? std::min<int64_t>(cus / units, key_tiles / 4) : std::min<int64_t>((2 * (int64_t)cus + units - 1) / units, key_tiles / 16);
     }
     a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(parts, kPagedMaxParts), key_tiles));
-    return a.parts > 1 ? (size_t)tiles * a.Hk * a.parts * part_floats(a.rows, a.D) * sizeof(float) : 0;
+    return a.parts > 1 ? (size_t)tiles * a.Hk * a.parts * paged_part_floats(a.rows, a.D) * sizeof(float) : 0;
 }
 
 double paged_units(const PagedAttentionArgs& a) { return (double)a.tiles * a.Hk * a.parts; }
@@ -742,9 +700,14 @@ hipError_t launch_paged_attention(const PagedAttentionArgs& a, hipStream_t strea
             else if (a.rows == 16) launch(std::integral_constant<int, 1>{}, bias_tag, W4{});
             else launch(std::integral_constant<int, 2>{}, bias_tag, W4{});
         };
-        if (a.S > 0) rows(std::true_type{});
-        else rows(std::false_type{});
-        const hipError_t e = hipGetLastError();
+        hipError_t e;
+        if (a.rows == kPagedTileRows) {
+            e = launch_paged_tiles(a, stream);
+        } else {
+            if (a.S > 0) rows(std::true_type{});
+            else rows(std::false_type{});
+            e = hipGetLastError();
+        }
         if (e != hipSuccess || a.parts == 1) return e;
         // a workgroup per row where there are many parts to read
         auto merge = [&](auto per_tag) {

@@ -69,13 +69,14 @@ class Pool:
         return out[0], out[1], have
 
 
-def check_attention(pool, q, o, lse, cu=None, visible=None, scale=None, bias=None):
+def check_attention(pool, q, o, lse, cu=None, visible=None, scale=None, bias=None, slack=0.0):
     """o and lse against the oracle on every stream, within what the roundings allow.
 
     A logit is a sum of D products in fp32 (off by D + 6 units of 2^-24 of the sum of their magnitudes, the scale and the
     exponent's FMA included, and 2^-22 of a bias beside it); a probability is off by that, 2^-22 of the
     exponential and, for bf16 values, half a step of bf16 (2^-8) in the product with the values alone; sums of L / 16
-    probabilities a lane and of L products by 2^-24 each; the output by half a step of its type. An empty row is exact."""
+    probabilities a lane and of L products by 2^-24 each; the output by half a step of its type. An empty row is exact.
+    `slack`: what a bias in separable form may add to a logit's error (8 units of its largest term)."""
     n, Hq, D = q.shape
     scale = scale or D ** -0.5
     q64 = q.float().double().cpu().numpy()
@@ -96,7 +97,7 @@ def check_attention(pool, q, o, lse, cu=None, visible=None, scale=None, bias=Non
         kk, vv = np.where(np.isfinite(k), np.abs(k), 0), np.where(np.isfinite(v), np.abs(v), 0)
         for h in range(Hq):
             mag = np.abs(q64[t0:t0 + m, h]) @ kk[h // (Hq // pool.H)].T * scale if L else np.zeros((m, 0))
-            d = np.where(on, (D + 6) * 2.0 ** -24 * mag + (0 if b is None else np.abs(b) * 2.0 ** -22), 0).max(1, initial=0) + 2.0 ** -22
+            d = np.where(on, (D + 6) * 2.0 ** -24 * mag + (0 if b is None else np.abs(b) * 2.0 ** -22), 0).max(1, initial=0) + 2.0 ** -22 + slack
             rows = on.any(1)
             tol_l = d + (L / 16 + 16) * 2.0 ** -24 + 4 * 2.0 ** -24 * np.abs(np.where(rows, wl[h], 0))
             got_l = l64[h, t0:t0 + m]

@@ -34,6 +34,7 @@ def _causal(lens, cu):
 @pytest.mark.parametrize("page,Hq,Hk,lens,new", [
     (32, 1, 1, [1], [1]), (64, 4, 4, [33], [1]), (32, 8, 2, [100, 7, 64], [1, 1, 1]), (128, 5, 1, [300], [3]), (64, 6, 3, [129, 65], [9, 2]),
     (32, 2, 2, [200], [40]), (256, 3, 1, [700], [21]), (32, 4, 2, [97, 0, 260, 31], [33, 2, 0, 70]), (64, 2, 1, [500], [150]),
+    (32, 2, 2, [33, 129], [129, 128]), (64, 6, 2, [300, 0, 64, 1], [200, 70, 30, 1]), (32, 1, 1, [31], [70]), (128, 3, 3, [160], [127]),
 ])
 @pytest.mark.parametrize("causal", [False, True])
 def test_shapes(dtype, D, page, Hq, Hk, lens, new, causal):
@@ -50,8 +51,9 @@ def test_shapes(dtype, D, page, Hq, Hk, lens, new, causal):
 
 @pytest.mark.parametrize("dtype", [FP8, BF16, F32])
 @pytest.mark.parametrize("parts", [1, 2, 3, 7, 64])
-def test_key_parts(dtype, parts):
-    lens, new = [1000, 45, 0, 333], [3, 1, 2, 20]
+@pytest.mark.parametrize("new", [[3, 1, 2, 20], [60, 0, 40, 150]])
+def test_key_parts(dtype, parts, new):
+    lens = [1000, 45, 0, 333]
     pool = Pool(3, dtype, lens, 2, 128, 64)
     cu = np.concatenate([[0], np.cumsum(new)])
     q = values(gen(4), GIVEN[dtype], int(cu[-1]), 4, 128)
@@ -104,19 +106,35 @@ def test_what_is_not_seen_may_be_anything(dtype, m):
 
 
 @pytest.mark.parametrize("dtype", [FP8, BF16, F32])
-def test_pages_that_are_none(dtype):
+@pytest.mark.parametrize("m", [3, 50])
+def test_pages_that_are_none(dtype, m):
     lens = [400, 90, 64]
     pool = Pool(7, dtype, lens, 2, 64, 32)
     pool.table[0, [0, 5, 6, 12]] = (-1, pool.n_pages, 2**31 - 1, -7)
     pool.table[1, :] = -1  # a stream without any page
-    q = values(gen(8), GIVEN[dtype], 9, 4, 64)
+    q = values(gen(8), GIVEN[dtype], 3 * m, 4, 64)
+    # what lies in the pool's pages must not show through entries that are none
+    pool.k[0], pool.v[0] = (torch.full_like(x[0].float(), NAN).to(dtype) for x in (pool.k, pool.v))
+    pool.table[pool.table == 0] = -1
     o, lse = _attend(pool, q)
     check_attention(pool, q, o, lse)
-    assert bool((o[3:6] == 0).all()) and bool((lse[:, 3:6] == -INF).all())
+    assert bool((o[m:2 * m] == 0).all()) and bool((lse[:, m:2 * m] == -INF).all())
     # two entries of one page
     pool.table[2, :] = pool.table[2, 0]
     o, lse = _attend(pool, q)
     check_attention(pool, q, o, lse)
+
+
+@pytest.mark.parametrize("dtype", [FP8, BF16, F32])
+def test_no_pages_at_all(dtype):
+    k = torch.empty(0, 2, 32, 64, dtype=dtype, device=DEV)
+    sc = dict(scale_k=torch.empty(0, 2, 1, dtype=torch.float8_e8m0fnu, device=DEV), scale_v=torch.empty(0, 2, 1, dtype=torch.float8_e8m0fnu, device=DEV))
+    for m in (1, 100):
+        for entries in (0, 3):
+            table = torch.zeros(2, entries, dtype=torch.int32, device=DEV)
+            o, lse = rv.paged_chunk_attention(values(gen(1), GIVEN[dtype], 2 * m, 4, 64), k, k, table, _i32([40, 96]), softmax_scale=0.1,
+                                              **(sc if dtype == FP8 else {}))
+            assert bool((o == 0).all()) and bool((lse == -INF).all())
 
 
 def _bias(pool, n, cu, S, h, w, slots, seed, sigma, lam):
@@ -151,9 +169,12 @@ def test_bias(dtype, h, w, Hq, Hk, D, lens, new, frames, seed):
     slots = rng.integers(-2, S + 2, (len(lens), frames)).astype(np.int32)  # beyond S: unbiased
     uv, idx, bias = _bias(pool, n, cu, S, h, w, slots, 11, 2.0, 1.3)
     q = values(gen(12), GIVEN[dtype], n, Hq, D)
+    off_centre = np.nan_to_num(uv.cpu().numpy().astype(np.float64) - (w / 2, h / 2))
+    largest = 1.3 * ((h * h + w * w) / 4 + (off_centre ** 2).sum(-1).max()) / (2 * 2.0 ** 2)
+    slack = 0.0 if dtype == F32 else 8 * 2.0 ** -24 * largest
     for visible in (None, _causal(lens, cu)):
         o, lse = _attend(pool, q, cu, visible, kv_frame_slot=_i32(slots), corr_uv=uv, corr_idx=idx, h=h, w=w, lam=1.3, sigma=2.0)
-        check_attention(pool, q, o, lse, cu, visible, bias=bias)
+        check_attention(pool, q, o, lse, cu, visible, bias=bias, slack=slack)
         off, _ = _attend(pool, q, cu, visible)
         assert torch.equal(off, o) == (not any(b.any() for b in bias))
     same, _ = _attend(pool, q, cu, visible, kv_frame_slot=_i32(slots), corr_uv=uv, corr_idx=idx, h=h, w=w, lam=0.0, sigma=2.0)
