@@ -386,8 +386,7 @@ constexpr int32_t kPagedMaxParts = 64;
 size_t paged_plan(PagedAttentionArgs& a, int32_t key_parts, int32_t max_keys, int32_t cus);
 double paged_units(const PagedAttentionArgs& a);
 hipError_t launch_paged_attention(const PagedAttentionArgs& a, hipStream_t stream);
-// its kernel of 128-row tiles (paged_tile.hip)
-constexpr int32_t kPagedTileRows = 128;
+// its kernel of tiles of 128 and 256 rows (paged_tile.hip)
 hipError_t launch_paged_tiles(const PagedAttentionArgs& a, hipStream_t stream);
 
 // Sets the calling thread's last-error string and returns status (capi.cpp).

@@ -658,7 +658,7 @@ size_t paged_plan(PagedAttentionArgs& a, int32_t key_parts, int32_t max_keys, in
     const PagedSeqs& q = a.seqs;
     const int64_t streams = q.B < q.n_tokens ? q.B : q.n_tokens;
     const int64_t rows = streams ? (int64_t)q.n_tokens * a.G / streams : 0;  // of a stream and key head, on average
-    a.rows = rows <= 16 ? 16 : (rows > 64 && a.dtype != kPagedF32 ? kPagedTileRows : 32);  // the tile kernel has no fp32 form
+    a.rows = rows <= 16 ? 16 : (rows <= 64 || a.dtype == kPagedF32 ? 32 : (rows <= 128 ? 128 : 256));  // the tile kernel has no fp32 form
     const int64_t tiles = q.cu ? (int64_t)q.n_tokens * a.G / a.rows + streams : q.B * (((int64_t)q.per * a.G + a.rows - 1) / a.rows);
     a.tiles = (int32_t)std::min<int64_t>(tiles, INT32_MAX);
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(max_keys, (int64_t)q.max_pages << q.page_log2));
@@ -667,9 +667,9 @@ size_t paged_plan(PagedAttentionArgs& a, int32_t key_parts, int32_t max_keys, in
     // workgroups of many waves where there are fewer units than compute units
     a.many = a.rows == 16 && units < cus;
     int64_t parts = key_parts;
-    if (parts == 0 && a.rows == kPagedTileRows) {
+    if (parts == 0 && a.rows >= 128) {
         AttentionArgs like{};  // its split is that of as many items of biased_chunk_attention
-        like.Lq = (int32_t)std::min<int64_t>(128 * tiles, INT32_MAX);
+        like.Lq = (int32_t)std::min<int64_t>(a.rows * tiles, INT32_MAX);
         like.Lk = (int32_t)most;
         like.H = a.Hk;
         like.layers = 1;
@@ -701,7 +701,7 @@ hipError_t launch_paged_attention(const PagedAttentionArgs& a, hipStream_t strea
             else launch(std::integral_constant<int, 2>{}, bias_tag, W4{});
         };
         hipError_t e;
-        if (a.rows == kPagedTileRows) {
+        if (a.rows >= 128) {
             e = launch_paged_tiles(a, stream);
         } else {
             if (a.S > 0) rows(std::true_type{});

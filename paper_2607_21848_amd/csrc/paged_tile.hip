@@ -40,7 +40,6 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 
 constexpr int kTK = 32;
-constexpr int kRows = 128;
 constexpr float kRescaleSlack = 8.0f;
 constexpr int kGridSide = 256;  // token-grid rows / columns of the bias tables
 constexpr int kCorrLds = 16;    // retrieved frames whose correspondences are staged in LDS
@@ -55,7 +54,7 @@ __device__ __forceinline__ int key_of(int hh, int i) { return 16 * (i >> 3) + 8 
 
 // chunk swizzle of LDS row r
 template <int D>
-__device__ __forceinline__ int swz(int r) { return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (r >> 1) & 7; }
+__device__ __forceinline__ int swz(int r) { return D == 128 ? ((r & 3) << 2) | (((r >> 2) & 3) ^ (r & 1)) : (r >> 1) & 7; }
 
 // max / sum of x over the lane and its partner in the other wave half
 __device__ __forceinline__ float half_swap_max(float x) {
@@ -95,17 +94,20 @@ struct Geom {
     int hw, w, h;
 };
 
-template <int D, int T, bool kBias>
-__global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a, Geom g, float c_log2) {
+template <int D, int T, bool kBias, int kW>
+__global__ __launch_bounds__(64 * kW, 2) void paged_tile_kernel(PagedAttentionArgs a, Geom g, float c_log2) {
     constexpr int kRowB = D * 2, kTileB = kTK * kRowB;      // in LDS
     constexpr int kStored = T == kPagedFp8 ? D : 2 * D;     // bytes of a row in the pages
     constexpr int kHalf = kTK * kStored / 16;               // 16-byte pieces of a K or V tile
-    constexpr int kPieces = 2 * kHalf / 256;                // of a thread
+    constexpr int kRows = 32 * kW, kThreads = 64 * kW;
+    constexpr int kPieces = (2 * kHalf + kThreads - 1) / kThreads;  // of a thread
     constexpr int kKk = D / 16, kDb = D / 32;
     __shared__ __attribute__((aligned(1024))) uint8_t ring[2][2 * kTileB];
     __shared__ u32x4 lds_tab[2][kBias ? kGridSide : 1];     // key operands by column and by row
     __shared__ float2 lds_corr[kBias ? kCorrLds : 1][kRows];  // centred correspondences, NaN: rejected
-    __shared__ int lds_seen[4], lds_least[4];
+    __shared__ int lds_block[512];
+    __shared__ float lds_scale[2][T == kPagedFp8 ? 512 : 1];
+    __shared__ int lds_seen[kW], lds_least[kW];
     __shared__ int lds_odd[2];  // V tile of a slot from which values that are not finite were taken out, or -1
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -157,8 +159,11 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
             lds_least[wave] = seen_min;
         }
         __syncthreads();
-        seen = max(max(lds_seen[0], lds_seen[1]), max(lds_seen[2], lds_seen[3]));
-        least = min(min(lds_least[0], lds_least[1]), min(lds_least[2], lds_least[3]));
+#pragma unroll
+        for (int w = 0; w < kW; ++w) {
+            seen = max(seen, lds_seen[w]);
+            least = min(least, lds_least[w]);
+        }
     }
     least = __builtin_amdgcn_readfirstlane(least);
     seen = __builtin_amdgcn_readfirstlane(seen);
@@ -168,47 +173,52 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
     const int nt = (int)((int64_t)(part + 1) * n_tiles / a.parts) - t0;  // this part's tiles
 
     // ---- the pages --------------------------------------------------------
-    const const_i32* pages = reinterpret_cast<const const_i32*>((uintptr_t)(sq.page_table + (int64_t)s * sq.max_pages));
     const int in_page = (1 << sq.page_log2) - 1;
-    // tile j of the part: its page entry, past the last one the last one's
-    auto entry_of = [&](int j) -> int { return pages[__builtin_amdgcn_readfirstlane(((t0 + min(j, nt - 1)) * kTK) >> sq.page_log2)]; };
-    auto is_page = [&](int entry) -> bool { return (unsigned)entry < (unsigned)sq.n_pages; };
-    // first row of a tile in the caches; a tile without a page takes page 0's rows, which nobody sees
-    auto tile_row = [&](int j, int entry) -> size_t {
-        return (((size_t)(is_page(entry) ? entry : 0) * a.Hk + hk) << sq.page_log2) + (((t0 + min(j, nt - 1)) * kTK) & in_page);
+    // Where the part's tiles lie, 256 at a time in LDS, the next 256 beside them (a scalar load in every step would make
+    // each wait for LDS a wait for it, a vector load one for the pieces in flight): the block of 32 rows of the
+    // caches, or -1 without a page (page 0's rows stand in for them, which nobody sees), and the scales.
+    auto fetch_info = [&](int j) __attribute__((always_inline)) {  // of tiles j + tid, past the last one the last one's
+        const int x = j + tid, pos = (t0 + min(x, nt - 1)) * kTK;
+        const int entry = sq.page_table[(int64_t)s * sq.max_pages + (pos >> sq.page_log2)];
+        const bool there = (unsigned)entry < (unsigned)sq.n_pages;
+        const int block = (((there ? entry : 0) * a.Hk + hk) << (sq.page_log2 - 5)) + ((pos & in_page) >> 5);
+        if constexpr (T == kPagedFp8) {
+            lds_scale[0][x & 511] = scale_value(a.scale_k[block]);
+            lds_scale[1][x & 511] = scale_value(a.scale_v[block]);
+        }
+        lds_block[x & 511] = there ? block : -1;
     };
+    auto block_of = [&](int j) __attribute__((always_inline)) -> int { return lds_block[j & 511]; };
     u32x4 piece[kPieces];
-    int k_byte = 0, v_byte = 0;
-    // pieces of K tile jk and V tile jv; piece p of a thread is number 256 p + tid of K's and then V's
-    auto load = [&](int jk, int ek, int jv, int ev) {
-        const size_t rk = tile_row(jk, ek), rv = tile_row(jv, ev);
-        const uint8_t* kb = static_cast<const uint8_t*>(a.cache_k) + rk * kStored;
-        const uint8_t* vb = static_cast<const uint8_t*>(a.cache_v) + rv * kStored;
+    // pieces of the K tile in block bk and the V tile in block bv; piece p of a thread is number kThreads p + tid of K's
+    // and then V's
+    auto load = [&](int bk, int bv) __attribute__((always_inline)) {
+        const uint8_t* kb = static_cast<const uint8_t*>(a.cache_k) + (size_t)(unsigned)max(bk, 0) * (kTK * kStored);
+        const uint8_t* vb = static_cast<const uint8_t*>(a.cache_v) + (size_t)(unsigned)max(bv, 0) * (kTK * kStored);
 #pragma unroll
         for (int p = 0; p < kPieces; ++p) {
-            const int i = 256 * p + tid;
-            const uint8_t* from = kHalf >= 256 ? (256 * p >= kHalf ? vb + 16 * (i - kHalf) : kb + 16 * i)
-                                               : (i >= kHalf ? vb + 16 * (i - kHalf) : kb + 16 * i);
-            piece[p] = *reinterpret_cast<const u32x4*>(from);
-        }
-        if constexpr (T == kPagedFp8) {
-            k_byte = a.scale_k[rk / kScaleBlock];
-            v_byte = a.scale_v[rv / kScaleBlock];
+            const int i = kThreads * p + tid;
+            if constexpr (kHalf % kThreads == 0) {
+                const uint32_t off = 16 * (uint32_t)tid;
+                piece[p] = *reinterpret_cast<const u32x4*>((kThreads * p >= kHalf ? vb + 16 * (kThreads * p - kHalf) : kb + 16 * kThreads * p) + off);
+            } else {
+                if (2 * kHalf % kThreads == 0 || i < 2 * kHalf) piece[p] = *reinterpret_cast<const u32x4*>(i >= kHalf ? vb + 16 * (i - kHalf) : kb + 16 * i);
+            }
         }
     };
     // A weight of 0 times a value that is not finite would be NaN. In a tile that some row does not see all of, such
     // values (and whatever lies behind the stream's end) are left out here; the rows that see them get them one by
     // one (`odd_values`).
-    auto store = [&](int which, int jv, int ev) {
+    auto store = [&](int which, float k_scale, float v_scale, int jv, int bv) __attribute__((always_inline)) {
         uint8_t* slot = ring[which];
-        if (__builtin_expect((t0 + jv + 1) * kTK > least || !is_page(ev), 0)) {
-            const float f = T == kPagedFp8 ? scale_value(v_byte) : 1.0f;
+        if (__builtin_expect((t0 + jv + 1) * kTK > least || bv < 0, 0)) {
+            const float f = T == kPagedFp8 ? v_scale : 1.0f;
             uint32_t odd = 0;
 #pragma unroll
             for (int p = 0; p < kPieces; ++p) {
-                const int i = 256 * p + tid - kHalf;
-                if (i < 0) continue;
-                const bool none = !is_page(ev) || (t0 + jv) * kTK + i / (kStored / 16) >= held;
+                const int i = kThreads * p + tid - kHalf;
+                if (i < 0 || (2 * kHalf % kThreads != 0 && i >= kHalf)) continue;
+                const bool none = bv < 0 || (t0 + jv) * kTK + i / (kStored / 16) >= held;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     uint32_t bad = f != f ? ~0u : spread<T>(not_finite<T>(piece[p][w]));
@@ -217,18 +227,19 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
                     piece[p][w] &= ~bad;
                 }
             }
-            if (f != f) v_byte = 127;
+            if (f != f) v_scale = 1.0f;
             if (odd) lds_odd[which] = jv;
         }
 #pragma unroll
         for (int p = 0; p < kPieces; ++p) {
-            const int i = 256 * p + tid;
+            const int i = kThreads * p + tid;
+            if (2 * kHalf % kThreads != 0 && i >= 2 * kHalf) continue;
             const bool is_v = i >= kHalf;
             const int at = is_v ? i - kHalf : i;
             const int row = at / (kStored / 16), c = at % (kStored / 16);
             uint8_t* to = slot + (is_v ? kTileB : 0) + row * kRowB;
             if constexpr (T == kPagedFp8) {
-                const float f = scale_value(is_v ? v_byte : k_byte);
+                const float f = is_v ? v_scale : k_scale;
                 u32x4 lo, hi;
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
@@ -268,12 +279,12 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
     const uint32_t one = 0x3f80u;
     const float inv_w = 1.0f / (float)g.w;
     const const_i32* slots = reinterpret_cast<const const_i32*>((uintptr_t)(a.slot + (int64_t)s * a.max_frames));
-    auto slot_of = [&](int f) -> int {
+    auto slot_of = [&](int f) __attribute__((always_inline)) -> int {
         const int v = f < a.max_frames ? slots[__builtin_amdgcn_readfirstlane(f)] : -1;
         return v >= 0 && v < a.S ? v : -1;
     };
     if constexpr (kBias) {
-        for (int i = tid; i < g.w + g.h; i += 256) {
+        for (int i = tid; i < g.w + g.h; i += kThreads) {
             const bool col = i < g.w;
             const int k = col ? i : i - g.w;
             const float ac = ((float)k + 0.5f) - (col ? g.cx : g.cy);
@@ -282,12 +293,12 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
             split3(-g.gamma * (ac * ac), ph, pm, pl);
             lds_tab[col ? 0 : 1][k] = u32x4{pack2(a2, a2), pack2(a2, ph), pack2(pm, pl), col ? pack2(one, one) : one};
         }
-        constexpr int kPer = kCorrLds * kRows / 256;
+        constexpr int kPer = kCorrLds * kRows / kThreads;
         int ci[kPer];
         float2 cu[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int e = tid + 256 * i, f = e >> 7, row = it.in * kRows + (e & 127);
+            const int e = tid + kThreads * i, f = e / kRows, row = it.in * kRows + e % kRows;
             ci[i] = -1;
             cu[i] = make_float2(0.0f, 0.0f);
             if (f < a.S && row < n_rows) {
@@ -298,12 +309,12 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
         }
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int e = tid + 256 * i;
-            lds_corr[e >> 7][e & 127] = ci[i] >= 0 ? make_float2(cu[i].x - g.cx, cu[i].y - g.cy) : make_float2(NAN, NAN);
+            const int e = tid + kThreads * i;
+            lds_corr[e / kRows][e % kRows] = ci[i] >= 0 ? make_float2(cu[i].x - g.cx, cu[i].y - g.cy) : make_float2(NAN, NAN);
         }
     }
     // query-side operand of retrieved frame f: zeros where the correspondence is rejected
-    auto query_operand = [&](int f) -> bf16x8 {
+    auto query_operand = [&](int f) __attribute__((always_inline)) -> bf16x8 {
         float ux = NAN, uy = NAN;
         if (f < kCorrLds) {
             const float2 u = lds_corr[f][wave * 32 + n];
@@ -326,7 +337,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
         }
         return as_bf16x8(v);
     };
-    auto key_operand = [&](int p) -> u32x4 {  // in-frame position p
+    auto key_operand = [&](int p) __attribute__((always_inline)) -> u32x4 {  // in-frame position p
         const int ky = (int)(((float)p + 0.5f) * inv_w);
         return lds_tab[hh][hh ? ky : p - ky * g.w];
     };
@@ -338,7 +349,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
         blk_t = t0 * kTK - blk_f * g.hw;
     }
     // 1: the tile lies in one retrieved frame (kop: the lane's key operand), 0: in one that is none, -1: across frames
-    auto classify = [&](u32x4& kop) -> int {
+    auto classify = [&](u32x4& kop) __attribute__((always_inline)) -> int {
         if (__builtin_expect(blk_t + kTK > g.hw, 0)) return -1;
         if (__builtin_expect(cur_f != blk_f, 0)) {
             cur_f = blk_f;
@@ -349,7 +360,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
         kop = key_operand(blk_t + krow);
         return 1;
     };
-    auto bias_add = [&](floatx16 x, int cls, const u32x4& kop) -> floatx16 {
+    auto bias_add = [&](floatx16 x, int cls, const u32x4& kop) __attribute__((always_inline)) -> floatx16 {
         if (cls > 0) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kop), qcur, x, 0, 0, 0);
         if (__builtin_expect(cls < 0, 0)) {
             const int lane_f = blk_f + (blk_t + krow) / g.hw, lane_p = (blk_t + krow) % g.hw;
@@ -377,12 +388,12 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
     float m_run = -FLT_MAX, m_thr = -INFINITY, l0 = 0.0f, l1 = 0.0f;
 
     // logits of tile j that a row does not see
-    auto mask = [&](floatx16& S, int j, int entry) {
-        const int k0 = (t0 + j) * kTK, lim = is_page(entry) ? vis : 0;
+    auto mask = [&](floatx16& S, int j, int block) __attribute__((always_inline)) {
+        const int k0 = (t0 + j) * kTK, lim = block < 0 ? 0 : vis;
 #pragma unroll
         for (int i = 0; i < 16; ++i) S[i] = k0 + key_of(hh, i) >= lim ? -INFINITY : S[i];
     };
-    auto row_max = [&](const floatx16& S) -> float {
+    auto row_max = [&](const floatx16& S) __attribute__((always_inline)) -> float {
         float x = max3(S[0], S[1], S[2]);
 #pragma unroll
         for (int i = 3; i < 15; i += 2) x = max3(x, S[i], S[i + 1]);
@@ -390,11 +401,10 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
     };
 
     // the values of V tile j that `store` left out, for the rows that see them (probabilities in S)
-    auto odd_values = [&](const floatx16& S, int j, int entry) {
+    auto odd_values = [&](const floatx16& S, int j, int block) __attribute__((always_inline)) {
         const int k0 = (t0 + j) * kTK;
-        const size_t row = tile_row(j, entry);
-        const uint8_t* base = static_cast<const uint8_t*>(a.cache_v) + row * kStored;
-        const float f = T == kPagedFp8 ? scale_value(a.scale_v[row / kScaleBlock]) : 1.0f;
+        const uint8_t* base = static_cast<const uint8_t*>(a.cache_v) + (size_t)(unsigned)block * (kTK * kStored);
+        const float f = T == kPagedFp8 ? scale_value(a.scale_v[block]) : 1.0f;
 #pragma unroll 1
         for (int key = 0; key < min(kTK, held - k0); ++key) {
             const int want = 8 * (key >> 4) + (key & 7);  // register of the lane that has its probability
@@ -415,7 +425,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
 
     floatx16 Sa, Sb;
     float mx = -INFINITY;
-    int e0 = 0, e1 = 0, e2 = 0;  // page entries of tiles j, j + 1 and j + 2
+    int b0 = 0, b1 = 0, b2 = 0;  // blocks of tiles j, j + 1 and j + 2
 
     // One step: softmax and P V of tile j, whose logits are in S_cur, beside the logits of tile j + 1.
     auto step = [&](int j, floatx16& S_cur, floatx16& S_next, auto slot_tag) __attribute__((always_inline)) {
@@ -429,7 +439,8 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
         kread(0);
         kread(1);
         kread(2);
-        const int e3 = entry_of(j + 3);
+        const int b3_lane = block_of(j + 3);
+        const float k_scale = T == kPagedFp8 ? lds_scale[0][(j + 2) & 511] : 1.0f, v_scale = T == kPagedFp8 ? lds_scale[1][(j + 1) & 511] : 1.0f;
         u32x4 kop = u32x4{0, 0, 0, 0};
         int cls = 0;
         if constexpr (kBias) cls = classify(kop);
@@ -479,12 +490,13 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
             S_next = bias_add(S_next, cls, kop);
             __builtin_amdgcn_sched_barrier(0);
         }
-        // the pieces of K_{j+2} and V_{j+1} go to LDS, those of the tiles behind them leave
-        store(kRefill, min(j + 1, nt - 1), e1);
-        load(j + 3, e3, j + 2, e2);
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int u = 0; u < 6; ++u) unit(u >> 2, u & 3);
+        __builtin_amdgcn_sched_barrier(0);
+        // the pieces of K_{j+2} and V_{j+1} go to LDS, those of the tiles behind them leave
+        store(kRefill, k_scale, v_scale, min(j + 1, nt - 1), b1);
+        const int b3 = __builtin_amdgcn_readfirstlane(b3_lane);
+        load(b3, b2);
         __builtin_amdgcn_sched_barrier(0);
         const bf16x8 pf0 = as_bf16x8(u32x4{w4[0][0], w4[0][1], w4[0][2], w4[0][3]});
 #pragma unroll
@@ -495,31 +507,39 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
             __builtin_amdgcn_sched_barrier(0);
         }
         const bf16x8 pf1 = as_bf16x8(u32x4{w4[1][0], w4[1][1], w4[1][2], w4[1][3]});
-        if (__builtin_expect((t0 + j + 2) * kTK > seen_min || !is_page(e1), 0)) mask(S_next, j + 1, e1);
 #pragma unroll
         for (int db = 0; db < kDb; ++db) {
             O[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(voperand(1, db), pf1, O[db], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
+        if (__builtin_expect((t0 + j + 2) * kTK > seen_min || b1 < 0, 0)) mask(S_next, j + 1, b1);
         mx = row_max(S_next);
-        if (__builtin_expect((t0 + j + 1) * kTK > least && lds_odd[(j + 1) & 1] == j, 0)) odd_values(S_cur, j, e0);
+        if (__builtin_expect((t0 + j + 1) * kTK > least, 0)) {
+            asm volatile("" ::: "memory");  // lds_odd is read for such tiles alone
+            if (lds_odd[1 - kRefill] == j) odd_values(S_cur, j, b0);
+        }
+        if (__builtin_expect(((j + 4) & 255) == 128, 0)) {
+            if (tid < 256) fetch_info(((j + 4) & ~255) + 256);
+        }
         if (!more) mx = -INFINITY;
-        e0 = e1;
-        e1 = e2;
-        e2 = e3;
+        b0 = b1;
+        b1 = b2;
+        b2 = b3;
     };
 
     if (nt > 0) {
-        e0 = entry_of(0);
-        e1 = entry_of(1);
-        e2 = entry_of(2);
-        load(0, e0, 0, e0);
+        if (tid < 256) fetch_info(0);
         if (tid < 2) lds_odd[tid] = -1;
         __syncthreads();
-        store(0, 0, e0);
-        load(1, e1, 0, e0);
-        store(1, 0, e0);
-        load(2, e2, 1, e1);
+        auto scale = [&](int which, int j) -> float { return T == kPagedFp8 ? lds_scale[which][j] : 1.0f; };
+        b0 = __builtin_amdgcn_readfirstlane(block_of(0));
+        b1 = __builtin_amdgcn_readfirstlane(block_of(1));
+        b2 = __builtin_amdgcn_readfirstlane(block_of(2));
+        load(b0, b0);
+        store(0, scale(0, 0), scale(1, 0), 0, b0);
+        load(b1, b0);
+        store(1, scale(0, 1), scale(1, 0), 0, b0);
+        load(b2, b1);
         __syncthreads();
         u32x4 kop = u32x4{0, 0, 0, 0};
         int cls = 0;
@@ -529,7 +549,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
         for (int kk = 0; kk < kKk; ++kk)
             Sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(ring[0] + koff[kk]), as_bf16x8(qf[kk]), Sa, 0, 0, 0);
         if constexpr (kBias) Sa = bias_add(Sa, cls, kop);
-        if ((t0 + 1) * kTK > seen_min || !is_page(e0)) mask(Sa, 0, e0);
+        if ((t0 + 1) * kTK > seen_min || b0 < 0) mask(Sa, 0, b0);
         mx = row_max(Sa);
         for (int j = 0;;) {
             step(j, Sa, Sb, std::integral_constant<int, 0>{});
@@ -580,12 +600,17 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttentionArgs a
 hipError_t launch_paged_tiles(const PagedAttentionArgs& a, hipStream_t stream) {
     const float c = a.softmax_scale * 1.4426950408889634f;
     const Geom g{a.gamma, 0.5f * (float)a.w, 0.5f * (float)a.h, a.h * a.w, a.w, a.h};
-    const dim3 grid = grid_rows(xcd_grid((unsigned)a.tiles * (unsigned)a.Hk * (unsigned)a.parts)), block(256);
+    const dim3 grid = grid_rows(xcd_grid((unsigned)a.tiles * (unsigned)a.Hk * (unsigned)a.parts)), block(2 * a.rows);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, g, c); };
     auto bias = [&](auto d_tag, auto t_tag) {
         constexpr int D = decltype(d_tag)::value, T = decltype(t_tag)::value;
-        if (a.S > 0) launch(paged_tile_kernel<D, T, true>);
-        else launch(paged_tile_kernel<D, T, false>);
+        if (a.rows == 256) {
+            if (a.S > 0) launch(paged_tile_kernel<D, T, true, 8>);
+            else launch(paged_tile_kernel<D, T, false, 8>);
+        } else {
+            if (a.S > 0) launch(paged_tile_kernel<D, T, true, 4>);
+            else launch(paged_tile_kernel<D, T, false, 4>);
+        }
     };
     using Fp8 = std::integral_constant<int, kPagedFp8>;
     using Bf16 = std::integral_constant<int, kPagedBf16>;
