@@ -16,7 +16,11 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "librevisit.so")
 SOURCES = ["capi.cpp", "retrieve.hip", "reproject.hip", "attention.hip", "kvpack.hip", "stream.cpp", "stream_kernels.hip",
-           "rotary.hip", "keyweight.hip", "select.hip", "compact.hip", "paged_append.hip", "paged_attention.hip", "paged_tile.hip"]
+           "rotary.hip", "keyweight.hip", "select.hip", "compact.hip", "paged_append.hip", "paged_attention.hip"]
+# compiled with the matrix instructions accumulating in the registers that vector instructions read: a kernel of more
+# than 256 registers otherwise gets the others, and a move for each element that it reads
+WIDE_SOURCES = ["paged_tile.hip"]
+WIDE_FLAGS = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
 ARCH = "gfx950"
 
 
@@ -43,10 +47,10 @@ def build(verbose: bool = False) -> str:
     objdir = os.path.join(PKG_DIR, "_build")
     os.makedirs(objdir, exist_ok=True)
     objs = []
-    for src in SOURCES:
+    for src in SOURCES + WIDE_SOURCES:
         obj = os.path.join(objdir, src.rsplit(".", 1)[0] + ".o")
         lang = ["-x", "hip"] if src.endswith(".hip") else []
-        cmd = [cc, *compile_flags(), *lang, "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [cc, *compile_flags(), *(WIDE_FLAGS if src in WIDE_SOURCES else []), *lang, "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.run(cmd, check=True)

@@ -658,22 +658,39 @@ size_t paged_plan(PagedAttentionArgs& a, int32_t key_parts, int32_t max_keys, in
     const PagedSeqs& q = a.seqs;
     const int64_t streams = q.B < q.n_tokens ? q.B : q.n_tokens;
     const int64_t rows = streams ? (int64_t)q.n_tokens * a.G / streams : 0;  // of a stream and key head, on average
-    a.rows = rows <= 16 ? 16 : (rows <= 64 || a.dtype == kPagedF32 ? 32 : (rows <= 128 ? 128 : 256));  // the tile kernel has no fp32 form
-    const int64_t tiles = q.cu ? (int64_t)q.n_tokens * a.G / a.rows + streams : q.B * (((int64_t)q.per * a.G + a.rows - 1) / a.rows);
-    a.tiles = (int32_t)std::min<int64_t>(tiles, INT32_MAX);
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(max_keys, (int64_t)q.max_pages << q.page_log2));
     const int64_t key_tiles = (most + kTK - 1) / kTK;
+    auto tiles_of = [&](int64_t r) { return q.cu ? (int64_t)q.n_tokens * a.G / r + streams : q.B * (((int64_t)q.per * a.G + r - 1) / r); };
+    // Up to 32 rows, and where a compute unit has no more than 32 tiles of 32 rows and keys to do, a wave for each range
+    // of keys (12 heads of 128: 300 queries on 300 keys 10 us, 64 on 2000 17); else the tile kernel (15 and 19 us; but
+    // 64 on 20000 37, for 50, and 1000 on 1000 31, for 42). That one has no fp32 form; at D = 128 its tiles are of 256
+    // rows where a stream has more than 128 (200 queries on 20000 keys 58 us, for 61; 4680 on 28080 878, for 1264).
+    if (rows <= 16) a.rows = 16;
+    else if (rows <= 32 || a.dtype == kPagedF32 || tiles_of(32) * a.Hk * key_tiles <= 32 * (int64_t)cus) a.rows = 32;
+    else a.rows = rows <= 128 || a.D == 64 ? 128 : 256;
+    const int64_t tiles = tiles_of(a.rows);
+    a.tiles = (int32_t)std::min<int64_t>(tiles, INT32_MAX);
     const int64_t units = std::max<int64_t>(1, tiles * a.Hk);
     // workgroups of many waves where there are fewer units than compute units
     a.many = a.rows == 16 && units < cus;
     int64_t parts = key_parts;
     if (parts == 0 && a.rows >= 128) {
-        AttentionArgs like{};  // its split is that of as many items of biased_chunk_attention
-        like.Lq = (int32_t)std::min<int64_t>(a.rows * tiles, INT32_MAX);
-        like.Lk = (int32_t)most;
-        like.H = a.Hk;
-        like.layers = 1;
-        parts = attention_bf16_key_parts(like, cus);
+        // The number of parts with the least estimated time: rounds of as many workgroups as the chip has places, a time
+        // per 32-key step that was measured at each tile, six steps' time for a workgroup's start and end, and a merge
+        // (a launch, and the parts' results written and read). 12 heads on 20000 keys: 100 queries 401 us whole, 43 in 16
+        // parts; 400 queries 551 whole, 89 in 9; 4680 queries on 28080 keys 878 whole, 911 in two.
+        const int64_t places = a.D == 64 ? 2 * (int64_t)cus : cus;
+        const double step = a.rows == 256 ? 0.9 : (a.D == 128 ? 0.65 : 0.72);
+        double best = INFINITY;
+        for (int64_t p = 1; p <= std::min<int64_t>(key_tiles, kPagedMaxParts) && (p == 1 || units * p <= 2 * places); ++p) {
+            const double rounds = (double)((units * p + places - 1) / places);
+            double us = rounds * (double)((key_tiles + p - 1) / p + 6) * step;
+            if (p > 1) us += 3.0 + 0.0002 * (double)(units * p * a.rows);
+            if (us < 0.985 * best) {
+                best = us;
+                parts = p;
+            }
+        }
     } else if (parts == 0) {
         parts = a.many ? std::min<int64_t>(cus / units, key_tiles / 4) : std::min<int64_t>((2 * (int64_t)cus + units - 1) / units, key_tiles / 16);
     }

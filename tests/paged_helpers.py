@@ -23,13 +23,15 @@ def values(g, dtype, *shape):
 class Pool:
     """A pool of pages full of values, the page table of streams of `lens` positions, and what they hold."""
 
+    room = 0  # positions that a table has entries for, at least
+
     def __init__(self, seed, dtype, lens, H, D, page, spare=2, max_pages=None):
         g = gen(seed)
         self.dtype, self.lens, self.H, self.D, self.page = dtype, list(lens), H, D, page
         need = [-(-n // page) for n in lens]
         self.n_pages = sum(need) + spare
         order = torch.randperm(self.n_pages, generator=g, device=DEV).cpu().numpy()
-        self.table = np.full((len(lens), max_pages or max(need + [1])), -1, np.int32)
+        self.table = np.full((len(lens), max_pages or max(need + [1, self.room // page])), -1, np.int32)
         at = 0
         for s, n in enumerate(need):
             self.table[s, :n] = order[at:at + n]

@@ -15,6 +15,13 @@ pytestmark = pytest.mark.gpu
 NAN, INF = float("nan"), float("inf")
 
 
+@pytest.fixture(autouse=True, params=[0, 1 << 19], ids=["table", "wide_table"])
+def room(request, monkeypatch):
+    """Page tables with just the entries that the streams need, and with entries for far longer ones, for which other
+    tiles are chosen."""
+    monkeypatch.setattr(Pool, "room", request.param)
+
+
 def _i32(x):
     return torch.tensor(np.asarray(x), dtype=torch.int32, device=DEV)
 
@@ -279,3 +286,32 @@ def test_refusals():
     ]:
         with pytest.raises(err):
             rv.paged_chunk_attention(*args, **kw)
+
+
+@pytest.mark.parametrize("dtype", [FP8, BF16, F32])
+@pytest.mark.parametrize("D,Hq,Hk,m", [(64, 2, 1, 80), (128, 1, 1, 70), (128, 1, 1, 140), (128, 4, 1, 2)])
+def test_long(dtype, D, Hq, Hk, m):
+    """20000 keys, of which a query sees up to its own one."""
+    L = 20000
+    pool = Pool(23, dtype, [L], Hk, D, 64)
+    q = values(gen(24), GIVEN[dtype], m, Hq, D)
+    visible = np.linspace(1, L, m).astype(np.int32)
+    for parts in (0, 1):
+        o, lse = _attend(pool, q, None, visible, key_parts=parts)
+        check_attention(pool, q, o, lse, None, visible)
+
+
+@pytest.mark.parametrize("dtype", [FP8, BF16, F32])
+@pytest.mark.parametrize("m", [3, 40, 150])
+def test_bias_of_many_frames(dtype, m):
+    """More retrieved frames than the kernels keep the correspondences of, and key frames of each of them."""
+    h, w, S, D = 3, 11, 19, 64 if m == 40 else 128
+    frames = 2 * S
+    pool = Pool(25, dtype, [frames * h * w - 5], 1, D, 32)
+    slots = np.random.default_rng(26).permutation(np.concatenate([np.arange(S), np.full(S, -1)]))[None].astype(np.int32)
+    uv, idx, bias = _bias(pool, m, None, S, h, w, slots, 27, 2.0, 1.3)
+    q = values(gen(28), GIVEN[dtype], m, 1, D)
+    off_centre = np.nan_to_num(uv.cpu().numpy().astype(np.float64) - (w / 2, h / 2))
+    largest = 1.3 * ((h * h + w * w) / 4 + (off_centre ** 2).sum(-1).max()) / (2 * 2.0 ** 2)
+    o, lse = _attend(pool, q, kv_frame_slot=_i32(slots), corr_uv=uv, corr_idx=idx, h=h, w=w, lam=1.3, sigma=2.0)
+    check_attention(pool, q, o, lse, bias=bias, slack=0.0 if dtype == F32 else 8 * 2.0 ** -24 * largest)
