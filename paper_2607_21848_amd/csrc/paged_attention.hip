@@ -674,25 +674,33 @@ size_t paged_plan(PagedAttentionArgs& a, int32_t key_parts, int32_t max_keys, in
     // workgroups of many waves where there are fewer units than compute units
     a.many = a.rows == 16 && units < cus;
     int64_t parts = key_parts;
-    if (parts == 0 && a.rows >= 128) {
-        // The number of parts with the least estimated time: rounds of as many workgroups as the chip has places, a time
-        // per 32-key step that was measured at each tile, six steps' time for a workgroup's start and end, and a merge
-        // (a launch, and the parts' results written and read). 12 heads on 20000 keys: 100 queries 401 us whole, 43 in 16
-        // parts; 400 queries 551 whole, 89 in 9; 4680 queries on 28080 keys 878 whole, 911 in two.
-        const int64_t places = a.D == 64 ? 2 * (int64_t)cus : cus;
-        const double step = a.rows == 256 ? 0.9 : (a.D == 128 ? 0.65 : 0.72);
+    if (parts == 0 && a.many) {
+        // One workgroup per compute unit, four key tiles a part (a token, 12 heads of 8 bits: 1560 keys whole 14.4 us, in 8
+        // parts 10.2; 12000 71.5 and 16.6), but a range as short as a launch takes whole (300 keys 7.6 us, in two 9.7).
+        parts = key_tiles <= (a.dtype == kPagedF32 ? 8 : 16) ? 1 : std::min<int64_t>(cus / units, key_tiles / 4);
+    } else if (parts == 0) {
+        // The number of parts with the least estimated time: the busiest compute unit's workgroups, one after the other (two
+        // at a time for the tile kernel at D = 64), a time per 32-key step that was measured at each size of tile, 4 us for
+        // a workgroup's start and end, and a merge (a launch, and the parts' results written and read). 12 heads of 8
+        // bits on 20000 keys: 100 queries 401 us whole, 43 in 16 parts; 400 queries 551 whole, 89 in 9; 4680 queries on 28080
+        // keys 878 whole, 911 in two. fp32: 200 queries on 4000 keys 155 us whole, 65 in 3; 800 305 and, in 4, 221;
+        // 1170 on 7020 583 whole, 628 in two. 264 single rows on 30000 keys: 503 us whole, 375 in 4.
+        const int64_t places = a.rows == 128 && a.D == 64 ? 2 * (int64_t)cus : cus;
+        const double step = a.rows == 256 ? 0.9
+                            : a.rows == 128 ? (a.D == 128 ? 0.65 : 0.72)
+                            : a.rows == 32  ? (a.dtype == kPagedF32 ? 1.25 : 0.32)
+                                            : (a.dtype == kPagedF32 ? 0.6 : 0.27);
+        const int64_t most_parts = std::min<int64_t>(kPagedMaxParts, a.rows >= 128 ? key_tiles : key_tiles / 16);
         double best = INFINITY;
-        for (int64_t p = 1; p <= std::min<int64_t>(key_tiles, kPagedMaxParts) && (p == 1 || units * p <= 2 * places); ++p) {
-            const double rounds = (double)((units * p + places - 1) / places);
-            double us = rounds * (double)((key_tiles + p - 1) / p + 6) * step;
-            if (p > 1) us += 3.0 + 0.0002 * (double)(units * p * a.rows);
+        for (int64_t n = 1; n == 1 || (n <= most_parts && units * n <= 4 * places); ++n) {
+            const double rounds = (double)((units * n + places - 1) / places);
+            double us = rounds * ((double)((key_tiles + n - 1) / n) * step + 4.0);
+            if (n > 1) us += 3.0 + 0.0002 * (double)(units * n * a.rows);
             if (us < 0.985 * best) {
                 best = us;
-                parts = p;
+                parts = n;
             }
         }
-    } else if (parts == 0) {
-        parts = a.many ? std::min<int64_t>(cus / units, key_tiles / 4) : std::min<int64_t>((2 * (int64_t)cus + units - 1) / units, key_tiles / 16);
     }
     a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(parts, kPagedMaxParts), key_tiles));
     return a.parts > 1 ? (size_t)tiles * a.Hk * a.parts * paged_part_floats(a.rows, a.D) * sizeof(float) : 0;
