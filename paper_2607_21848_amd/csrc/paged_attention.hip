@@ -87,7 +87,8 @@ struct PagedBias {
     float ng;
 };
 
-constexpr int kManyWaves = 8;  // of a workgroup where there are few
+constexpr int kManyWaves = 8;   // of a workgroup where there are few
+constexpr int kCorrFrames = 16, kSlotFrames = 256;  // retrieved and key frames whose correspondences and slots are kept in LDS
 
 template <int D, int T, int NQ, bool kBias, int kW>
 __global__ __launch_bounds__(64 * kW, kW > 4 || (NQ == 1 && (T != kPagedF32 || D == 64)) ? 2 : 1) void paged_wave_kernel(PagedAttentionArgs a, float c_log2) {
@@ -98,6 +99,9 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (NQ == 1 && (T != kPagedF32 || D
     // few rows leave the matrix cores idle: their probabilities go in as two bf16 values each, off by 2^-17 (a single
     // one, 2^-9, made outputs of a few heavy keys 1.6 times as far off as their own rounding does)
     constexpr bool kFine = !kF32 && NQ == 1;
+    // The next tile's keys leave behind this one's logits, its values behind this one's product, where the registers hold both
+    // beside each other (1170 fp32 queries on 7020 keys 606 us without, 567 with).
+    constexpr bool kAhead = !kF32 || NQ == 2 || D == 64 || kW == 4;
     __shared__ float lds_o[kW][NQ * kDb * 64 * 4];
     __shared__ float lds_m[kW][kRows], lds_l[kW][kRows];
     __shared__ int lds_token[kRows], lds_head[kRows];
@@ -241,24 +245,43 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (NQ == 1 && (T != kPagedF32 || D
     auto grid_row = [&](int p) -> int { return kF32 && hw > (1 << 20) ? p / a.w : (int)(((float)p + 0.5f) * inv_w); };
     Corr corr[NQ];
     int corr_f = -1;
-    // what a new frame needs waits in LDS: as kernel arguments in scalar registers it made the compiler spill some
+    // What a new frame needs waits in LDS: loaded when the frame changes, it made the tiles in flight be waited for, too (30
+    // queries on 7020 8-bit keys, 3 of their 18 frames retrieved, in one part: 97 us, from LDS 92); and the arguments of
+    // frames past those that are kept, in scalar registers, made the compiler spill some.
     __shared__ PagedBias lds_b;
+    __shared__ float2 lds_corr[kBias ? kCorrFrames : 1][kRows];  // NaN: rejected
+    __shared__ int lds_slot[kBias ? kSlotFrames : 1];
     if constexpr (kBias) {
-        if (threadIdx.x == 0) lds_b = PagedBias{a.slot + (int64_t)s * a.max_frames, a.corr_uv, a.corr_idx, a.max_frames, a.S, sq.n_tokens, -a.gamma};
+        const int* slots = a.slot + (int64_t)s * a.max_frames;
+        if (threadIdx.x == 0) lds_b = PagedBias{slots, a.corr_uv, a.corr_idx, a.max_frames, a.S, sq.n_tokens, -a.gamma};
+        for (int f = threadIdx.x; f < min(a.max_frames, kSlotFrames); f += 64 * kW) lds_slot[f] = slots[f];
+        for (int e = threadIdx.x; e < min(a.S, kCorrFrames) * kRows; e += 64 * kW) {
+            const int r = it.in * kRows + e % kRows;
+            float2 u = make_float2(NAN, NAN);
+            if (r < n_rows) {
+                const int64_t o = (int64_t)(e / kRows) * sq.n_tokens + tok.x + r / G;
+                if (a.corr_idx[o] >= 0) u = reinterpret_cast<const float2*>(a.corr_uv)[o];
+            }
+            lds_corr[e / kRows][e % kRows] = u;
+        }
         __syncthreads();
     }
     auto frame_corr = [&](int f) {
         corr_f = f;
         const PagedBias c = lds_b;
-        const int slot = f < c.max_frames ? c.slot[f] : -1;
+        const int slot = f >= c.max_frames ? -1 : (f < kSlotFrames ? lds_slot[f] : c.slot[f]);
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) {
             corr[nq] = Corr{0.0f, 0.0f, 0.0f};
-            if (slot >= 0 && slot < c.S && token[nq] >= 0) {
+            if (slot < 0 || slot >= c.S) continue;
+            float2 u = make_float2(NAN, NAN);
+            if (slot < kCorrFrames) {
+                u = lds_corr[slot][16 * nq + m];
+            } else if (token[nq] >= 0) {
                 const int64_t o = (int64_t)slot * c.n_tokens + token[nq];
-                const float2 u = reinterpret_cast<const float2*>(c.corr_uv)[o];
-                if (c.corr_idx[o] >= 0) corr[nq] = Corr{c.ng, u.x, u.y};
+                if (c.corr_idx[o] >= 0) u = reinterpret_cast<const float2*>(c.corr_uv)[o];
             }
+            if (!__builtin_isnan(u.x)) corr[nq] = Corr{c.ng, u.x, u.y};
         }
     };
 
@@ -279,7 +302,7 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (NQ == 1 && (T != kPagedF32 || D
     auto work = [&](Tile& b) __attribute__((always_inline)) {
         const int t = b.t, page = b.page, k0 = t * kTK;
         const bool masked = k0 + kTK > seen_min;  // some query does not see all of the tile's keys
-        if constexpr (kF32) load_k(b, t, page);
+        if constexpr (!kAhead) load_k(b, t, page);
         take(b);
         const bool more = b.t < t_end;
         const int t_load = more ? b.t : t, page_load = more ? b.page : page;  // without another it is loaded again and not used
@@ -326,17 +349,18 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (NQ == 1 && (T != kPagedF32 || D
         }
         if constexpr (kF32) {
 #pragma unroll
-            for (int u = 0; u < D / 16; ++u)
+            for (int u = 0; u < D / 16; ++u) {
+                floatx4 qv[NQ];
 #pragma unroll
-                for (int nq = 0; nq < NQ; ++nq) {
-                    const floatx4 qv = lds_q[nq * (D / 16) + u][lane];
+                for (int nq = 0; nq < NQ; ++nq) qv[nq] = lds_q[nq * (D / 16) + u][lane];
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const floatx4 kv = __builtin_bit_cast(floatx4, b.kr[half][u]);
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) S[nq][half] = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[i], qv[i], S[nq][half], 0, 0, 0);
-                    }
-                }
+                    for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                        for (int half = 0; half < 2; ++half)
+                            S[nq][half] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(floatx4, b.kr[half][u])[i], qv[nq][i], S[nq][half], 0, 0, 0);
+            }
         } else {
             const float k_scale = T == kPagedFp8 ? scale_value(b.k_byte) : 1.0f;
 #pragma unroll
@@ -355,8 +379,8 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (NQ == 1 && (T != kPagedF32 || D
                         S[nq][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), as_bf16x8(qf[nq][st]), S[nq][half], 0, 0, 0);
                 }
         }
-        if constexpr (kF32) load_v(b, t, page);
-        else load_k(b, t_load, page_load);
+        if constexpr (kAhead) load_k(b, t_load, page_load);
+        else load_v(b, t, page);
 
         // softmax: the lane's eight logits of each of its columns
         u32x4 pf[NQ], pl[1];
@@ -500,12 +524,12 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (NQ == 1 && (T != kPagedF32 || D
                 }
             }
         }
-        if constexpr (!kF32) load_v(b, t_load, page_load);
+        if constexpr (kAhead) load_v(b, t_load, page_load);
     };
 
     Tile now;
     take(now);
-    if (!kF32 && now.t < t_end) {
+    if (kAhead && now.t < t_end) {
         load_k(now, now.t, now.page);
         load_v(now, now.t, now.page);
     }
