@@ -1090,8 +1090,9 @@ int append_paged_kv(const void* k, int64_t k_row, const void* v, int64_t v_row, 
     a.n_t = pairs_t;
     a.n_y = pairs_y;
     a.n_x = pairs_x;
-    const int pairs = pairs_t + pairs_y + pairs_x;
-    a.inv_pairs = pairs > 0 ? 1.0f / (float)pairs : 0.0f;
+    a.inv_pairs[0] = pairs_t > 0 ? 1.0f / (float)pairs_t : 0.0f;
+    a.inv_pairs[1] = pairs_y > 0 ? 1.0f / (float)pairs_y : 0.0f;
+    a.inv_pairs[2] = pairs_x > 0 ? 1.0f / (float)pairs_x : 0.0f;
     if (revisit::paged_append_blocks(a) > (1 << 30)) return fail(REVISIT_ERR_SHAPE, "%s: problem too large", fn);
     revisit::PagedFreq f;
     band_quarters((double)theta, pairs_t, f.quarter);

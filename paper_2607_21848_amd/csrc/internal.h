@@ -347,7 +347,7 @@ struct PagedAppendArgs {
     const int32_t* pos;     // nullable [n_tokens][3]: time, row, column
     int32_t t0, hw, w;      // pos NULL: position c of a stream stands at (t0 + c / hw, c / w mod h, c mod w)
     int32_t n_t, n_y, n_x;  // pairs of each band
-    float inv_pairs;        // 1 / (n_t + n_y + n_x)
+    float inv_pairs[3];     // 1 / n_t, 1 / n_y, 1 / n_x
 };
 struct PagedFreq {
     double quarter[64];  // quarter turns per position, of every pair (D <= 128)

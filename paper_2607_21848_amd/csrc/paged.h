@@ -17,20 +17,25 @@ constexpr int kScaleBlock = 32;    // positions that share a scale
 constexpr int kScaleLow = -100;    // smallest exponent that is written: 2^-110, the smallest value, is far above what bf16 flushes
 constexpr int kScaleHigh = 120;    // largest one that an fp32 value needs
 
+typedef const __attribute__((address_space(4))) int32_t const_i32;  // memory that does not change while the kernel runs
+
+// Element i of a list that no output overlaps: a scalar load where i is uniform.
+__device__ __forceinline__ int32_t listed(const int32_t* list, int64_t i) { return reinterpret_cast<const_i32*>((uintptr_t)list)[i]; }
+
 // Positions that stream s holds, within what its row of the table can hold.
-__device__ __forceinline__ int held_of(const PagedSeqs& q, int s) { return min(max(q.kv_len[s], 0), q.max_pages << q.page_log2); }
+__device__ __forceinline__ int held_of(const PagedSeqs& q, int s) { return min(max(listed(q.kv_len, s), 0), q.max_pages << q.page_log2); }
 
 // First token of stream s among the call's and how many it has. Lists that are not ascending give no access out of range.
 __device__ __forceinline__ int2 tokens_of(const PagedSeqs& q, int s) {
     if (!q.cu) return make_int2(s * q.per, q.per);
-    const int a = min(max(q.cu[s], 0), q.n_tokens);
-    return make_int2(a, max(min(q.cu[s + 1], q.n_tokens), a) - a);
+    const int a = min(max(listed(q.cu, s), 0), q.n_tokens);
+    return make_int2(a, max(min(listed(q.cu, (int64_t)s + 1), q.n_tokens), a) - a);
 }
 
 // Page of entry i of stream s, or -1: outside the table's row or the pool.
 __device__ __forceinline__ int page_of(const PagedSeqs& q, int s, int i) {
     if (i >= q.max_pages) return -1;
-    const int p = q.page_table[(int64_t)s * q.max_pages + i];
+    const int p = listed(q.page_table, (int64_t)s * q.max_pages + i);
     return p < q.n_pages ? p : -1;
 }
 
@@ -82,8 +87,6 @@ __device__ __forceinline__ StreamItem row_tile(const PagedAttentionArgs& a, int 
 
 // floats of a part's result of a tile: O [rows][D], maxima [rows], sums [rows]
 __host__ __device__ constexpr int paged_part_floats(int rows, int D) { return rows * (D + 2); }
-
-typedef __attribute__((address_space(4))) int32_t const_i32;  // memory that does not change while the kernel runs
 
 // 2^(byte - 127) of a scale: byte 0 counts as 1, 255 is NaN
 __device__ __forceinline__ float scale_value(int byte) { return byte == 255 ? NAN : __uint_as_float((uint32_t)max(byte, 1) << 23); }

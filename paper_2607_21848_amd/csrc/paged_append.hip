@@ -10,7 +10,11 @@
 //
 // Every input byte is read once and every output byte written once: bound by HBM. One wave takes a (block of 32
 // positions, head), so that it has what a scale depends on in its registers: all loads leave first, the
-// angles' cos and sin, which the four heads of a workgroup share, are computed while they are in flight.
+// angles' cos and sin, which the four heads of a workgroup share, are computed while they are in flight. A chunk's
+// waves are all resident at once, so its time is one wave's: few instructions, and few waits one after the other.
+// Lengths and pages come by scalar loads; largest values are found two bf16 at a time; a conversion takes the scale
+// along. 10800 tokens of 40 heads of 128 into 8 bits 65.6 us (5.05 TB/s), 4680 of 12 heads 12.5 us, a token of each of
+// 128 streams 7.7. Workgroups of eight waves: 70.5, 20.8 and 9.4 (of 65, 16 and 8.7 with four at that step).
 
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -27,6 +31,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short shortx2 __attribute__((ext_vector_type(2)));
+typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;  // heads of a workgroup
 
@@ -40,9 +46,6 @@ __device__ __forceinline__ uint32_t finite_bits(float x) {
     return b < 0x7f800000u ? b : 0u;
 }
 
-// what is not finite is stored as NaN: e4m3 has no infinity, and its largest value would hide one
-__device__ __forceinline__ float nan_if_not_finite(float x) { return finite_bits(x) == (__float_as_uint(x) & 0x7fffffffu) ? x : NAN; }
-
 // least e in [kScaleLow, kScaleHigh] with m <= 448 2^e, m >= 0 by its bits: 448 = 1.75 2^8
 __device__ __forceinline__ int scale_exponent(uint32_t m) {
     const int e = (int)(m >> 23) - 127 - 8 + ((m & 0x7fffffu) > 0x600000u ? 1 : 0);
@@ -51,9 +54,15 @@ __device__ __forceinline__ int scale_exponent(uint32_t m) {
 
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // e in [-126, 127]
 
-__device__ __forceinline__ uint32_t pack_e4m3(floatx2 a, floatx2 b) {
-    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a[0], a[1], 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(b[0], b[1], lo, true);
+// Four codes of values over a power of two, to nearest even; NaN, infinities and what would pass 464 give NaN (all finite bf16
+// values over powers of two from 2^-100 to 2^120 were compared with a product and a conversion).
+__device__ __forceinline__ uint32_t pack_e4m3(floatx2 a, floatx2 b, float scale) {
+    const shortx2 lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(shortx2{0, 0}, a[0], a[1], scale, false);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, b[0], b[1], scale, true));
+}
+__device__ __forceinline__ uint32_t pack_e4m3(uint32_t a, uint32_t b, float scale) {  // of bf16 pairs
+    const shortx2 lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(shortx2{0, 0}, __builtin_bit_cast(bf16x2, a), scale, false);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2, b), scale, true));
 }
 
 // Codes of `rows` positions, rounded again from the scale 2^was to 2^now.
@@ -67,7 +76,7 @@ __device__ __forceinline__ void round_again(uint8_t* codes, int rows, int was, i
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const floatx2 a = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], true);
-            w[i] = pack_e4m3(floatx2{a[0] * f, a[1] * f}, floatx2{b[0] * f, b[1] * f});
+            w[i] = pack_e4m3(floatx2{a[0] * f, a[1] * f}, floatx2{b[0] * f, b[1] * f}, 1.0f);
         }
         *p = w;
     }
@@ -78,22 +87,26 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 3 : 4) void append_kernel(P
     constexpr int kElems = 16 / ES, kPairs = kElems / 2;      // of a lane's vector
     constexpr int kLanes = D / kElems, kRows = 64 / kLanes;   // lanes of a row, rows of a load
     constexpr int kLoads = kScaleBlock / kRows;
-    __shared__ CosSin table[kScaleBlock * (D / 2)];  // [new row of the block][pair]
-    __shared__ int at[kScaleBlock][3];
+    __shared__ CosSin table[kScaleBlock * (D / 2)];  // by axis, run of new rows with one place on it, pair of its band
+    __shared__ double freq[D / 2];
+    __shared__ double place[3][kScaleBlock];         // of an axis' runs
+    __shared__ int4 row_at[kScaleBlock];             // where a row's angles of each axis begin
+    __shared__ int ends[3];                          // of the axes' entries
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const PagedSeqs& q = a.seqs;
     const unsigned block = row_block();
-    // the streams' new lengths
-    if (a.out_len) {
-        const int64_t stride = (int64_t)gridDim.x * gridDim.y * (64 * kWaves);
-        for (int64_t s = (int64_t)block * (64 * kWaves) + tid; s < q.B; s += stride) {
-            const int n = tokens_of(q, (int)s).y, held = held_of(q, (int)s);
-            a.out_len[s] = (int)min((int64_t)held + n, (int64_t)(q.max_pages << q.page_log2));
-        }
+    if (block >= blocks) {  // behind the pieces: the streams' new lengths
+        const int64_t s = (int64_t)(block - blocks) * (64 * kWaves) + tid;
+        if (a.out_len && s < q.B)
+            a.out_len[s] = (int)min((int64_t)held_of(q, (int)s) + tokens_of(q, (int)s).y, (int64_t)(q.max_pages << q.page_log2));
+        return;
     }
-    if (block >= blocks) return;  // grid padding (uniform)
+    // What the angles need is loaded before the rows, and all of it without branches around it, so that the waits are by
+    // count and the rows stay in flight.
+    const int P = a.n_t + a.n_y + a.n_x;
+    const double own_freq = f.quarter[min(tid, D / 2 - 1)];
     const int groups = (a.H + kWaves - 1) / kWaves;
     const int piece = (int)(block / (unsigned)groups);
     const int head = (int)(block - (unsigned)piece * (unsigned)groups) * kWaves + wave;
@@ -118,113 +131,193 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 3 : 4) void append_kernel(P
     const int start = held / kScaleBlock * kScaleBlock + it.in * kScaleBlock;
     const int lo = max(held - start, 0), hi = (int)min((int64_t)held + tok.y - start, (int64_t)kScaleBlock);  // its new rows
     const int page = page_of(q, it.s, start >> q.page_log2);
-    if (page < 0) return;  // nowhere to store them (uniform)
     const int row0 = start & ((1 << q.page_log2) - 1);
     const bool live = head < a.H;
+    const int head_in = min(head, a.H - 1);
 
     // row r of the block is token tok.x + start + r - held
     const int64_t first = (int64_t)tok.x + start - held;
+    int at[3] = {0, 0, 0};  // lane r of the first wave: the place of row r
+    const bool placed = tid < kScaleBlock && tid >= lo && tid < hi;
+    if (a.pos && placed) {
+#pragma unroll
+        for (int j = 0; j < 3; ++j) at[j] = a.pos[(first + tid) * 3 + j];
+    }
     const int r_lane = lane / kLanes, c_lane = lane % kLanes;
+    // the lane's row of load i; beside the new rows one of them, which changes no maximum and is not stored
+    auto row_in = [&](int i) -> int { return min(max(i * kRows + r_lane, lo), hi - 1); };
     u32x4 x[2][kLoads];
     auto load = [&](int which) {
-        const uint8_t* src = static_cast<const uint8_t*>(which ? a.v : a.k) + (size_t)head * D * ES + 16 * c_lane;
+        const uint8_t* src = static_cast<const uint8_t*>(which ? a.v : a.k) + (size_t)head_in * D * ES + 16 * c_lane;
         const int64_t row = which ? a.v_row_bytes : a.k_row_bytes;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int r = i * kRows + r_lane;
-            x[which][i] = u32x4{0, 0, 0, 0};
-            if (live && r >= lo && r < hi) x[which][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (first + r) * row));
+            x[which][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (first + row_in(i)) * row));
         }
     };
     load(0);
     if constexpr (ES == 2) load(1);
+    if (page < 0) return;  // nowhere to store them (uniform)
+    const size_t slot = ((size_t)page * a.H + head_in) << q.page_log2;  // first position of the head's page
+    uint8_t was[2] = {0, 0};  // the block's scales
+    if constexpr (kFp8) {
+        was[0] = a.scale_k[(slot + row0) / kScaleBlock];
+        was[1] = a.scale_v[(slot + row0) / kScaleBlock];
+    }
+    if (tid < P) freq[tid] = own_freq;
 
-    const int P = a.n_t + a.n_y + a.n_x;
-    if (tid < kScaleBlock && tid >= lo && tid < hi) {
-        if (a.pos) {
-#pragma unroll
-            for (int j = 0; j < 3; ++j) at[tid][j] = a.pos[(first + tid) * 3 + j];
-        } else {
-            const int c = start + tid, frame = c / a.hw, in = c - frame * a.hw, y = in / a.w;
-            at[tid][0] = frame;
-            at[tid][1] = y;
-            at[tid][2] = in - y * a.w;
+    // The rows of a piece share most of their places on two of the axes: an angle is computed once per run of rows with
+    // one place (32 tokens of a 30 x 52 grid: some 750 of 2048).
+    if (wave == 0) {
+        if (!a.pos) {
+            const int c = start + lane, frame = c / a.hw, in = c - frame * a.hw, y = in / a.w;
+            at[0] = frame;
+            at[1] = y;
+            at[2] = in - y * a.w;
         }
+        const int n[3] = {a.n_t, a.n_y, a.n_x};
+        int from[3], total = 0;
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            const int before = __shfl_up(at[j], 1);
+            const bool starts = placed && (lane == lo || at[j] != before);
+            const unsigned long long runs = __ballot(starts);
+            const int run = __popcll(runs & ((2ull << lane) - 1)) - 1;
+            if (starts) place[j][run] = (double)at[j] + (j == 0 && !a.pos ? (double)a.t0 : 0.0);
+            from[j] = total + run * n[j];
+            total += __popcll(runs) * n[j];
+            if (lane == 0) ends[j] = total;
+        }
+        if (placed) row_at[lane] = make_int4(from[0], from[1], from[2], 0);
     }
     __syncthreads();
-    const double t0 = a.pos ? 0.0 : (double)a.t0;
-    for (int e = tid; e < (hi - lo) * P; e += 64 * kWaves) {
-        const int r = (int)(((float)e + 0.5f) * a.inv_pairs);  // at most 2048 entries: exact
-        const int pair = e - r * P;
-        const int axis = pair < a.n_t ? 0 : (pair < a.n_t + a.n_y ? 1 : 2);
-        table[e] = quarter_turns(((double)at[lo + r][axis] + (axis == 0 ? t0 : 0.0)) * f.quarter[pair]);
+    {
+        const int e0 = ends[0], e1 = ends[1], e2 = ends[2];
+        for (int e = tid; e < e2; e += 64 * kWaves) {
+            const int axis = e < e0 ? 0 : (e < e1 ? 1 : 2);
+            const int i = e - (axis == 0 ? 0 : (axis == 1 ? e0 : e1)), n = axis == 0 ? a.n_t : (axis == 1 ? a.n_y : a.n_x);
+            const int run = (int)(((float)i + 0.5f) * (axis == 0 ? a.inv_pairs[0] : (axis == 1 ? a.inv_pairs[1] : a.inv_pairs[2])));  // at most 2048 entries: exact
+            table[e] = quarter_turns(place[axis][run] * freq[(axis > 0 ? a.n_t : 0) + (axis > 1 ? a.n_y : 0) + i - run * n]);
+        }
     }
     __syncthreads();
     if (!live) return;
+    // the lane's pairs: which axis each is of, and its place in that band
+    int axis_of[kPairs], in_band[kPairs];
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) {
+        const int pair = c_lane * kPairs + j;
+        axis_of[j] = pair < a.n_t ? 0 : (pair < a.n_t + a.n_y ? 1 : (pair < P ? 2 : 3));
+        in_band[j] = axis_of[j] == 3 ? 0 : pair - (axis_of[j] > 0 ? a.n_t : 0) - (axis_of[j] > 1 ? a.n_y : 0);
+    }
 
-    const size_t slot = ((size_t)page * a.H + head) << q.page_log2;  // first position of the head's page
+    // The lane's part of load i as pairs, turned to the row's position; pairs behind the last band as they are.
+    auto turned = [&](int i, floatx2 (&p)[kPairs]) __attribute__((always_inline)) {
+        const int4 angles = row_at[row_in(i)];
+        const u32x4 w = x[0][i];
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        if constexpr (ES == 4) {
-            if (which == 1) load(1);
+        for (int j = 0; j < kPairs; ++j) {
+            if constexpr (ES == 2) p[j] = floatx2{__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u)};
+            else p[j] = floatx2{__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1])};
+            const floatx2 t = turn(p[j], table[(axis_of[j] == 0 ? angles.x : (axis_of[j] == 1 ? angles.y : angles.z)) + in_band[j]]);
+            p[j] = axis_of[j] < 3 ? t : p[j];
         }
-        uint8_t* out = static_cast<uint8_t*>(which ? a.cache_v : a.cache_k) + (slot + row0) * (size_t)(D * (kFp8 ? 1 : ES));
-        floatx2 p[kFp8 ? kLoads : 1][kPairs];
-        uint32_t most = 0;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int r = i * kRows + r_lane;
-            const bool ok = r >= lo && r < hi;
-            const CosSin* cs = table + (ok ? r - lo : 0) * P;
-            floatx2* pi = p[kFp8 ? i : 0];
-            u32x4& w = x[which][i];
-#pragma unroll
-            for (int j = 0; j < kPairs; ++j) {
-                if constexpr (ES == 2) pi[j] = floatx2{__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u)};
-                else pi[j] = floatx2{__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1])};
-                const int pair = c_lane * kPairs + j;
-                const bool turned = which == 0 && pair < P;
-                if (turned && ok) pi[j] = turn(pi[j], cs[pair]);
-                if constexpr (kFp8) {
-                    most = max(most, max(finite_bits(pi[j][0]), finite_bits(pi[j][1])));
-                } else if (turned) {
-                    if constexpr (ES == 2) {
-                        w[j] = pack_bf16(pi[j]);
-                    } else {
-                        w[2 * j] = __float_as_uint(pi[j][0]);
-                        w[2 * j + 1] = __float_as_uint(pi[j][1]);
-                    }
-                }
-            }
-            if constexpr (!kFp8) {
-                if (ok) *reinterpret_cast<u32x4*>(out + r * (D * ES) + 16 * c_lane) = w;
-            }
-        }
-        if constexpr (kFp8) {
+    };
+    auto is_new = [&](int i) -> bool { return i * kRows + r_lane >= lo && i * kRows + r_lane < hi; };
+    constexpr int kOut = kFp8 ? D : D * ES;  // bytes of a stored row
+    const size_t to_lane = (slot + row0 + r_lane) * (size_t)kOut + (kOut / kLanes) * c_lane;
+    if constexpr (kFp8) {
+        // a block's codes from its largest value's bits: word(i, scale) is the lane's part of load i
+        auto store = [&](int which, uint32_t most, auto word) __attribute__((always_inline)) {
 #pragma unroll
             for (int off = 1; off < 64; off *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, off));
             int e = scale_exponent(most);
-            uint8_t* scale = (which ? a.scale_v : a.scale_k) + ((slot + row0) / kScaleBlock);
+            uint8_t* cache = static_cast<uint8_t*>(which ? a.cache_v : a.cache_k);
             if (lo > 0) {
-                const int was = min((int)*scale, kScaleHigh + 127) - 127;
-                if (e > was) round_again<D>(out, lo, was, e, lane);
-                e = max(e, was);
+                const int old = min((int)was[which], kScaleHigh + 127) - 127;
+                if (e > old) round_again<D>(cache + (slot + row0) * D, lo, old, e, lane);
+                e = max(e, old);
             }
-            const float inv = power_of_two(-e);
+            const float to = power_of_two(e);
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const int r = i * kRows + r_lane;
-                u32x2 w;
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const floatx2 u = p[i][2 * j], v = p[i][2 * j + 1];
-                    w[j] = pack_e4m3(floatx2{nan_if_not_finite(u[0] * inv), nan_if_not_finite(u[1] * inv)},
-                                     floatx2{nan_if_not_finite(v[0] * inv), nan_if_not_finite(v[1] * inv)});
-                }
-                if (r >= lo && r < hi) *reinterpret_cast<u32x2*>(out + r * D + 8 * c_lane) = w;
+                const u32x2 w = word(i, to);
+                if (is_new(i)) *reinterpret_cast<u32x2*>(cache + to_lane + i * (kRows * kOut)) = w;
             }
-            if (lane == 0) *scale = (uint8_t)(e + 127);
+            if (lane == 0) (which ? a.scale_v : a.scale_k)[(slot + row0) / kScaleBlock] = (uint8_t)(e + 127);
+        };
+        // Largest values: of keys by fp32, of values by the bits of two bf16 at a time. Where one is not finite (bf16 with an
+        // exponent of ones, or a turned pair past fp32), the others are looked at one by one.
+        {
+            floatx2 p[kLoads][kPairs];
+            float top = 0.0f;
+            ushortx2 bits = {0, 0};
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+#pragma unroll
+                for (int j = 0; j < kPairs; ++j) bits = __builtin_elementwise_max(bits, __builtin_bit_cast(ushortx2, x[0][i][j] & 0x7fff7fffu));
+                turned(i, p[i]);
+#pragma unroll
+                for (int j = 0; j < kPairs; ++j) top = fmaxf(top, fmaxf(fabsf(p[i][j][0]), fabsf(p[i][j][1])));
+                if (i & 1) __builtin_amdgcn_sched_barrier(0);  // the angles of two loads at a time
+            }
+            if (__any(max(bits[0], bits[1]) >= 0x7f80 || top == INFINITY)) {
+                uint32_t most = 0;
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                    for (int j = 0; j < kPairs; ++j)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            most = max(most, finite_bits(p[i][j][h]));
+                            __builtin_amdgcn_sched_barrier(0);  // one mask at a time
+                        }
+                top = __uint_as_float(most);
+            }
+            store(0, __float_as_uint(top), [&](int i, float to) -> u32x2 { return u32x2{pack_e4m3(p[i][0], p[i][1], to), pack_e4m3(p[i][2], p[i][3], to)}; });
         }
+        ushortx2 bits = {0, 0};
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) bits = __builtin_elementwise_max(bits, __builtin_bit_cast(ushortx2, x[1][i][j] & 0x7fff7fffu));
+        if (__any(max(bits[0], bits[1]) >= 0x7f80)) {
+            bits = ushortx2{0, 0};
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                for (int j = 0; j < kPairs; ++j) {
+                    const uint32_t bad = spread<kPagedBf16>(not_finite<kPagedBf16>(x[1][i][j]));
+                    bits = __builtin_elementwise_max(bits, __builtin_bit_cast(ushortx2, x[1][i][j] & ~bad & 0x7fff7fffu));
+                }
+        }
+        store(1, (uint32_t)max(bits[0], bits[1]) << 16, [&](int i, float to) -> u32x2 {
+            return u32x2{pack_e4m3(x[1][i][0], x[1][i][1], to), pack_e4m3(x[1][i][2], x[1][i][3], to)};
+        });
+    } else {
+        uint8_t* out = static_cast<uint8_t*>(a.cache_k) + to_lane;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            floatx2 p[kPairs];
+            turned(i, p);
+            u32x4 w = x[0][i];
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) {
+                if (axis_of[j] == 3) continue;  // copied
+                if constexpr (ES == 2) {
+                    w[j] = pack_bf16(p[j]);
+                } else {
+                    w[2 * j] = __float_as_uint(p[j][0]);
+                    w[2 * j + 1] = __float_as_uint(p[j][1]);
+                }
+            }
+            if (is_new(i)) *reinterpret_cast<u32x4*>(out + i * (kRows * kOut)) = w;
+        }
+        if constexpr (ES == 4) load(1);
+        out = static_cast<uint8_t*>(a.cache_v) + to_lane;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            if (is_new(i)) *reinterpret_cast<u32x4*>(out + i * (kRows * kOut)) = x[1][i];
     }
 }
 
@@ -244,8 +337,9 @@ int64_t paged_append_blocks(const PagedAppendArgs& a) {
 
 hipError_t launch_paged_append(const PagedAppendArgs& a, const PagedFreq& f, hipStream_t stream) {
     const unsigned blocks = (unsigned)paged_append_blocks(a);
-    if (blocks == 0 && !a.out_len) return hipSuccess;
-    const dim3 grid = blocks ? grid_rows(blocks) : dim3(1), block(64 * kWaves);
+    const unsigned lengths = a.out_len ? (unsigned)((a.seqs.B + 64 * kWaves - 1) / (64 * kWaves)) : 0;
+    if (blocks + lengths == 0) return hipSuccess;
+    const dim3 grid = grid_rows(blocks + lengths), block(64 * kWaves);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, f, blocks); };
     if (a.D == 128) {
         if (a.dtype == kPagedFp8) launch(append_kernel<128, 2, true>);
