@@ -64,8 +64,8 @@ def _stream(device: torch.device):
 
 
 def _need(t: torch.Tensor, name: str, dtype: torch.dtype, shape: Optional[Sequence[int]] = None, device=None):
-    if (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()
-            and (shape is None or t.shape == shape) and (device is None or t.device == device)):
+    if (isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_contiguous() and (shape is None or t.shape == shape)
+            and (t.is_cuda if device is None else t.get_device() == device.index)):  # -1 and None on the CPU
         return t
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
@@ -682,7 +682,7 @@ def append_paged_kv(k: torch.Tensor, v: torch.Tensor, cache_k: torch.Tensor, cac
     if pos is not None:
         _need(pos, "pos", torch.int32, (n, 3), dev)
     if out_len is None:
-        out_len = torch.empty((B,), dtype=torch.int32, device=dev)
+        out_len = kv_len.new_empty((B,))
     else:
         _need(out_len, "out_len", torch.int32, (B,), dev)
     nt, ny, nx = pairs
@@ -736,16 +736,18 @@ def paged_chunk_attention(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch
         _need(visible, "visible", torch.int32, (n,), dev)
     S = frames = 0
     if corr_uv is not None:
-        S = corr_uv.shape[0]
+        S = corr_uv.shape[0] if isinstance(corr_uv, torch.Tensor) and corr_uv.dim() else -1
         _need(corr_uv, "corr_uv", torch.float32, (S, n, 2), dev)
         _need(corr_idx, "corr_idx", torch.int32, (S, n), dev)
         _need(kv_frame_slot, "kv_frame_slot", torch.int32, None, dev)
         if kv_frame_slot.dim() != 2 or kv_frame_slot.shape[0] != B:
             raise ValueError(f"kv_frame_slot has shape {tuple(kv_frame_slot.shape)}, expected ({B}, frames)")
         frames = kv_frame_slot.shape[1]
+    elif corr_idx is not None or kv_frame_slot is not None:
+        raise ValueError("corr_idx and kv_frame_slot belong to corr_uv")
     if out is None:
-        o = torch.empty((n, Hq, D), dtype=idt, device=dev)
-        lse = torch.empty((Hq, n), dtype=torch.float32, device=dev) if return_lse else None
+        o = q.new_empty((n, Hq, D))
+        lse = q.new_empty((Hq, n), dtype=torch.float32) if return_lse else None
     else:
         o, lse = out
         _need(o, "o", idt, (n, Hq, D), dev)
@@ -761,7 +763,7 @@ def paged_chunk_attention(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch
             with torch.cuda.device(dev):
                 nbytes = paged_attention_workspace_size(*size)
         if nbytes:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+            workspace = q.new_empty(nbytes, dtype=torch.uint8)
     _call(dev.index, "paged_chunk_attention", q.data_ptr(), q_row, cache_k.data_ptr(), cache_v.data_ptr(), _ptr(scale_k), _ptr(scale_v),
           o.data_ptr(), _ptr(lse), dt, n, _ptr(cu), B, kv_len.data_ptr(), _ptr(visible), page_table.data_ptr(), n_pages, page, max_pages,
           Hq, Hk, D, h, w, _ptr(kv_frame_slot), frames, _ptr(corr_uv), _ptr(corr_idx), S, softmax_scale, lam, sigma, max_keys, key_parts,
