@@ -90,8 +90,10 @@ struct PagedBias {
 constexpr int kManyWaves = 8;   // of a workgroup where there are few
 constexpr int kCorrFrames = 16, kSlotFrames = 256;  // retrieved and key frames whose correspondences and slots are kept in LDS
 
+// Two waves per SIMD where the registers do for it (fp32 at D = 64, 1170 queries on 7020 keys: one 283 us, two 271; at D = 128
+// two would need each tile's keys and values loaded when their turn comes, 544 us with one and 561 with two so).
 template <int D, int T, int NQ, bool kBias, int kW>
-__global__ __launch_bounds__(64 * kW, kW > 4 || (NQ == 1 && (T != kPagedF32 || D == 64)) ? 2 : 1) void paged_wave_kernel(PagedAttentionArgs a, float c_log2) {
+__global__ __launch_bounds__(64 * kW, kW > 4 || (T == kPagedF32 ? D == 64 : NQ == 1) ? 2 : 1) void paged_wave_kernel(PagedAttentionArgs a, float c_log2) {
     using Sh = Shape<D, T>;
     constexpr int kRows = 16 * NQ;
     constexpr int kDb = Sh::kDb;
@@ -102,7 +104,7 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (NQ == 1 && (T != kPagedF32 || D
     // The next tile's keys leave behind this one's logits, its values behind this one's product, where the registers hold both
     // beside each other (1170 fp32 queries on 7020 keys 606 us without, 567 with).
     constexpr bool kAhead = !kF32 || NQ == 2 || D == 64 || kW == 4;
-    __shared__ float lds_o[kW][NQ * kDb * 64 * 4];
+    __shared__ float lds_o[kW][kDb * 64 * 4];  // of one block of 16 rows
     __shared__ float lds_m[kW][kRows], lds_l[kW][kRows];
     __shared__ int lds_token[kRows], lds_head[kRows];
     __shared__ floatx4 lds_q[kF32 ? NQ * D / 16 : 1][64];  // fp32 queries: the lane's vector of four steps
@@ -566,12 +568,15 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (NQ == 1 && (T != kPagedF32 || D
                 lds_head[16 * nq + m] = head[nq];
             }
         }
-#pragma unroll
-        for (int db = 0; db < kDb; ++db) *reinterpret_cast<floatx4*>(&lds_o[wave][((nq * kDb + db) * 64 + lane) * 4]) = O[nq][db];
     }
-    __syncthreads();
-    for (int e = threadIdx.x; e < NQ * 256; e += 64 * kW) {
-        const int nq = e >> 8, l = (e >> 2) & 63, i = e & 3, col = 16 * nq + (l & 15);
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+        if (nq > 0) __syncthreads();  // the block before has been read
+#pragma unroll
+        for (int db = 0; db < kDb; ++db) *reinterpret_cast<floatx4*>(&lds_o[wave][(db * 64 + lane) * 4]) = O[nq][db];
+        __syncthreads();
+        if (threadIdx.x >= 256) continue;
+        const int l = threadIdx.x >> 2, i = threadIdx.x & 3, col = 16 * nq + (l & 15);
         const int to = lds_token[col];
         float M = -FLT_MAX, L = 0.0f;
 #pragma unroll
@@ -584,7 +589,7 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (NQ == 1 && (T != kPagedF32 || D
             const float c = __builtin_amdgcn_exp2f(lds_m[w][col] - M);
             L = fmaf(c, lds_l[w][col], L);
 #pragma unroll
-            for (int db = 0; db < kDb; ++db) x[db] = fmaf(c, lds_o[w][((nq * kDb + db) * 64 + l) * 4 + i], x[db]);
+            for (int db = 0; db < kDb; ++db) x[db] = fmaf(c, lds_o[w][(db * 64 + l) * 4 + i], x[db]);
         }
         // its head dims: blocks 4 b .. 4 b + 3 from first[b] on
         auto first = [&](int b) -> int { return kVHalves == 2 ? 64 * b + 4 * (4 * (l >> 4) + i) : kDb * (4 * (l >> 4) + i) + 4 * b; };

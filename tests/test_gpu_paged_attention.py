@@ -315,3 +315,14 @@ def test_bias_of_many_frames(dtype, m):
     largest = 1.3 * ((h * h + w * w) / 4 + (off_centre ** 2).sum(-1).max()) / (2 * 2.0 ** 2)
     o, lse = _attend(pool, q, kv_frame_slot=_i32(slots), corr_uv=uv, corr_idx=idx, h=h, w=w, lam=1.3, sigma=2.0)
     check_attention(pool, q, o, lse, bias=bias, slack=0.0 if dtype == F32 else 8 * 2.0 ** -24 * largest)
+
+
+def test_bias_arguments_belong_together():
+    """Slots or codes without correspondences would be a bias that is silently off."""
+    pool = Pool(29, BF16, [64], 2, 64, 32)
+    q = values(gen(30), BF16, 4, 2, 64)
+    uv, idx, slot = torch.zeros(1, 4, 2, device=DEV), torch.zeros(1, 4, dtype=torch.int32, device=DEV), _i32([[0, 0]])
+    for err, kw in [(ValueError, dict(kv_frame_slot=slot)), (ValueError, dict(corr_idx=idx)), (TypeError, dict(corr_uv=uv)),
+                    (TypeError, dict(corr_uv=uv, corr_idx=idx)), (TypeError, dict(corr_uv=[0.0], corr_idx=idx, kv_frame_slot=slot))]:
+        with pytest.raises(err):
+            _attend(pool, q, h=4, w=8, lam=1.0, **kw)
