@@ -669,7 +669,8 @@ def append_paged_kv(k: torch.Tensor, v: torch.Tensor, cache_k: torch.Tensor, cac
     each); they go to its positions kv_len[s] on. Keys get the rotary position of
     rotary_embed (pairs, theta): position c stands at (t0 + c // (h*w), c // w % h,
     c % w), or a token at pos[i] with pos [n, 3] i32. Returns the new lengths [B]
-    i32 (out_len, which must not be kv_len)."""
+    i32 (out_len, which must not be kv_len). No output may overlap an input; no
+    autograd graph is recorded."""
     if not isinstance(k, torch.Tensor) or k.dim() != 3:
         raise ValueError("k must be a tensor [n, heads, D]")
     n = k.shape[0]
@@ -723,7 +724,9 @@ def paged_chunk_attention(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch
     corr_uv [S, n, 2] f32 and corr_idx [S, n] i32 are given: kv_frame_slot [B, frames]
     i32, position j of a stream being token j % (h*w) of its frame j // (h*w).
     max_keys: the longest stream's length if it is known, for the choice of the key
-    split only. Returns (o [n, Hq, D], lse [Hq, n] f32 or None)."""
+    split only. Returns (o [n, Hq, D], lse [Hq, n] f32 or None); rows behind the last
+    stream's tokens are not written. Outputs must not overlap inputs; no autograd
+    graph is recorded."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor [n, heads, D]")
     n, _, D = q.shape
