@@ -16,10 +16,10 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "librevisit.so")
 SOURCES = ["capi.cpp", "retrieve.hip", "reproject.hip", "attention.hip", "kvpack.hip", "stream.cpp", "stream_kernels.hip",
-           "rotary.hip", "keyweight.hip", "select.hip", "compact.hip", "paged_append.hip", "paged_attention.hip"]
+           "rotary.hip", "keyweight.hip", "select.hip", "compact.hip", "paged_append.hip"]
 # compiled with the matrix instructions accumulating in the registers that vector instructions read: a kernel of more
 # than 256 registers otherwise gets the others, and a move for each element that it reads
-WIDE_SOURCES = ["paged_tile.hip"]
+WIDE_SOURCES = ["paged_attention.hip", "paged_tile.hip"]
 WIDE_FLAGS = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
 ARCH = "gfx950"
 

@@ -91,7 +91,9 @@ constexpr int kManyWaves = 8;   // of a workgroup where there are few
 constexpr int kCorrFrames = 16, kSlotFrames = 256;  // retrieved and key frames whose correspondences and slots are kept in LDS
 
 // Two waves per SIMD where the registers do for it (fp32 at D = 64, 1170 queries on 7020 keys: one 283 us, two 271; at D = 128
-// two would need each tile's keys and values loaded when their turn comes, 544 us with one and 561 with two so).
+// two would need each tile's keys and values loaded when their turn comes, 544 us with one and 561 with two so). The MFMAs
+// accumulate in the registers that vector instructions read (-amdgpu-mfma-vgpr-form, set for this file): 1170 biased fp32
+// queries at D = 128 543 us without, 514 with. Loads put between the products by hand instead of by the compiler: 528.
 template <int D, int T, int NQ, bool kBias, int kW>
 __global__ __launch_bounds__(64 * kW, kW > 4 || (T == kPagedF32 ? D == 64 : NQ == 1) ? 2 : 1) void paged_wave_kernel(PagedAttentionArgs a, float c_log2) {
     using Sh = Shape<D, T>;
@@ -102,7 +104,7 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (T == kPagedF32 ? D == 64 : NQ =
     // one, 2^-9, made outputs of a few heavy keys 1.6 times as far off as their own rounding does)
     constexpr bool kFine = !kF32 && NQ == 1;
     // The next tile's keys leave behind this one's logits, its values behind this one's product, where the registers hold both
-    // beside each other (1170 fp32 queries on 7020 keys 606 us without, 567 with).
+    // beside each other (1170 fp32 queries on 7020 keys, when it was taken: 606 us without, 567 with).
     constexpr bool kAhead = !kF32 || NQ == 2 || D == 64 || kW == 4;
     __shared__ float lds_o[kW][kDb * 64 * 4];  // of one block of 16 rows
     __shared__ float lds_m[kW][kRows], lds_l[kW][kRows];
@@ -712,12 +714,12 @@ size_t paged_plan(PagedAttentionArgs& a, int32_t key_parts, int32_t max_keys, in
         // at a time for the tile kernel at D = 64), a time per 32-key step that was measured at each size of tile, 4 us for
         // a workgroup's start and end, and a merge (a launch, and the parts' results written and read). 12 heads of 8
         // bits on 20000 keys: 100 queries 401 us whole, 43 in 16 parts; 400 queries 551 whole, 89 in 9; 4680 queries on 28080
-        // keys 878 whole, 911 in two. fp32: 200 queries on 4000 keys 155 us whole, 65 in 3; 800 305 and, in 4, 221;
-        // 1170 on 7020 583 whole, 628 in two. 264 single rows on 30000 keys: 503 us whole, 375 in 4.
+        // keys 878 whole, 911 in two. fp32: 200 queries on 4000 keys 141 us whole, 63 in 3; 800 284 and, in 4, 216;
+        // 1170 on 7020 484 whole, 513 in two. 264 single rows on 30000 keys: 503 us whole, 375 in 4.
         const int64_t places = a.rows == 128 && a.D == 64 ? 2 * (int64_t)cus : cus;
         const double step = a.rows == 256 ? 0.9
                             : a.rows == 128 ? (a.D == 128 ? 0.65 : 0.72)
-                            : a.rows == 32  ? (a.dtype == kPagedF32 ? 1.25 : 0.32)
+                            : a.rows == 32  ? (a.dtype == kPagedF32 ? 1.1 : 0.32)
                                             : (a.dtype == kPagedF32 ? 0.6 : 0.27);
         const int64_t most_parts = std::min<int64_t>(kPagedMaxParts, a.rows >= 128 ? key_tiles : key_tiles / 16);
         double best = INFINITY;

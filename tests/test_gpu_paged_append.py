@@ -234,3 +234,39 @@ def test_refusals():
     ]:
         with pytest.raises(err):
             rv.append_paged_kv(*args, **kw)
+
+
+@pytest.mark.parametrize("dtype", [FP8, BF16, F32])
+@pytest.mark.parametrize("pairs", [(0, 0, 0), (64, 0, 0), (0, 64, 0), (0, 0, 64), (0, 1, 2), (63, 0, 1), (31, 33, 0)])
+def test_places_in_runs(dtype, pairs):
+    """Bands of any size, at places that repeat on one axis or another, in order or not, far from zero and below it."""
+    H, D, page, before, n = 3, 128, 64, [20, 3], 2 * 50
+    rng = np.random.default_rng(30)
+    pos = np.stack([np.repeat(rng.integers(-2**30, 2**30, 10), 10), np.tile([4, 4, 4, -7], 25), rng.permutation(n)], 1).astype(np.int32)
+    pos[60:] = pos[60]  # all alike
+    k, v = (values(gen(31 + i), GIVEN[dtype], n, H, D) for i in range(2))
+    _run(Pool(32, dtype, [b + 50 for b in before], H, D, page), k, v, None, before, pairs, pos=pos)
+    _run(Pool(33, dtype, [b + 50 for b in before], H, D, page), k, v, None, before, pairs, h=1, w=1, t0=-5)
+
+
+def test_turned_pairs_past_fp32():
+    """A pair of finite values whose turn leaves fp32 is stored as NaN, and its block's scale comes from the others."""
+    H, D, page = 1, 64, 32
+    pool = Pool(34, FP8, [32], H, D, page)
+    k = torch.ones(32, H, D, dtype=BF16, device=DEV)
+    k[7, 0, 2:4] = torch.tensor([3.3e38, 3.3e38])
+    pos = torch.zeros(32, 3, dtype=torch.int32, device=DEV)
+    pos[7, 0] = 1  # theta^(-1/2) = pi / 4 for pair 1
+    rv.append_paged_kv(k, torch.ones_like(k), pool.k, pool.v, torch.from_numpy(pool.table).to(DEV), torch.zeros(1, dtype=torch.int32, device=DEV),
+                       pairs=(2, 0, 0), theta=(4 / np.pi) ** 2, pos=pos, **pool.kw())
+    page0 = int(pool.table[0, 0])
+    got = pool.k[page0, 0].float()
+    # x cos - y sin is far below y's own rounding or not, x sin + y cos = 4.7e38 in any case
+    assert bool(torch.isnan(got[7, 3]))
+    small = float(3.3e38 * 2.0 ** -7)  # what a rounded pi / 4 may leave of the difference
+    e = int(pool.scales[0].view(torch.uint8)[page0, 0, 0]) - 127
+    assert 2.0 ** e * 448 < small
+    rest = torch.ones(32, D, dtype=torch.bool, device=DEV)
+    rest[7, :4] = False
+    back = got * 2.0 ** e
+    assert bool((back[rest] <= 1).all()) and bool(torch.isfinite(back[rest]).all())
