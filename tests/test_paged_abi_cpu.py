@@ -62,7 +62,7 @@ def test_append_nothing_to_do(L):
 
 
 def _attend(L, **kw):
-    a = dict(q=at(1), q_row=3072 // 2, ck=at(4), cv=at(8), sk=at(12), sv=at(13), o=at(2), lse=at(2, 1 << 20), dtype=4, n=10, cu=NULL, B=2, len=at(3),
+    a = dict(q=at(1), q_row=1536, ck=at(4), cv=at(8), sk=at(12), sv=at(13), o=at(2), lse=at(2, 1 << 20), dtype=4, n=10, cu=NULL, B=2, len=at(3),
              vis=NULL, table=at(14), pages=100, page=64, most=40, Hq=12, Hk=12, D=128, h=30, w=52, slot=at(15), frames=2, uv=at(16), idx=at(17),
              S=2, scale=1 / math.sqrt(128), lam=1.0, sigma=2.0, max_keys=0, parts=1, ws=NULL, ws_bytes=0)
     a.update(kw)
