@@ -623,13 +623,15 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (T == kPagedF32 ? D == 64 : NQ =
 }
 
 // O = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p over the key parts of a tile's row: a part without keys has m = -inf
-// and is not read. A workgroup takes kRowsPer rows, 256 / kRowsPer threads each: D / 4 of them hold a part's head dims,
-// and as many parts are read at once as there are such groups; their sums meet in LDS.
+// and nothing else that counts. A workgroup takes kRowsPer rows, 256 / kRowsPer threads each: D / 4 of them hold a part's
+// head dims, and as many parts are read at once as there are such groups; their maxima and sums meet in LDS. Bound by
+// latency: four parts of a group are loaded at a time, maxima with the rest (12 rows of 8 and of 21 parts: 4.1 us; the maxima
+// first and each part when its own is there: 5.1).
 template <int D, bool kF32, int kRowsPer>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttentionArgs a, unsigned blocks) {
     constexpr int kLanes = D / 4, kThreads = 256 / kRowsPer, kGroups = kThreads / kLanes;
     __shared__ floatx4 lds_x[kGroups > 1 ? 256 : 1];
-    __shared__ float lds_l[kGroups > 1 ? 256 / kLanes : 1];
+    __shared__ float lds_l[kGroups > 1 ? 256 / kLanes : 1], lds_m[kGroups > 1 ? 256 / kLanes : 1];
     const unsigned block = row_block();
     if (block >= blocks) return;
     const unsigned per = (unsigned)(a.rows / kRowsPer);
@@ -650,30 +652,54 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttentionArgs a, 
     const float* stat = a.partial + (size_t)item * a.parts * step + a.rows * D + r;
     float M = -INFINITY, L = 0.0f;
     floatx4 x = floatx4{0, 0, 0, 0};
+    auto add = [&](float to, float m, float l, floatx4 v) {  // of a sum's maximum m; to >= m
+        if (m == -INFINITY) return;
+        const float c = __builtin_amdgcn_exp2f(m - to);
+        L = fmaf(c, l, L);
+        x += c * v;
+    };
     if (ok) {
-#pragma unroll 8
-        for (int p = 0; p < a.parts; ++p) M = fmaxf(M, stat[p * step]);
-#pragma unroll 4
-        for (int p = g; p < a.parts; p += kGroups) {
-            const float mp = stat[p * step], lp = stat[p * step + a.rows];
-            if (mp == -INFINITY) continue;
-            const float c = __builtin_amdgcn_exp2f(mp - M);
-            L = fmaf(c, lp, L);
-            x += c * *reinterpret_cast<const floatx4*>(base + p * step);
+        constexpr int kBatch = 4;
+        for (int p = g; p < a.parts; p += kBatch * kGroups) {
+            float m[kBatch], l[kBatch], top = M;
+            floatx4 v[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int at = min(p + i * kGroups, a.parts - 1);
+                m[i] = stat[at * step];
+                l[i] = stat[at * step + a.rows];
+                v[i] = *reinterpret_cast<const floatx4*>(base + at * step);
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                if (p + i * kGroups >= a.parts) m[i] = -INFINITY;
+                top = fmaxf(top, m[i]);
+            }
+            const float l_old = L;
+            const floatx4 x_old = x;
+            L = 0.0f;
+            x = floatx4{0, 0, 0, 0};
+            add(top, M, l_old, x_old);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) add(top, m[i], l[i], v[i]);
+            M = top;
         }
     }
     if constexpr (kGroups > 1) {
         lds_x[threadIdx.x] = x;
-        if (d == 0) lds_l[threadIdx.x / kLanes] = L;
+        if (d == 0) {
+            lds_l[threadIdx.x / kLanes] = L;
+            lds_m[threadIdx.x / kLanes] = M;
+        }
         __syncthreads();
         if (g != 0) return;
-        const int t0 = (int)threadIdx.x;
-        L = lds_l[t0 / kLanes];
+        const int t0 = (int)threadIdx.x, g0 = t0 / kLanes;
 #pragma unroll
-        for (int i = 1; i < kGroups; ++i) {
-            x += lds_x[t0 + i * kLanes];
-            L += lds_l[t0 / kLanes + i];
-        }
+        for (int i = 0; i < kGroups; ++i) M = fmaxf(M, lds_m[g0 + i]);
+        L = 0.0f;
+        x = floatx4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) add(M, lds_m[g0 + i], lds_l[g0 + i], lds_x[t0 + i * kLanes]);
     }
     if (!ok) return;
     x *= L == 0.0f ? 0.0f : 1.0f / L;
