@@ -732,8 +732,8 @@ size_t paged_plan(PagedAttentionArgs& a, int32_t key_parts, int32_t max_keys, in
     a.many = a.rows == 16 && units < cus;
     int64_t parts = key_parts;
     if (parts == 0 && a.many) {
-        // One workgroup per compute unit, four key tiles a part (a token, 12 heads of 8 bits: 1560 keys whole 14.4 us, in 8
-        // parts 10.2; 12000 71.5 and 16.6), but a range as short as a launch takes whole (300 keys 7.6 us, in two 9.7).
+        // One workgroup per compute unit, four key tiles a part (a token, 12 heads of 8 bits: 1560 keys whole 14.5 us, in 12
+        // parts 9.7; 12000 71.3 and, in 21, 13.5), but a range as short as a launch takes whole (300 keys 7.6 us, in two 8.9).
         parts = key_tiles <= (a.dtype == kPagedF32 ? 8 : 16) ? 1 : std::min<int64_t>(cus / units, key_tiles / 4);
     } else if (parts == 0) {
         // The number of parts with the least estimated time: the busiest compute unit's workgroups, one after the other (two
