@@ -627,7 +627,17 @@ int compact_kv(const void* src_k, const void* src_v, int32_t src_rows,
  *                 positions of a block share one scale per head, 2^(byte - 127); a
  *                 stored value is its code times that, a bf16 value exactly. Byte 0
  *                 counts as 1, and 255 is NaN.
+ *
+ * append_paged_kv_strided and paged_chunk_attention_strided take pools that lie otherwise
+ * (positions before heads, keys and values in one tensor, ...): their layout
+ * says how far apart pages, heads and positions are. The D elements of a position lie
+ * together. NULL is the layout above, and so is one that says the same. Where
+ * memory may not overlap, a strided cache counts as all from its first to its last byte.
  */
+typedef struct rc_pool_layout {
+    int64_t k[3], v[3];             /* elements from page to page, head to head, position to position; multiples of 16 bytes */
+    int64_t scale_k[3], scale_v[3]; /* bytes from page to page, head to head, block of 32 positions to block */
+} rc_pool_layout;
 
 /*
  * append_paged_kv -- new keys and values into the pages.
@@ -657,7 +667,10 @@ int compact_kv(const void* src_k, const void* src_v, int32_t src_rows,
  *                 keys are copied
  *
  * No output (caches, scales, out_len) may overlap an input or another output
- * (REVISIT_ERR_SHAPE). Rows of the pages that no token goes to are left as they are, but for
+ * (REVISIT_ERR_SHAPE); but caches and scales may have their pages, heads or positions
+ * between each other's where their layouts are alike from the outermost distance on.
+ * A layout is refused in which a distance is less than what lies within it
+ * spans. Rows of the pages that no token goes to are left as they are, but for
  * the codes of a block whose scale grows. B == 0, and n_tokens == 0 without out_len, is
  * valid (nothing to do). Two calls that may overlap in time must not write the
  * same 32 positions.
@@ -668,6 +681,14 @@ int append_paged_kv(const void* k, int64_t k_row, const void* v, int64_t v_row, 
                     const int32_t* page_table, int32_t n_pages, int32_t page, int32_t max_pages,
                     int32_t H, int32_t D, const int32_t* pos, int32_t t0, int32_t h, int32_t w,
                     int32_t pairs_t, int32_t pairs_y, int32_t pairs_x, float theta, hipStream_t stream);
+
+int append_paged_kv_strided(const void* k, int64_t k_row, const void* v, int64_t v_row, int32_t dtype, int32_t n_tokens,
+                            const int32_t* cu_tokens, int32_t B, const int32_t* kv_len, int32_t* out_len,
+                            void* cache_k, void* cache_v, uint8_t* scale_k, uint8_t* scale_v,
+                            const int32_t* page_table, int32_t n_pages, int32_t page, int32_t max_pages,
+                            int32_t H, int32_t D, const int32_t* pos, int32_t t0, int32_t h, int32_t w,
+                            int32_t pairs_t, int32_t pairs_y, int32_t pairs_x, float theta,
+                            const rc_pool_layout* layout, hipStream_t stream);
 
 /*
  * paged_chunk_attention -- biased_chunk_attention over the pages, for the queries
@@ -720,6 +741,17 @@ int paged_chunk_attention(const void* q, int64_t q_row, const void* cache_k, con
                           const float* corr_uv, const int32_t* corr_idx, int32_t S,
                           float softmax_scale, float lambda, float sigma,
                           int32_t max_keys, int32_t key_parts, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+int paged_chunk_attention_strided(const void* q, int64_t q_row, const void* cache_k, const void* cache_v,
+                                  const uint8_t* scale_k, const uint8_t* scale_v, void* o, float* lse, int32_t dtype,
+                                  int32_t n_tokens, const int32_t* cu_tokens, int32_t B, const int32_t* kv_len, const int32_t* visible,
+                                  const int32_t* page_table, int32_t n_pages, int32_t page, int32_t max_pages,
+                                  int32_t Hq, int32_t Hk, int32_t D, int32_t h, int32_t w,
+                                  const int32_t* kv_frame_slot, int32_t max_frames,
+                                  const float* corr_uv, const int32_t* corr_idx, int32_t S,
+                                  float softmax_scale, float lambda, float sigma,
+                                  int32_t max_keys, int32_t key_parts, void* workspace, size_t workspace_bytes,
+                                  const rc_pool_layout* layout, hipStream_t stream);
 
 int rc_paged_attention_workspace_size(int32_t dtype, int32_t n_tokens, int32_t ragged, int32_t B, int32_t Hq, int32_t Hk, int32_t D,
                                       int32_t page, int32_t max_pages, int32_t max_keys, int32_t key_parts, size_t* bytes);

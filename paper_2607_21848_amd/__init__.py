@@ -67,6 +67,11 @@ def _need(t: torch.Tensor, name: str, dtype: torch.dtype, shape: Optional[Sequen
     if (isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_contiguous() and (shape is None or t.shape == shape)
             and (t.is_cuda if device is None else t.get_device() == device.index)):  # -1 and None on the CPU
         return t
+    return _unfit(t, name, dtype, shape, device)
+
+
+def _unfit(t, name: str, dtype: torch.dtype, shape=None, device=None, contiguous: bool = True):
+    """What is wrong with a tensor; the tensor where nothing is."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.device.type != "cuda":
@@ -75,7 +80,7 @@ def _need(t: torch.Tensor, name: str, dtype: torch.dtype, shape: Optional[Sequen
         raise ValueError(f"{name} is on {t.device}, expected {device}")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
-    if not t.is_contiguous():
+    if contiguous and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     if shape is not None and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
@@ -387,7 +392,7 @@ def _call(index: int, name: str, *args):
         with torch.cuda.device(index):
             st = getattr(lib(), name)(*args, _raw_stream(index))
     if st:
-        _lib.check(name, st)
+        _lib.check(name.removesuffix("_strided"), st)
 
 
 def _rows(t: torch.Tensor, name: str, dtype: torch.dtype, n: int, D: int, index: int):
@@ -625,8 +630,20 @@ def compact_kv(src_k: torch.Tensor, src_v: torch.Tensor, sel: torch.Tensor, dst_
 _PAGED_DTYPES = {torch.bfloat16: (BF16, torch.bfloat16), torch.float32: (F32, torch.float32), torch.float8_e4m3fn: (FP8_KV, torch.bfloat16)}
 
 
+def _pool(t, name, dtype, shape, dev):
+    """Checks a pool of pages (or its scales), whose pages, heads and positions may be any distances apart; whether they lie
+    one behind the other."""
+    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.shape == shape and t.get_device() == dev.index):
+        _unfit(t, name, dtype, shape, dev, contiguous=False)
+    if t.is_contiguous():
+        return True
+    if len(shape) == 4 and t.stride(3) != 1:
+        raise ValueError(f"{name}: a position's elements must be contiguous (strides {t.stride()})")
+    return False
+
+
 def _pages(cache_k, cache_v, scale_k, scale_v, page_table, kv_len, cu, n, dev):
-    """Checks a paged cache's tensors; (type, type of q, k, v and o, n_pages, H, page, D, B, max_pages)."""
+    """Checks a paged cache's tensors; (type, type of q, k, v and o, n_pages, H, page, D, B, max_pages, layout or None)."""
     if not isinstance(cache_k, torch.Tensor) or cache_k.dim() != 4:
         raise ValueError("cache_k must be a tensor [pages, heads, page, D]")
     dt, idt = _PAGED_DTYPES.get(cache_k.dtype, (None, None))
@@ -634,12 +651,13 @@ def _pages(cache_k, cache_v, scale_k, scale_v, page_table, kv_len, cu, n, dev):
         raise TypeError(f"cache_k must be bfloat16, float32 or float8_e4m3fn (got {cache_k.dtype})")
     if not cache_k.is_cuda:
         raise ValueError(f"cache_k must be a GPU tensor (got {cache_k.device}); there is no CPU path")
-    n_pages, H, page, D = cache_k.shape
-    _need(cache_k, "cache_k", cache_k.dtype, None, dev)
-    _need(cache_v, "cache_v", cache_k.dtype, (n_pages, H, page, D), dev)
+    n_pages, H, page, D = shape = cache_k.shape
+    whole = _pool(cache_k, "cache_k", cache_k.dtype, shape, dev)
+    whole = _pool(cache_v, "cache_v", cache_k.dtype, shape, dev) and whole
     if dt == FP8_KV:
-        _need(scale_k, "scale_k", torch.float8_e8m0fnu, (n_pages, H, page // 32), dev)
-        _need(scale_v, "scale_v", torch.float8_e8m0fnu, (n_pages, H, page // 32), dev)
+        shape = (n_pages, H, page // 32)
+        whole = _pool(scale_k, "scale_k", torch.float8_e8m0fnu, shape, dev) and whole
+        whole = _pool(scale_v, "scale_v", torch.float8_e8m0fnu, shape, dev) and whole
     elif scale_k is not None or scale_v is not None:
         raise ValueError("scale_k and scale_v belong to float8_e4m3fn pages")
     _need(page_table, "page_table", torch.int32, None, dev)
@@ -651,7 +669,10 @@ def _pages(cache_k, cache_v, scale_k, scale_v, page_table, kv_len, cu, n, dev):
         _need(cu, "cu", torch.int32, (B + 1,), dev)
     elif n % B if B else n:
         raise ValueError(f"{n} tokens are not shared evenly by {B} streams: give cu")
-    return dt, idt, n_pages, H, page, D, B, max_pages
+    layout = None
+    if not whole:
+        layout = _lib.PoolLayout(*cache_k.stride()[:3], *cache_v.stride()[:3], *(scale_k.stride() + scale_v.stride() if dt == FP8_KV else ()))
+    return dt, idt, n_pages, H, page, D, B, max_pages, layout
 
 
 def append_paged_kv(k: torch.Tensor, v: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tensor, page_table: torch.Tensor,
@@ -663,8 +684,10 @@ def append_paged_kv(k: torch.Tensor, v: torch.Tensor, cache_k: torch.Tensor, cac
     k, v [n, H, D] (rows may lie apart, as views of a packed projection do); cache_k,
     cache_v [pages, H, page, D] in the type of k and v (bf16, fp32), or
     float8_e4m3fn for bf16 k and v, with scale_k, scale_v [pages, H, page // 32]
-    float8_e8m0fnu: a power of two for each 32 positions of a head. page_table
-    [B, pages of a stream] i32, kv_len [B] i32 the positions that the streams hold.
+    float8_e8m0fnu: a power of two for each 32 positions of a head. Pools and
+    scales may be views (of [pages, page, H, D], of one tensor for keys and values):
+    a position's D elements lie together, rows start on 16 bytes, and no two
+    positions share memory. page_table [B, pages of a stream] i32, kv_len [B] i32 the positions that the streams hold.
     Stream s has tokens cu[s] .. cu[s+1]-1 of the n (cu [B+1] i32; None: n // B
     each); they go to its positions kv_len[s] on. Keys get the rotary position of
     rotary_embed (pairs, theta): position c stands at (t0 + c // (h*w), c // w % h,
@@ -675,7 +698,7 @@ def append_paged_kv(k: torch.Tensor, v: torch.Tensor, cache_k: torch.Tensor, cac
         raise ValueError("k must be a tensor [n, heads, D]")
     n = k.shape[0]
     dev = k.device
-    dt, idt, n_pages, H, page, D, B, max_pages = _pages(cache_k, cache_v, scale_k, scale_v, page_table, kv_len, cu, n, dev)
+    dt, idt, n_pages, H, page, D, B, max_pages, layout = _pages(cache_k, cache_v, scale_k, scale_v, page_table, kv_len, cu, n, dev)
     Hk, k_row = _rows(k, "k", idt, n, D, dev.index)
     Hv, v_row = _rows(v, "v", idt, n, D, dev.index)
     if Hk != H or Hv != H:
@@ -687,9 +710,9 @@ def append_paged_kv(k: torch.Tensor, v: torch.Tensor, cache_k: torch.Tensor, cac
     else:
         _need(out_len, "out_len", torch.int32, (B,), dev)
     nt, ny, nx = pairs
-    _call(dev.index, "append_paged_kv", k.data_ptr(), k_row, v.data_ptr(), v_row, dt, n, _ptr(cu), B, kv_len.data_ptr(), out_len.data_ptr(),
-          cache_k.data_ptr(), cache_v.data_ptr(), _ptr(scale_k), _ptr(scale_v), page_table.data_ptr(), n_pages, page, max_pages, H, D,
-          _ptr(pos), t0, h, w, nt, ny, nx, theta)
+    _call(dev.index, "append_paged_kv_strided", k.data_ptr(), k_row, v.data_ptr(), v_row, dt, n, _ptr(cu), B, kv_len.data_ptr(),
+          out_len.data_ptr(), cache_k.data_ptr(), cache_v.data_ptr(), _ptr(scale_k), _ptr(scale_v), page_table.data_ptr(), n_pages, page,
+          max_pages, H, D, _ptr(pos), t0, h, w, nt, ny, nx, theta, layout)
     return out_len
 
 
@@ -731,7 +754,7 @@ def paged_chunk_attention(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch
         raise ValueError("q must be a tensor [n, heads, D]")
     n, _, D = q.shape
     dev = q.device
-    dt, idt, n_pages, Hk, page, Dk, B, max_pages = _pages(cache_k, cache_v, scale_k, scale_v, page_table, kv_len, cu, n, dev)
+    dt, idt, n_pages, Hk, page, Dk, B, max_pages, layout = _pages(cache_k, cache_v, scale_k, scale_v, page_table, kv_len, cu, n, dev)
     Hq, q_row = _rows(q, "q", idt, n, Dk, dev.index)
     if Hq % Hk:
         raise ValueError(f"{Hq} query heads are not a multiple of {Hk} key heads")
@@ -767,10 +790,10 @@ def paged_chunk_attention(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch
                 nbytes = paged_attention_workspace_size(*size)
         if nbytes:
             workspace = q.new_empty(nbytes, dtype=torch.uint8)
-    _call(dev.index, "paged_chunk_attention", q.data_ptr(), q_row, cache_k.data_ptr(), cache_v.data_ptr(), _ptr(scale_k), _ptr(scale_v),
-          o.data_ptr(), _ptr(lse), dt, n, _ptr(cu), B, kv_len.data_ptr(), _ptr(visible), page_table.data_ptr(), n_pages, page, max_pages,
-          Hq, Hk, D, h, w, _ptr(kv_frame_slot), frames, _ptr(corr_uv), _ptr(corr_idx), S, softmax_scale, lam, sigma, max_keys, key_parts,
-          _ptr(workspace), workspace.numel() if workspace is not None else 0)
+    _call(dev.index, "paged_chunk_attention_strided", q.data_ptr(), q_row, cache_k.data_ptr(), cache_v.data_ptr(), _ptr(scale_k),
+          _ptr(scale_v), o.data_ptr(), _ptr(lse), dt, n, _ptr(cu), B, kv_len.data_ptr(), _ptr(visible), page_table.data_ptr(), n_pages, page,
+          max_pages, Hq, Hk, D, h, w, _ptr(kv_frame_slot), frames, _ptr(corr_uv), _ptr(corr_idx), S, softmax_scale, lam, sigma, max_keys,
+          key_parts, _ptr(workspace), workspace.numel() if workspace is not None else 0, layout)
     return o, lse
 
 

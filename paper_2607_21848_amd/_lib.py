@@ -21,7 +21,8 @@ EXPORTED = ("rc_status_string", "rc_last_error", "retrieve_chunks", "reproject_c
             "rc_attention_workspace_size",
             "pack_retrieved_kv", "pool_token_depth", "rc_stream_create", "rc_stream_step", "rc_stream_view",
             "rc_stream_destroy", "rotary_embed", "attention_key_weight", "rc_key_weight_workspace_size", "select_kept",
-            "rc_select_workspace_size", "compact_kv", "append_paged_kv", "paged_chunk_attention", "rc_paged_attention_workspace_size")
+            "rc_select_workspace_size", "compact_kv", "append_paged_kv", "paged_chunk_attention", "rc_paged_attention_workspace_size",
+            "append_paged_kv_strided", "paged_chunk_attention_strided")
 
 _p = ctypes.c_void_p
 _i = ctypes.c_int32
@@ -50,6 +51,10 @@ class RevisitError(RuntimeError):
     def __init__(self, fn: str, status: int, detail: str):
         super().__init__(f"{fn}: status {status} ({status_string(status)}): {detail}")
         self.status = status
+
+
+# rc_pool_layout: how far apart a paged cache's pages, heads and positions are, of k and v, and of scale_k and scale_v
+PoolLayout = ctypes.c_int64 * 12
 
 
 def lib() -> ctypes.CDLL:
@@ -116,6 +121,10 @@ def lib() -> ctypes.CDLL:
         L.paged_chunk_attention.restype = ctypes.c_int
         L.paged_chunk_attention.argtypes = [_p, _l, _p, _p, _p, _p, _p, _p, _i, _i, _p, _i, _p, _p, _p, _i, _i, _i, _i, _i, _i, _i,
                                             _i, _p, _i, _p, _p, _i, _f, _f, _f, _i, _i, _p, _z, _p]
+        for name in ("append_paged_kv", "paged_chunk_attention"):  # with a layout before the stream
+            strided = getattr(L, name + "_strided")
+            strided.restype = ctypes.c_int
+            strided.argtypes = getattr(L, name).argtypes[:-1] + [ctypes.POINTER(PoolLayout), _p]
         L.rc_paged_attention_workspace_size.restype = ctypes.c_int
         L.rc_paged_attention_workspace_size.argtypes = [_i] * 11 + [ctypes.POINTER(ctypes.c_size_t)]
         _LIB = L

@@ -9,6 +9,8 @@
 #include <stdint.h>
 #include <stdio.h>
 
+#include <utility>
+
 #include <hip/hip_runtime.h>
 
 #include "../../include/revisit.h"
@@ -987,16 +989,109 @@ struct Range {
     double bytes;
 };
 
-// Refuses a written range that shares a byte with a read one or with another written one.
-int check_apart(const char* fn, const Range* written, int n_written, const Range* read, int n_read) {
+// Refuses a written range that shares a byte with a read one or with another written one (the first `known` of those apart from
+// each other already).
+int check_apart(const char* fn, const Range* written, int n_written, const Range* read, int n_read, int known = 0) {
     for (int i = 0; i < n_written; ++i) {
         if (!written[i].at) continue;
-        for (int j = i + 1; j < n_written; ++j)
+        for (int j = i + 1 < known ? known : i + 1; j < n_written; ++j)
             if (written[j].at && overlap(written[i].at, written[i].bytes, written[j].at, written[j].bytes))
                 return fail(REVISIT_ERR_SHAPE, "%s: %s and %s overlap", fn, written[i].name, written[j].name);
         for (int j = 0; j < n_read; ++j)
             if (read[j].at && overlap(written[i].at, written[i].bytes, read[j].at, read[j].bytes))
                 return fail(REVISIT_ERR_SHAPE, "%s: %s overlaps %s", fn, written[i].name, read[j].name);
+    }
+    return REVISIT_OK;
+}
+
+// A pool as runs of `run` bytes at at + i0 step[0] + i1 step[1] + i2 step[2], i_d < size[d], steps in falling order.
+struct Runs {
+    const void* at;
+    int64_t size[3], step[3], run;
+};
+
+Runs runs_of(const void* at, int64_t pages, int64_t heads, int64_t rows, revisit::PagedStrides& s, int64_t run) {
+    // a distance that nothing is apart by does not count
+    if (pages <= 1) s.page = 0;
+    if (heads <= 1) s.head = 0;
+    if (rows <= 1) s.row = 0;
+    Runs r{at, {pages, heads, rows}, {s.page, s.head, s.row}, run};
+    auto order = [&](int i, int j) {
+        if (r.step[i] > r.step[j] || (r.step[i] == r.step[j] && r.size[i] >= r.size[j])) return;
+        std::swap(r.step[i], r.step[j]);
+        std::swap(r.size[i], r.size[j]);
+    };
+    order(0, 1);
+    order(1, 2);
+    order(0, 1);
+    return r;
+}
+
+// Bytes from the first to behind the last of the dimensions from d on.
+double extent(const Runs& r, int d) {
+    double e = (double)r.run;
+    for (; d < 3; ++d) {
+        if (r.size[d] == 0) return 0.0;
+        e += (double)(r.size[d] - 1) * (double)r.step[d];
+    }
+    return e;
+}
+
+// Whether all runs are apart: each dimension's step spans what lies within it.
+bool all_apart(const Runs& r) {
+    for (int d = 0; d < 3; ++d)
+        if (r.size[d] > 1 && (double)r.step[d] < extent(r, d + 1)) return false;
+    return true;
+}
+
+// Whether runs of two pools, each all apart and the second one's `delta` bytes behind the first's, share a byte. Where an outer dimension
+// is the same, only neighbours in it can (keys beside values in one tensor); else their extents decide.
+bool share(const Runs& x, const Runs& y, int64_t delta, int d) {
+    if (d == 3 || x.size[d] != y.size[d] || x.step[d] != y.step[d]) return (double)delta < extent(x, d) && (double)-delta < extent(y, d);
+    if (x.size[d] <= 1) return share(x, y, delta, d + 1);
+    int64_t t = -delta / x.step[d];
+    if (t * x.step[d] > -delta) --t;  // floor
+    for (int64_t i = t; i <= t + 1; ++i)
+        if (i > -x.size[d] && i < x.size[d] && share(x, y, delta + i * x.step[d], d + 1)) return true;
+    return false;
+}
+
+// The pools as the kernels take them: cache_k, cache_v and, of 8 bits, scale_k and scale_v.
+struct Pools {
+    Range whole[4];  // from the first to behind the last byte
+    int count;
+    bool strided;
+    revisit::PagedLayout layout;  // in bytes, of strided ones
+    Runs runs[4];
+};
+
+// Contiguous pools (given NULL, or a layout that says so) need no distances.
+int check_layout(const char* fn, const revisit::PagedSeqs& q, int32_t dtype, int32_t H, int32_t D, const void* cache_k, const void* cache_v,
+                 const uint8_t* scale_k, const uint8_t* scale_v, const rc_pool_layout* given, Pools& p) {
+    const int64_t page = (int64_t)1 << q.page_log2, es = dtype == REVISIT_FP8_KV ? 1 : (dtype == REVISIT_F32 ? 4 : 2);
+    const double positions = (double)q.n_pages * page * H;
+    p.count = dtype == REVISIT_FP8_KV ? 4 : 2;
+    p.whole[0] = Range{"cache_k", cache_k, positions * (D * es)};
+    p.whole[1] = Range{"cache_v", cache_v, positions * (D * es)};
+    p.whole[2] = p.count == 4 ? Range{"scale_k", scale_k, positions / 32} : Range{};
+    p.whole[3] = p.count == 4 ? Range{"scale_v", scale_v, positions / 32} : Range{};
+    p.strided = false;
+    if (!given) return REVISIT_OK;
+    const int64_t* const from[4] = {given->k, given->v, given->scale_k, given->scale_v};
+    revisit::PagedStrides* const to[4] = {&p.layout.k, &p.layout.v, &p.layout.scale_k, &p.layout.scale_v};
+    for (int i = 0; i < p.count; ++i) {
+        const bool codes = i < 2;
+        const int64_t size = codes ? es : 1, run = codes ? D * es : 1, rows = codes ? page : page / 32;
+        for (int d = 0; d < 3; ++d)
+            if (from[i][d] < 0 || from[i][d] > kMaxElems) return fail(REVISIT_ERR_SHAPE, "%s: a stride of %s is negative or too large", fn, p.whole[i].name);
+        revisit::PagedStrides& s = *to[i];
+        s = revisit::PagedStrides{from[i][0] * size, from[i][1] * size, from[i][2] * size};
+        p.runs[i] = runs_of(p.whole[i].at, q.n_pages, H, rows, s, run);
+        if (codes && (s.page % 16 != 0 || s.head % 16 != 0 || s.row % 16 != 0))
+            return fail(REVISIT_ERR_SHAPE, "%s: positions of %s must start on 16 bytes", fn, p.whole[i].name);
+        p.whole[i].bytes = extent(p.runs[i], 0);
+        if (p.whole[i].bytes > (double)kMaxElems) return fail(REVISIT_ERR_SHAPE, "%s: %s spans too much memory", fn, p.whole[i].name);
+        p.strided = p.strided || (q.n_pages > 1 && s.page != H * rows * run) || (H > 1 && s.head != rows * run) || (rows > 1 && s.row != run);
     }
     return REVISIT_OK;
 }
@@ -1030,11 +1125,12 @@ int plan_paged_attention(const char* fn, int32_t Hq, int32_t max_keys, int32_t k
 
 extern "C" {
 
-int append_paged_kv(const void* k, int64_t k_row, const void* v, int64_t v_row, int32_t dtype, int32_t n_tokens,
-                    const int32_t* cu_tokens, int32_t B, const int32_t* kv_len, int32_t* out_len, void* cache_k, void* cache_v,
-                    uint8_t* scale_k, uint8_t* scale_v, const int32_t* page_table, int32_t n_pages, int32_t page, int32_t max_pages,
-                    int32_t H, int32_t D, const int32_t* pos, int32_t t0, int32_t h, int32_t w, int32_t pairs_t, int32_t pairs_y,
-                    int32_t pairs_x, float theta, hipStream_t stream) {
+int append_paged_kv_strided(const void* k, int64_t k_row, const void* v, int64_t v_row, int32_t dtype, int32_t n_tokens,
+                            const int32_t* cu_tokens, int32_t B, const int32_t* kv_len, int32_t* out_len, void* cache_k, void* cache_v,
+                            uint8_t* scale_k, uint8_t* scale_v, const int32_t* page_table, int32_t n_pages, int32_t page,
+                            int32_t max_pages, int32_t H, int32_t D, const int32_t* pos, int32_t t0, int32_t h, int32_t w,
+                            int32_t pairs_t, int32_t pairs_y, int32_t pairs_x, float theta, const rc_pool_layout* layout,
+                            hipStream_t stream) {
     const char* fn = "append_paged_kv";
     revisit::PagedAppendArgs a{};
     int st = check_paged(fn, dtype, n_tokens, cu_tokens, B, kv_len, page_table, n_pages, page, max_pages, H, D, a.seqs);
@@ -1044,7 +1140,7 @@ int append_paged_kv(const void* k, int64_t k_row, const void* v, int64_t v_row, 
     if (!(finite(theta) && theta > 0.0f)) return fail(REVISIT_ERR_PARAM, "%s: theta must be finite and > 0", fn);
     if (!pos && (h < 1 || w < 1 || (int64_t)h * w > INT32_MAX))
         return fail(REVISIT_ERR_SHAPE, "%s: without positions the token grid is needed: h, w >= 1", fn);
-    const int esize = dtype == REVISIT_F32 ? 4 : 2, osize = dtype == REVISIT_FP8_KV ? 1 : esize;
+    const int esize = dtype == REVISIT_F32 ? 4 : 2;
     const int64_t row = (int64_t)H * D, most = kMaxElems / (n_tokens > 1 ? n_tokens : 1);
     if (k_row < row || v_row < row || k_row > most || v_row > most)
         return fail(REVISIT_ERR_SHAPE, "%s: a row stride is below the row's %lld elements or too large", fn, (long long)row);
@@ -1055,21 +1151,26 @@ int append_paged_kv(const void* k, int64_t k_row, const void* v, int64_t v_row, 
     if (st != REVISIT_OK) return st;
     if (!aligned(k, 16) || !aligned(v, 16)) return fail(REVISIT_ERR_SHAPE, "%s: k and v must be 16-byte aligned", fn);
     if (!aligned(out_len, 4) || !aligned(pos, 4)) return fail(REVISIT_ERR_SHAPE, "%s: out_len and pos must be 4-byte aligned", fn);
-    const bool fp8 = dtype == REVISIT_FP8_KV;
-    const double positions = (double)n_pages * page * H, in_k = n_tokens ? ((double)(n_tokens - 1) * k_row + row) * esize : 0.0,
+    Pools pools;
+    st = check_layout(fn, a.seqs, dtype, H, D, cache_k, cache_v, scale_k, scale_v, layout, pools);
+    if (st != REVISIT_OK) return st;
+    for (int i = 0; i < pools.count && pools.strided; ++i) {
+        const Runs& x = pools.runs[i];
+        if (!all_apart(x)) return fail(REVISIT_ERR_SHAPE, "%s: positions of %s share memory", fn, pools.whole[i].name);
+        for (int j = i + 1; j < pools.count; ++j)
+            if (n_pages > 0 && share(x, pools.runs[j], (int64_t)((uintptr_t)pools.runs[j].at - (uintptr_t)x.at), 0))
+                return fail(REVISIT_ERR_SHAPE, "%s: %s and %s overlap", fn, pools.whole[i].name, pools.whole[j].name);
+    }
+    const double in_k = n_tokens ? ((double)(n_tokens - 1) * k_row + row) * esize : 0.0,
                  in_v = n_tokens ? ((double)(n_tokens - 1) * v_row + row) * esize : 0.0;
-    const Range written[] = {{"cache_k", cache_k, positions * D * osize},
-                             {"cache_v", cache_v, positions * D * osize},
-                             {"scale_k", fp8 ? scale_k : nullptr, positions / 32},
-                             {"scale_v", fp8 ? scale_v : nullptr, positions / 32},
-                             {"out_len", out_len, 4.0 * B}};
+    const Range written[] = {pools.whole[0], pools.whole[1], pools.whole[2], pools.whole[3], {"out_len", out_len, 4.0 * B}};
     const Range read[] = {{"k", k, in_k},
                           {"v", v, in_v},
                           {"cu_tokens", cu_tokens, 4.0 * (B + 1.0)},
                           {"kv_len", kv_len, 4.0 * B},
                           {"page_table", page_table, 4.0 * B * max_pages},
                           {"pos", pos, 12.0 * n_tokens}};
-    st = check_apart(fn, written, 5, read, 6);
+    st = check_apart(fn, written, 5, read, 6, pools.strided ? 4 : 0);
     if (st != REVISIT_OK) return st;
     a.k = k;
     a.v = v;
@@ -1079,6 +1180,8 @@ int append_paged_kv(const void* k, int64_t k_row, const void* v, int64_t v_row, 
     a.cache_v = cache_v;
     a.scale_k = scale_k;
     a.scale_v = scale_v;
+    a.strided = pools.strided;
+    a.layout = pools.layout;
     a.out_len = out_len;
     a.dtype = dtype;
     a.H = H;
@@ -1101,6 +1204,15 @@ int append_paged_kv(const void* k, int64_t k_row, const void* v, int64_t v_row, 
     return launched(revisit::launch_paged_append(a, f, stream), fn);
 }
 
+int append_paged_kv(const void* k, int64_t k_row, const void* v, int64_t v_row, int32_t dtype, int32_t n_tokens,
+                    const int32_t* cu_tokens, int32_t B, const int32_t* kv_len, int32_t* out_len, void* cache_k, void* cache_v,
+                    uint8_t* scale_k, uint8_t* scale_v, const int32_t* page_table, int32_t n_pages, int32_t page, int32_t max_pages,
+                    int32_t H, int32_t D, const int32_t* pos, int32_t t0, int32_t h, int32_t w, int32_t pairs_t, int32_t pairs_y,
+                    int32_t pairs_x, float theta, hipStream_t stream) {
+    return append_paged_kv_strided(k, k_row, v, v_row, dtype, n_tokens, cu_tokens, B, kv_len, out_len, cache_k, cache_v, scale_k, scale_v,
+                                   page_table, n_pages, page, max_pages, H, D, pos, t0, h, w, pairs_t, pairs_y, pairs_x, theta, nullptr, stream);
+}
+
 int rc_paged_attention_workspace_size(int32_t dtype, int32_t n_tokens, int32_t ragged, int32_t B, int32_t Hq, int32_t Hk, int32_t D,
                                       int32_t page, int32_t max_pages, int32_t max_keys, int32_t key_parts, size_t* bytes) {
     const char* fn = "rc_paged_attention_workspace_size";
@@ -1116,12 +1228,13 @@ int rc_paged_attention_workspace_size(int32_t dtype, int32_t n_tokens, int32_t r
     return plan_paged_attention(fn, Hq, max_keys, key_parts, a, bytes);
 }
 
-int paged_chunk_attention(const void* q, int64_t q_row, const void* cache_k, const void* cache_v, const uint8_t* scale_k,
-                          const uint8_t* scale_v, void* o, float* lse, int32_t dtype, int32_t n_tokens, const int32_t* cu_tokens, int32_t B,
-                          const int32_t* kv_len, const int32_t* visible, const int32_t* page_table, int32_t n_pages, int32_t page,
-                          int32_t max_pages, int32_t Hq, int32_t Hk, int32_t D, int32_t h, int32_t w, const int32_t* kv_frame_slot,
-                          int32_t max_frames, const float* corr_uv, const int32_t* corr_idx, int32_t S, float softmax_scale, float lambda,
-                          float sigma, int32_t max_keys, int32_t key_parts, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+int paged_chunk_attention_strided(const void* q, int64_t q_row, const void* cache_k, const void* cache_v, const uint8_t* scale_k,
+                                  const uint8_t* scale_v, void* o, float* lse, int32_t dtype, int32_t n_tokens, const int32_t* cu_tokens,
+                                  int32_t B, const int32_t* kv_len, const int32_t* visible, const int32_t* page_table, int32_t n_pages,
+                                  int32_t page, int32_t max_pages, int32_t Hq, int32_t Hk, int32_t D, int32_t h, int32_t w,
+                                  const int32_t* kv_frame_slot, int32_t max_frames, const float* corr_uv, const int32_t* corr_idx, int32_t S,
+                                  float softmax_scale, float lambda, float sigma, int32_t max_keys, int32_t key_parts, void* workspace,
+                                  size_t workspace_bytes, const rc_pool_layout* layout, hipStream_t stream) {
     const char* fn = "paged_chunk_attention";
     revisit::PagedAttentionArgs a{};
     int st = check_paged(fn, dtype, n_tokens, cu_tokens, B, kv_len, page_table, n_pages, page, max_pages, Hk, D, a.seqs);
@@ -1158,13 +1271,16 @@ int paged_chunk_attention(const void* q, int64_t q_row, const void* cache_k, con
     if (!aligned(q, 16) || !aligned(o, 16)) return fail(REVISIT_ERR_SHAPE, "%s: q and o must be 16-byte aligned", fn);
     if (!aligned(lse, 4) || !aligned(visible, 4) || (bias && (!aligned(kv_frame_slot, 4) || !aligned(corr_uv, 8) || !aligned(corr_idx, 4))))
         return fail(REVISIT_ERR_SHAPE, "%s: lse, visible, kv_frame_slot and corr_idx must be 4-byte, corr_uv 8-byte aligned", fn);
-    const double out = (double)n_tokens * row * esize, cache = (double)n_pages * page * Hk * D * (dtype == REVISIT_FP8_KV ? 1 : esize);
+    Pools pools;
+    st = check_layout(fn, a.seqs, dtype, Hk, D, cache_k, cache_v, scale_k, scale_v, layout, pools);
+    if (st != REVISIT_OK) return st;
+    const double out = (double)n_tokens * row * esize;
     const Range written[] = {{"o", o, out}, {"lse", lse, 4.0 * Hq * n_tokens}, {"workspace", need ? workspace : nullptr, (double)need}};
     const Range read[] = {{"q", q, ((double)(n_tokens - 1) * q_row + row) * esize},
-                          {"cache_k", cache_k, cache},
-                          {"cache_v", cache_v, cache},
-                          {"scale_k", dtype == REVISIT_FP8_KV ? scale_k : nullptr, (double)n_pages * page / 32 * Hk},
-                          {"scale_v", dtype == REVISIT_FP8_KV ? scale_v : nullptr, (double)n_pages * page / 32 * Hk},
+                          pools.whole[0],
+                          pools.whole[1],
+                          pools.whole[2],
+                          pools.whole[3],
                           {"cu_tokens", cu_tokens, 4.0 * (B + 1.0)},
                           {"kv_len", kv_len, 4.0 * B},
                           {"visible", visible, 4.0 * n_tokens},
@@ -1182,6 +1298,8 @@ int paged_chunk_attention(const void* q, int64_t q_row, const void* cache_k, con
     a.cache_v = cache_v;
     a.scale_k = scale_k;
     a.scale_v = scale_v;
+    a.strided = pools.strided;
+    a.layout = pools.layout;
     a.o = o;
     a.lse = lse;
     a.visible = visible;
@@ -1196,6 +1314,17 @@ int paged_chunk_attention(const void* q, int64_t q_row, const void* cache_k, con
     if (n_pages == 0) a.seqs.max_pages = 0;  // nobody has a key; the kernels take page 0 to be there
     a.partial = static_cast<float*>(workspace);
     return launched(revisit::launch_paged_attention(a, stream), fn);
+}
+
+int paged_chunk_attention(const void* q, int64_t q_row, const void* cache_k, const void* cache_v, const uint8_t* scale_k,
+                          const uint8_t* scale_v, void* o, float* lse, int32_t dtype, int32_t n_tokens, const int32_t* cu_tokens, int32_t B,
+                          const int32_t* kv_len, const int32_t* visible, const int32_t* page_table, int32_t n_pages, int32_t page,
+                          int32_t max_pages, int32_t Hq, int32_t Hk, int32_t D, int32_t h, int32_t w, const int32_t* kv_frame_slot,
+                          int32_t max_frames, const float* corr_uv, const int32_t* corr_idx, int32_t S, float softmax_scale, float lambda,
+                          float sigma, int32_t max_keys, int32_t key_parts, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    return paged_chunk_attention_strided(q, q_row, cache_k, cache_v, scale_k, scale_v, o, lse, dtype, n_tokens, cu_tokens, B, kv_len, visible,
+                                         page_table, n_pages, page, max_pages, Hq, Hk, D, h, w, kv_frame_slot, max_frames, corr_uv, corr_idx, S,
+                                         softmax_scale, lambda, sigma, max_keys, key_parts, workspace, workspace_bytes, nullptr, stream);
 }
 
 }  // extern "C"

@@ -332,6 +332,14 @@ struct PagedSeqs {
     int32_t n_pages, max_pages, page_log2;
 };
 
+// Bytes from page to page, head to head and position to position of a cache (of its scales: block of 32 to block).
+struct PagedStrides {
+    int64_t page, head, row;
+};
+struct PagedLayout {
+    PagedStrides k, v, scale_k, scale_v;
+};
+
 // New keys and values into the pages (paged_append.hip).
 struct PagedAppendArgs {
     PagedSeqs seqs;
@@ -348,6 +356,8 @@ struct PagedAppendArgs {
     int32_t t0, hw, w;      // pos NULL: position c of a stream stands at (t0 + c / hw, c / w mod h, c mod w)
     int32_t n_t, n_y, n_x;  // pairs of each band
     float inv_pairs[3];     // 1 / n_t, 1 / n_y, 1 / n_x
+    bool strided;           // the pools lie as `layout` says, else one page behind the other
+    PagedLayout layout;
 };
 struct PagedFreq {
     double quarter[64];  // quarter turns per position, of every pair (D <= 128)
@@ -381,6 +391,8 @@ struct PagedAttentionArgs {
     int32_t parts;  // of the keys
     int32_t many;   // workgroups of many waves
     float* partial;  // parts > 1: [tile][key head][part] results
+    bool strided;    // the pools lie as `layout` says, else one page behind the other
+    PagedLayout layout;
 };
 constexpr int32_t kPagedMaxParts = 64;
 size_t paged_plan(PagedAttentionArgs& a, int32_t key_parts, int32_t max_keys, int32_t cus);

@@ -20,6 +20,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "internal.h"
 #include "paged.h"
 #include "rope.h"
@@ -65,13 +67,13 @@ __device__ __forceinline__ uint32_t pack_e4m3(uint32_t a, uint32_t b, float scal
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2, b), scale, true));
 }
 
-// Codes of `rows` positions, rounded again from the scale 2^was to 2^now.
+// Codes of `rows` positions `step` bytes apart, rounded again from the scale 2^was to 2^now.
 template <int D>
-__device__ __forceinline__ void round_again(uint8_t* codes, int rows, int was, int now, int lane) {
+__device__ __forceinline__ void round_again(uint8_t* codes, int64_t step, int rows, int was, int now, int lane) {
     constexpr int kLanes = D / 8, kRows = 64 / kLanes;
     const float f = was - now < -126 ? 0.0f : power_of_two(was - now);
     for (int r = lane / kLanes; r < rows; r += kRows) {
-        u32x2* p = reinterpret_cast<u32x2*>(codes + r * D) + lane % kLanes;
+        u32x2* p = reinterpret_cast<u32x2*>(codes + r * step) + lane % kLanes;
         u32x2 w = *p;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -82,7 +84,7 @@ __device__ __forceinline__ void round_again(uint8_t* codes, int rows, int was, i
     }
 }
 
-template <int D, int ES, bool kFp8>
+template <int D, int ES, bool kFp8, bool kStrided>
 __global__ __launch_bounds__(64 * kWaves, D == 128 ? 3 : 4) void append_kernel(PagedAppendArgs a, PagedFreq f, unsigned blocks) {
     constexpr int kElems = 16 / ES, kPairs = kElems / 2;      // of a lane's vector
     constexpr int kLanes = D / kElems, kRows = 64 / kLanes;   // lanes of a row, rows of a load
@@ -158,11 +160,27 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 3 : 4) void append_kernel(P
     load(0);
     if constexpr (ES == 2) load(1);
     if (page < 0) return;  // nowhere to store them (uniform)
+    constexpr int kOut = kFp8 ? D : D * ES;  // bytes of a stored row
     const size_t slot = ((size_t)page * a.H + head_in) << q.page_log2;  // first position of the head's page
+    // the block's first position in a cache, its scale, and the bytes from position to position
+    auto block_at = [&](int which) -> uint8_t* {
+        uint8_t* cache = static_cast<uint8_t*>(which ? a.cache_v : a.cache_k);
+        if constexpr (kStrided) return cache + strided_at(which ? a.layout.v : a.layout.k, page, head_in, row0);
+        else return cache + (slot + row0) * kOut;
+    };
+    auto scale_at = [&](int which) -> uint8_t* {
+        uint8_t* scale = which ? a.scale_v : a.scale_k;
+        if constexpr (kStrided) return scale + strided_at(which ? a.layout.scale_v : a.layout.scale_k, page, head_in, row0 / kScaleBlock);
+        else return scale + (slot + row0) / kScaleBlock;
+    };
+    auto step_of = [&](int which) -> int64_t {
+        if constexpr (kStrided) return which ? a.layout.v.row : a.layout.k.row;
+        else return kOut;
+    };
     uint8_t was[2] = {0, 0};  // the block's scales
     if constexpr (kFp8) {
-        was[0] = a.scale_k[(slot + row0) / kScaleBlock];
-        was[1] = a.scale_v[(slot + row0) / kScaleBlock];
+        was[0] = *scale_at(0);
+        was[1] = *scale_at(1);
     }
     if (tid < P) freq[tid] = own_freq;
 
@@ -224,27 +242,30 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 3 : 4) void append_kernel(P
         }
     };
     auto is_new = [&](int i) -> bool { return i * kRows + r_lane >= lo && i * kRows + r_lane < hi; };
-    constexpr int kOut = kFp8 ? D : D * ES;  // bytes of a stored row
+    // the lane's part of load i in a cache
     const size_t to_lane = (slot + row0 + r_lane) * (size_t)kOut + (kOut / kLanes) * c_lane;
+    auto lane_at = [&](int which, int i) -> uint8_t* {
+        if constexpr (kStrided) return block_at(which) + r_lane * step_of(which) + (kOut / kLanes) * c_lane + i * (kRows * step_of(which));
+        else return static_cast<uint8_t*>(which ? a.cache_v : a.cache_k) + to_lane + i * (kRows * kOut);
+    };
     if constexpr (kFp8) {
         // a block's codes from its largest value's bits: word(i, scale) is the lane's part of load i
         auto store = [&](int which, uint32_t most, auto word) __attribute__((always_inline)) {
 #pragma unroll
             for (int off = 1; off < 64; off *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, off));
             int e = scale_exponent(most);
-            uint8_t* cache = static_cast<uint8_t*>(which ? a.cache_v : a.cache_k);
             if (lo > 0) {
                 const int old = min((int)was[which], kScaleHigh + 127) - 127;
-                if (e > old) round_again<D>(cache + (slot + row0) * D, lo, old, e, lane);
+                if (e > old) round_again<D>(block_at(which), step_of(which), lo, old, e, lane);
                 e = max(e, old);
             }
             const float to = power_of_two(e);
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const u32x2 w = word(i, to);
-                if (is_new(i)) *reinterpret_cast<u32x2*>(cache + to_lane + i * (kRows * kOut)) = w;
+                if (is_new(i)) *reinterpret_cast<u32x2*>(lane_at(which, i)) = w;
             }
-            if (lane == 0) (which ? a.scale_v : a.scale_k)[(slot + row0) / kScaleBlock] = (uint8_t)(e + 127);
+            if (lane == 0) *scale_at(which) = (uint8_t)(e + 127);
         };
         // Largest values: of keys by fp32, of values by the bits of two bf16 at a time. Where one is not finite (bf16 with an
         // exponent of ones, or a turned pair past fp32), the others are looked at one by one.
@@ -295,7 +316,6 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 3 : 4) void append_kernel(P
             return u32x2{pack_e4m3(x[1][i][0], x[1][i][1], to), pack_e4m3(x[1][i][2], x[1][i][3], to)};
         });
     } else {
-        uint8_t* out = static_cast<uint8_t*>(a.cache_k) + to_lane;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             floatx2 p[kPairs];
@@ -311,13 +331,12 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 3 : 4) void append_kernel(P
                     w[2 * j + 1] = __float_as_uint(p[j][1]);
                 }
             }
-            if (is_new(i)) *reinterpret_cast<u32x4*>(out + i * (kRows * kOut)) = w;
+            if (is_new(i)) *reinterpret_cast<u32x4*>(lane_at(0, i)) = w;
         }
         if constexpr (ES == 4) load(1);
-        out = static_cast<uint8_t*>(a.cache_v) + to_lane;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            if (is_new(i)) *reinterpret_cast<u32x4*>(out + i * (kRows * kOut)) = x[1][i];
+            if (is_new(i)) *reinterpret_cast<u32x4*>(lane_at(1, i)) = x[1][i];
     }
 }
 
@@ -341,15 +360,19 @@ hipError_t launch_paged_append(const PagedAppendArgs& a, const PagedFreq& f, hip
     if (blocks + lengths == 0) return hipSuccess;
     const dim3 grid = grid_rows(blocks + lengths), block(64 * kWaves);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, f, blocks); };
-    if (a.D == 128) {
-        if (a.dtype == kPagedFp8) launch(append_kernel<128, 2, true>);
-        else if (a.dtype == kPagedBf16) launch(append_kernel<128, 2, false>);
-        else launch(append_kernel<128, 4, false>);
-    } else {
-        if (a.dtype == kPagedFp8) launch(append_kernel<64, 2, true>);
-        else if (a.dtype == kPagedBf16) launch(append_kernel<64, 2, false>);
-        else launch(append_kernel<64, 4, false>);
-    }
+    auto by_type = [&](auto d_tag, auto strided_tag) {
+        constexpr int D = decltype(d_tag)::value;
+        constexpr bool S = decltype(strided_tag)::value;
+        if (a.dtype == kPagedFp8) launch(append_kernel<D, 2, true, S>);
+        else if (a.dtype == kPagedBf16) launch(append_kernel<D, 2, false, S>);
+        else launch(append_kernel<D, 4, false, S>);
+    };
+    auto by_layout = [&](auto d_tag) {
+        if (a.strided) by_type(d_tag, std::true_type{});
+        else by_type(d_tag, std::false_type{});
+    };
+    if (a.D == 128) by_layout(std::integral_constant<int, 128>{});
+    else by_layout(std::integral_constant<int, 64>{});
     return hipGetLastError();
 }
 

@@ -94,7 +94,7 @@ constexpr int kCorrFrames = 16, kSlotFrames = 256;  // retrieved and key frames 
 // two would need each tile's keys and values loaded when their turn comes, 544 us with one and 561 with two so). The MFMAs
 // accumulate in the registers that vector instructions read (-amdgpu-mfma-vgpr-form, set for this file): 1170 biased fp32
 // queries at D = 128 543 us without, 514 with. Loads put between the products by hand instead of by the compiler: 528.
-template <int D, int T, int NQ, bool kBias, int kW>
+template <int D, int T, int NQ, bool kBias, int kW, bool kStrided>
 __global__ __launch_bounds__(64 * kW, kW > 4 || (T == kPagedF32 ? D == 64 : NQ == 1) ? 2 : 1) void paged_wave_kernel(PagedAttentionArgs a, float c_log2) {
     using Sh = Shape<D, T>;
     constexpr int kRows = 16 * NQ;
@@ -202,31 +202,42 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (T == kPagedF32 ? D == 64 : NQ =
         int t, page;
     };
     const int in_page = (1 << sq.page_log2) - 1;
+    // where a tile's rows of a cache and its scale are, and the bytes from row to row
     auto tile_row = [&](int t, int page) -> size_t { return (((size_t)page * a.Hk + hk) << sq.page_log2) + ((t * kTK) & in_page); };
+    auto tile_at = [&](const void* cache, const PagedStrides& st, int t, int page) -> const uint8_t* {
+        if constexpr (kStrided) return static_cast<const uint8_t*>(cache) + strided_at(st, page, hk, (t * kTK) & in_page);
+        else return static_cast<const uint8_t*>(cache) + tile_row(t, page) * Sh::kRowBytes;
+    };
+    auto scale_of = [&](const uint8_t* scale, const PagedStrides& st, int t, int page) -> int {
+        if constexpr (kStrided) return scale[strided_at(st, page, hk, ((t * kTK) & in_page) / kScaleBlock)];
+        else return scale[tile_row(t, page) / kScaleBlock];
+    };
+    auto step_of = [&](const PagedStrides& st) -> int64_t {
+        if constexpr (kStrided) return st.row;
+        else return Sh::kRowBytes;
+    };
     auto load_k = [&](Tile& b, int t, int page) {
-        const size_t row = tile_row(t, page);
-        const uint8_t* base = static_cast<const uint8_t*>(a.cache_k) + row * Sh::kRowBytes;
+        const uint8_t* base = tile_at(a.cache_k, a.layout.k, t, page);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int u = 0; u < Sh::kKLoads; ++u)
-                b.kr[i][u] = *reinterpret_cast<const u32x4*>(base + (16 * i + m) * Sh::kRowBytes + 64 * u + 16 * grp);
-        if constexpr (T == kPagedFp8) b.k_byte = a.scale_k[row / kScaleBlock];
+                b.kr[i][u] = *reinterpret_cast<const u32x4*>(base + (16 * i + m) * step_of(a.layout.k) + 64 * u + 16 * grp);
+        if constexpr (T == kPagedFp8) b.k_byte = scale_of(a.scale_k, a.layout.scale_k, t, page);
     };
     // key of the lane's element j
     auto key_of = [&](int j) -> int { return 16 * (j >> 2) + 4 * grp + (j & 3); };
     auto load_v = [&](Tile& b, int t, int page) {
-        const size_t row = tile_row(t, page);
-        const uint8_t* base = static_cast<const uint8_t*>(a.cache_v) + row * Sh::kRowBytes;
+        const uint8_t* base = tile_at(a.cache_v, a.layout.v, t, page);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int u = 0; u < kVHalves; ++u) {
                 // fp32 at D 128: head dims 64 u + 4 m .., else kDb m ..
                 const int off = kVHalves == 2 ? 256 * u + 16 * m : Sh::kVBytes * m;
-                b.vr[j][u] = *reinterpret_cast<const VVec*>(base + key_of(j) * Sh::kRowBytes + off);
+                b.vr[j][u] = *reinterpret_cast<const VVec*>(base + key_of(j) * step_of(a.layout.v) + off);
             }
-        if constexpr (T == kPagedFp8) b.v_byte = a.scale_v[row / kScaleBlock];
+        if constexpr (T == kPagedFp8) b.v_byte = scale_of(a.scale_v, a.layout.scale_v, t, page);
     };
 
     // head dim of row 4 grp + i, block db
@@ -445,8 +456,7 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (T == kPagedF32 ? D == 64 : NQ =
 #pragma unroll
                     for (int w = 0; w < Sh::kVWords / kVHalves; ++w) bad |= not_finite<T>(value_word(j, u, w));
             if (__builtin_expect(__any(bad != 0), 0)) {
-                const size_t row = tile_row(t, page);
-                const uint8_t* base = static_cast<const uint8_t*>(a.cache_v) + row * Sh::kRowBytes;
+                const uint8_t* base = tile_at(a.cache_v, a.layout.v, t, page);
 #pragma unroll 1
                 for (int key = 0; key < min(kTK, held - k0); ++key) {
                     const int j = 4 * (key >> 4) + (key & 3), from = 16 * ((key >> 2) & 3) + m;
@@ -462,7 +472,7 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (T == kPagedF32 ? D == 64 : NQ =
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
                         for (int db = 0; db < kDb; ++db) {
-                            const float x = stored<T>(base + key * Sh::kRowBytes, dim(i, db)) * v_scale;
+                            const float x = stored<T>(base + key * step_of(a.layout.v), dim(i, db)) * v_scale;
 #pragma unroll
                             for (int nq = 0; nq < NQ; ++nq)
                                 if (!(fabsf(x) < INFINITY) && k0 + key < vis[nq]) O[nq][db][i] += p[nq] * x;
@@ -774,7 +784,8 @@ hipError_t launch_paged_attention(const PagedAttentionArgs& a, hipStream_t strea
         auto launch = [&](auto nq_tag, auto bias_tag, auto w_tag) {
             constexpr int NQ = decltype(nq_tag)::value, W = decltype(w_tag)::value;
             constexpr bool B = decltype(bias_tag)::value;
-            hipLaunchKernelGGL((paged_wave_kernel<D, T, NQ, B, W>), grid, dim3(64 * W), 0, stream, a, c);
+            if (a.strided) hipLaunchKernelGGL((paged_wave_kernel<D, T, NQ, B, W, true>), grid, dim3(64 * W), 0, stream, a, c);
+            else hipLaunchKernelGGL((paged_wave_kernel<D, T, NQ, B, W, false>), grid, dim3(64 * W), 0, stream, a, c);
         };
         auto rows = [&](auto bias_tag) {
             using W4 = std::integral_constant<int, 4>;

@@ -108,7 +108,7 @@ __device__ __forceinline__ RareArgs rare_args() {
     return (RareArgs)p;
 }
 
-template <int D, int T, bool kBias, int kQ>
+template <int D, int T, bool kBias, int kQ, bool kStrided>
 __global__ __launch_bounds__(256, kQ == 2 ? 1 : 2) void paged_tile_kernel(PagedAttentionArgs a, float c_log2) {
     constexpr int kRowB = D * 2, kTileB = kTK * kRowB;      // in LDS
     constexpr int kStored = T == kPagedFp8 ? D : 2 * D;     // bytes of a row in the pages
@@ -120,6 +120,7 @@ __global__ __launch_bounds__(256, kQ == 2 ? 1 : 2) void paged_tile_kernel(PagedA
     __shared__ u32x4 lds_tab[2][kBias ? kGridSide : 1];     // key operands by column and by row
     __shared__ float2 lds_corr[kBias ? kCorrLds : 1][kRows];  // centred correspondences, NaN: rejected
     __shared__ int lds_block[512];
+    __shared__ int64_t lds_at[2][kStrided ? 512 : 1];       // strided pools: bytes at which a tile's keys and values begin
     __shared__ int2 lds_bias[kBias ? 512 : 1];              // slot (-1: unbiased, -2: across frames) and in-frame position of a tile
     __shared__ u32x4 lds_qop[kBias ? kW : 1][kQ][64];       // the waves' query operands of the frame at hand
     __shared__ float lds_scale[2][T == kPagedFp8 ? 512 : 1];
@@ -212,10 +213,23 @@ __global__ __launch_bounds__(256, kQ == 2 ? 1 : 2) void paged_tile_kernel(PagedA
         const int page_log2 = r->seqs.page_log2;
         const int entry = r->seqs.page_table[(int64_t)s * r->seqs.max_pages + (pos >> page_log2)];
         const bool there = (unsigned)entry < (unsigned)r->seqs.n_pages;
-        const int block = (((there ? entry : 0) * r->Hk + hk) << (page_log2 - 5)) + ((pos & ((1 << page_log2) - 1)) >> 5);
-        if constexpr (T == kPagedFp8) {
-            lds_scale[0][x & 511] = scale_value(r->scale_k[block]);
-            lds_scale[1][x & 511] = scale_value(r->scale_v[block]);
+        const int page = there ? entry : 0, in_page = (pos & ((1 << page_log2) - 1)) >> 5;
+        int block;
+        if constexpr (kStrided) {
+            block = (page << (page_log2 - 5)) + in_page;
+            auto at = [&](const __attribute__((address_space(4))) PagedStrides& st, int row) -> int64_t { return page * st.page + hk * st.head + row * st.row; };
+            lds_at[0][x & 511] = at(r->layout.k, in_page * kTK);
+            lds_at[1][x & 511] = at(r->layout.v, in_page * kTK);
+            if constexpr (T == kPagedFp8) {
+                lds_scale[0][x & 511] = scale_value(r->scale_k[at(r->layout.scale_k, in_page)]);
+                lds_scale[1][x & 511] = scale_value(r->scale_v[at(r->layout.scale_v, in_page)]);
+            }
+        } else {
+            block = ((page * r->Hk + hk) << (page_log2 - 5)) + in_page;
+            if constexpr (T == kPagedFp8) {
+                lds_scale[0][x & 511] = scale_value(r->scale_k[block]);
+                lds_scale[1][x & 511] = scale_value(r->scale_v[block]);
+            }
         }
         lds_block[x & 511] = there ? block : -1;
         if constexpr (kBias) {
@@ -230,15 +244,29 @@ __global__ __launch_bounds__(256, kQ == 2 ? 1 : 2) void paged_tile_kernel(PagedA
     };
     auto block_of = [&](int j) __attribute__((always_inline)) -> int { return lds_block[j & 511]; };
     u32x4 piece[kPieces];
-    // pieces of the K tile in block bk and the V tile in block bv; piece p of a thread is number kThreads p + tid of K's
-    // and then V's
-    auto load = [&](int bk, int bv) __attribute__((always_inline)) {
-        const uint8_t* kb = static_cast<const uint8_t*>(a.cache_k) + (size_t)(unsigned)max(bk, 0) * (kTK * kStored);
-        const uint8_t* vb = static_cast<const uint8_t*>(a.cache_v) + (size_t)(unsigned)max(bv, 0) * (kTK * kStored);
+    auto scalar = [](int64_t x) __attribute__((always_inline)) -> int64_t {  // the same in all of the wave
+        return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+    };
+    // pieces of the K tile in block bk and the V tile in block bv (of strided pools: at bytes ak and av); piece p of a thread is
+    // number kThreads p + tid of K's and then V's
+    auto load = [&](int bk, int bv, int64_t ak, int64_t av) __attribute__((always_inline)) {
+        const uint8_t* kb = static_cast<const uint8_t*>(a.cache_k) + (kStrided ? ak : (int64_t)(unsigned)max(bk, 0) * (kTK * kStored));
+        const uint8_t* vb = static_cast<const uint8_t*>(a.cache_v) + (kStrided ? av : (int64_t)(unsigned)max(bv, 0) * (kTK * kStored));
 #pragma unroll
         for (int p = 0; p < kPieces; ++p) {
             const int i = kThreads * p + tid;
-            if constexpr (kHalf % kThreads == 0) {
+            if constexpr (kStrided) {
+                constexpr int kOf = kStored / 16;  // pieces of a row
+                const bool is_v = kHalf % kThreads == 0 ? kThreads * p >= kHalf : i >= kHalf;
+                const int64_t step = is_v ? a.layout.v.row : a.layout.k.row;
+                if constexpr (kHalf % kThreads == 0) {
+                    const int first = kThreads * p - (kThreads * p >= kHalf ? kHalf : 0);  // of the threads' pieces
+                    piece[p] = *reinterpret_cast<const u32x4*>((is_v ? vb : kb) + first / kOf * step + (tid / kOf * step + 16 * (tid % kOf)));
+                } else {
+                    const int at = is_v ? i - kHalf : i;
+                    if (2 * kHalf % kThreads == 0 || i < 2 * kHalf) piece[p] = *reinterpret_cast<const u32x4*>((is_v ? vb : kb) + at / kOf * step + 16 * (at % kOf));
+                }
+            } else if constexpr (kHalf % kThreads == 0) {
                 const uint32_t off = 16 * (uint32_t)tid;
                 piece[p] = *reinterpret_cast<const u32x4*>((kThreads * p >= kHalf ? vb + 16 * (kThreads * p - kHalf) : kb + 16 * kThreads * p) + off);
             } else {
@@ -432,8 +460,17 @@ __global__ __launch_bounds__(256, kQ == 2 ? 1 : 2) void paged_tile_kernel(PagedA
     auto odd_values = [&](const uint32_t (&w4)[kQ][2][4], int j, int block) __attribute__((always_inline)) {
         const int k0 = (t0 + j) * kTK;
         const RareArgs r = rare_args();
-        const uint8_t* base = static_cast<const uint8_t*>(r->cache_v) + (size_t)(unsigned)block * (kTK * kStored);
-        const float f = T == kPagedFp8 ? scale_value(r->scale_v[block]) : 1.0f;
+        const uint8_t* base;
+        int64_t step = kStored, scale_at = block;
+        if constexpr (kStrided) {
+            const int shift = r->seqs.page_log2 - 5, page = block >> shift, in_page = block & ((1 << shift) - 1);
+            base = static_cast<const uint8_t*>(r->cache_v) + lds_at[1][j & 511];
+            step = r->layout.v.row;
+            scale_at = page * r->layout.scale_v.page + hk * r->layout.scale_v.head + in_page * r->layout.scale_v.row;
+        } else {
+            base = static_cast<const uint8_t*>(r->cache_v) + (size_t)(unsigned)block * (kTK * kStored);
+        }
+        const float f = T == kPagedFp8 ? scale_value(r->scale_v[scale_at]) : 1.0f;
 #pragma unroll 1
         for (int key = 0; key < min(kTK, held - k0); ++key) {
             const int want = 8 * (key >> 4) + (key & 7);  // register of the lane that has its probability
@@ -455,7 +492,7 @@ __global__ __launch_bounds__(256, kQ == 2 ? 1 : 2) void paged_tile_kernel(PagedA
             for (int db = 0; db < kDb; ++db)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float x = stored<T>(base + key * kStored, 32 * db + 8 * (i >> 2) + 4 * hh + (i & 3)) * f;
+                    const float x = stored<T>(base + key * step, 32 * db + 8 * (i >> 2) + 4 * hh + (i & 3)) * f;
 #pragma unroll
                     for (int b = 0; b < kQ; ++b) {
                         const float seen_x = __uint_as_float(__float_as_uint(x) & sees[b]);
@@ -548,11 +585,20 @@ __global__ __launch_bounds__(256, kQ == 2 ? 1 : 2) void paged_tile_kernel(PagedA
             __builtin_amdgcn_sched_barrier(0);
         }
         // P V of tile j beside the staging (the pieces of K_{j+2} and V_{j+1} go to LDS, those behind them leave) and the row maxima of tile j + 1
+        int64_t at_k = 0, at_v = 0;
+        if constexpr (kStrided) {
+            at_k = lds_at[0][(j + 4) & 511];
+            at_v = lds_at[1][(j + 3) & 511];
+        }
         lds_barrier();  // slot kRefill was read two steps ago; what was written to the others is there
         const int jv = min(j + 2, nt - 1);
         if (__builtin_expect((t0 + jv + 1) * kTK > least || b2 < 0, 0)) leave_out(kRefill, v_scale, jv, b2);
         if (__builtin_expect((t0 + j + 2) * kTK > seen_min || b1 < 0, 0)) mask(S_next, j + 1, b1);
         const int b4 = __builtin_amdgcn_readfirstlane(b4_lane);
+        if constexpr (kStrided) {
+            at_k = scalar(at_k);
+            at_v = scalar(at_v);
+        }
         bf16x8 pf[kQ][2];
 #pragma unroll
         for (int b = 0; b < kQ; ++b)
@@ -568,7 +614,7 @@ __global__ __launch_bounds__(256, kQ == 2 ? 1 : 2) void paged_tile_kernel(PagedA
             if (t == 0) {
 #pragma unroll
                 for (int x = i * kPuts / (kSlotsB / 2); x < (i + 1) * kPuts / (kSlotsB / 2); ++x) put(kRefill, x >> 1, x & 1, k_scale, v_scale);
-                if (i == kSlotsB / 2 - 1) load(b4, b3);
+                if (i == kSlotsB / 2 - 1) load(b4, b3, at_k, at_v);
             } else {
                 const int slot = i - kSlotsB / 2, per = 16 * kQ / (kSlotsB / 2);  // logits of a slot
 #pragma unroll
@@ -603,17 +649,18 @@ __global__ __launch_bounds__(256, kQ == 2 ? 1 : 2) void paged_tile_kernel(PagedA
         if (tid < 4) lds_odd[tid] = -1;
         __syncthreads();
         auto scale = [&](int which, int j) -> float { return T == kPagedFp8 ? lds_scale[which][j] : 1.0f; };
+        auto place = [&](int which, int j) -> int64_t { return kStrided ? scalar(lds_at[which][j]) : 0; };
         b0 = __builtin_amdgcn_readfirstlane(block_of(0));
         b1 = __builtin_amdgcn_readfirstlane(block_of(1));
         b2 = __builtin_amdgcn_readfirstlane(block_of(2));
         b3 = __builtin_amdgcn_readfirstlane(block_of(3));
-        load(b0, b0);
+        load(b0, b0, place(0, 0), place(1, 0));
         put_all(0, scale(0, 0), scale(1, 0), 0, b0);
-        load(b1, b0);
+        load(b1, b0, place(0, 1), place(1, 0));
         put_all(1, scale(0, 1), scale(1, 0), 0, b0);
-        load(b2, b1);
+        load(b2, b1, place(0, 2), place(1, 1));
         put_all(2, scale(0, 2), scale(1, 1), min(1, nt - 1), b1);
-        load(b3, b2);
+        load(b3, b2, place(0, 3), place(1, 2));
         __syncthreads();
 #pragma unroll
         for (int kk = 0; kk < 3; ++kk) kf[kk] = *reinterpret_cast<const u32x4*>(ring[1] + koff[kk]);
@@ -701,8 +748,13 @@ hipError_t launch_paged_tiles(const PagedAttentionArgs& a, hipStream_t stream) {
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, c); };
     auto bias = [&](auto d_tag, auto t_tag, auto q_tag) {
         constexpr int D = decltype(d_tag)::value, T = decltype(t_tag)::value, kQ = decltype(q_tag)::value;
-        if (a.S > 0) launch(paged_tile_kernel<D, T, true, kQ>);
-        else launch(paged_tile_kernel<D, T, false, kQ>);
+        auto layout = [&](auto strided_tag) {
+            constexpr bool kStrided = decltype(strided_tag)::value;
+            if (a.S > 0) launch(paged_tile_kernel<D, T, true, kQ, kStrided>);
+            else launch(paged_tile_kernel<D, T, false, kQ, kStrided>);
+        };
+        if (a.strided) layout(std::true_type{});
+        else layout(std::false_type{});
     };
     auto rows = [&](auto t_tag) {
         using One = std::integral_constant<int, 1>;
