@@ -655,7 +655,8 @@ typedef struct rc_pool_layout {
  * with |x| <= 448 2^e for the finite values x of its new rows (e4m3 is a floating format, so
  * a power of two leaves its normal values' precision as it is). Where it holds
  * positions, the exponent is that or the stored one, whichever is larger; if
- * it grows, the codes that are there are rounded to it again, to nearest even.
+ * it grows, the codes that are there are rounded to it again, to nearest even. A
+ * stored scale of NaN stays, with the codes beside it, and new rows there are NaN.
  * What is not finite is stored as NaN.
  *
  *   k, v          [n_tokens] rows of [H][D] elements, row r starting k_row / v_row

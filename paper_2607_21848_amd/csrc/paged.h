@@ -21,7 +21,6 @@ namespace revisit {
 
 constexpr int kScaleBlock = 32;    // positions that share a scale
 constexpr int kScaleLow = -100;    // smallest exponent that is written: 2^-110, the smallest value, is far above what bf16 flushes
-constexpr int kScaleHigh = 120;    // largest one that an fp32 value needs
 
 typedef const __attribute__((address_space(4))) int32_t const_i32;  // memory that does not change while the kernel runs
 

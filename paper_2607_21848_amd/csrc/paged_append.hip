@@ -48,7 +48,7 @@ __device__ __forceinline__ uint32_t finite_bits(float x) {
     return b < 0x7f800000u ? b : 0u;
 }
 
-// least e in [kScaleLow, kScaleHigh] with m <= 448 2^e, m >= 0 by its bits: 448 = 1.75 2^8
+// least e >= kScaleLow with m <= 448 2^e, m >= 0 by its bits: 448 = 1.75 2^8. At most 120.
 __device__ __forceinline__ int scale_exponent(uint32_t m) {
     const int e = (int)(m >> 23) - 127 - 8 + ((m & 0x7fffffu) > 0x600000u ? 1 : 0);
     return max(e, kScaleLow);
@@ -254,15 +254,16 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 3 : 4) void append_kernel(P
 #pragma unroll
             for (int off = 1; off < 64; off *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, off));
             int e = scale_exponent(most);
-            if (lo > 0) {
-                const int old = min((int)was[which], kScaleHigh + 127) - 127;
+            if (lo > 0) {  // byte 0 counts as 1; 255, NaN, stays, and so do the codes that are there
+                const int old = max((int)was[which], 1) - 127;
                 if (e > old) round_again<D>(block_at(which), step_of(which), lo, old, e, lane);
                 e = max(e, old);
             }
-            const float to = power_of_two(e);
+            const float to = power_of_two(min(e, 127));
+            const uint32_t lost = e > 127 ? 0x7f7f7f7fu : 0u;  // beside a NaN scale codes are NaN too
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const u32x2 w = word(i, to);
+                const u32x2 w = word(i, to) | lost;
                 if (is_new(i)) *reinterpret_cast<u32x2*>(lane_at(which, i)) = w;
             }
             if (lane == 0) *scale_at(which) = (uint8_t)(e + 127);
