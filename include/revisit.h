@@ -657,7 +657,8 @@ typedef struct rc_pool_layout {
  * positions, the exponent is that or the stored one, whichever is larger; if
  * it grows, the codes that are there are rounded to it again, to nearest even. A
  * stored scale of NaN stays, with the codes beside it, and new rows there are NaN.
- * What is not finite is stored as NaN.
+ * What is not finite is stored as NaN, and what is finite but above 1.875 2^127 in
+ * magnitude as that: the next code would stand for 2^128.
  *
  *   k, v          [n_tokens] rows of [H][D] elements, row r starting k_row / v_row
  *                 elements after row r - 1 (both may be views into the rows of one

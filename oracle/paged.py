@@ -6,7 +6,7 @@ but where the cache's definition rounds (the codes and scales of 8-bit pages).
 * position c of stream s lies in row c mod page of page table[s][c // page], if that is a page;
 * scales: of the 32 positions of a block, per head, 2^e with the least e >= -100 that brings the largest finite new
   value to 448 2^e or below, never below the stored e where the block held positions of the stream;
-* codes: the nearest e4m3 value of x 2^-e, ties to even; NaN where x is not finite;
+* codes: the nearest e4m3 value of x 2^-e, ties to even, of those that stand for less than 2^128; NaN where x is not finite;
 * attention: softmax over the keys below min(length, visible) that have a page, biased in retrieved frames.
 """
 

@@ -37,6 +37,9 @@ typedef short shortx2 __attribute__((ext_vector_type(2)));
 typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;  // heads of a workgroup
+// Largest value that is stored: a code times its scale below 2^128. What is finite above it would get, under 2^120 or more, the
+// code of 2^128, which no bf16 holds; it is stored as this, less than half a step of e4m3 (2^-4 of it) away.
+constexpr float kLargest = 0x1.ep127f;
 
 __device__ __forceinline__ floatx2 turn(floatx2 p, CosSin r) { return floatx2{p[0] * r.c - p[1] * r.s, p[0] * r.s + p[1] * r.c}; }
 
@@ -296,6 +299,18 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 3 : 4) void append_kernel(P
                         }
                 top = __uint_as_float(most);
             }
+            if (__any(top > kLargest)) {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                    for (int j = 0; j < kPairs; ++j)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float x = p[i][j][h], c = fminf(fmaxf(x, -kLargest), kLargest);
+                            p[i][j][h] = fabsf(x) < INFINITY ? c : x;
+                            __builtin_amdgcn_sched_barrier(0);  // one mask at a time
+                        }
+            }
             store(0, __float_as_uint(top), [&](int i, float to) -> u32x2 { return u32x2{pack_e4m3(p[i][0], p[i][1], to), pack_e4m3(p[i][2], p[i][3], to)}; });
         }
         ushortx2 bits = {0, 0};
@@ -311,6 +326,17 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 3 : 4) void append_kernel(P
                 for (int j = 0; j < kPairs; ++j) {
                     const uint32_t bad = spread<kPagedBf16>(not_finite<kPagedBf16>(x[1][i][j]));
                     bits = __builtin_elementwise_max(bits, __builtin_bit_cast(ushortx2, x[1][i][j] & ~bad & 0x7fff7fffu));
+                }
+        }
+        if (__any(max(bits[0], bits[1]) > __float_as_uint(kLargest) >> 16)) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                for (int j = 0; j < kPairs; ++j) {
+                    // the sign and the magnitude, or the largest one where the magnitude is between it and infinity
+                    const uint32_t w = x[1][i][j], inf = spread<kPagedBf16>(not_finite<kPagedBf16>(w));
+                    const uint32_t least = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(ushortx2, w & 0x7fff7fffu), ushortx2{0x7f70, 0x7f70}));
+                    x[1][i][j] = (w & (inf | 0x80008000u)) | (least & ~inf);
                 }
         }
         store(1, (uint32_t)max(bits[0], bits[1]) << 16, [&](int i, float to) -> u32x2 {

@@ -70,3 +70,37 @@ def test_append_behind_a_stored_scale(D, byte, top):
         # the rest of the page
         assert torch.equal(_byte(cache)[p, :, held + new:], was[i][p, :, held + new:])
         assert torch.equal(_byte(scale)[p, :, 1:], was[2 + i][p, :, 1:])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("held", [0, 9])
+def test_append_largest_values(D, held):
+    """Finite values whose nearest code would stand for 2^128: the largest code that stands for a bf16 value instead, less than
+    half a step of e4m3 (2^-4 of the value) away. What is read back is finite."""
+    H, page, new = 2, 32, 6
+    x = torch.zeros(new, H, D, dtype=BF16, device=DEV)
+    top = torch.finfo(BF16).max
+    x[0, 0, :6] = torch.tensor([top, -top, 3.3e38, -3.3e38, 3.2e38, 1.0])
+    x[5, 1, -1] = -top
+    pool = Pool(3, FP8, [held + new], H, D, page)
+    p = int(pool.table[0, 0])
+    for byte in (1, 247, 250, 254):
+        for s in pool.scales:
+            _byte(s)[p, :, 0] = byte
+        ck, cv, table, _ = pool.args()
+        rv.append_paged_kv(x, x, ck, cv, table, _i32([held]), pairs=(0, 0, 0), theta=10000.0, h=1, w=1, **pool.kw())
+        for cache, scale in ((ck, pool.scales[0]), (cv, pool.scales[1])):
+            b = _byte(scale)[p, :, 0].tolist()
+            least = [247, 247] if held == 0 else [max(byte, 247)] * 2
+            assert b == least
+            back = cache[p, :, held:held + new].double() * torch.exp2(torch.tensor(b, device=DEV).double() - 127)[:, None, None]
+            want = x.double().transpose(0, 1)
+            assert bool(((back - want).abs() <= want.abs() * 2.0 ** -4 + 2.0 ** -10 * 2.0 ** (max(b) - 127)).all())
+            assert float(back.abs().max()) == 1.875 * 2.0 ** 127
+    # turned keys: by half a turn of the second pair, in fp32
+    k = torch.zeros(new, H, D, dtype=BF16, device=DEV)
+    k[..., 2], k[..., 3] = top, 1.0
+    pos = torch.zeros(new, 3, dtype=torch.int32, device=DEV)
+    pos[1::2, 0] = 1
+    rv.append_paged_kv(k, k, *pool.args()[:3], _i32([0]), pairs=(2, 0, 0), theta=float(np.float32(np.pi) ** -2), pos=pos, **pool.kw())
+    assert bool((pool.k[p, :, :new, 2].float().abs() == 240).all()) and _byte(pool.scales[0])[p, :, 0].tolist() == [247, 247]
