@@ -625,8 +625,10 @@ int compact_kv(const void* src_k, const void* src_v, int32_t src_rows,
  *                 or 128
  *   scale_k, scale_v  REVISIT_FP8_KV only: [n_pages][H][page / 32] bytes. The 32
  *                 positions of a block share one scale per head, 2^(byte - 127); a
- *                 stored value is its code times that, a bf16 value exactly. Byte 0
- *                 counts as 1, and 255 is NaN.
+ *                 stored value is its code times that, a bf16 value exactly but for
+ *                 the ends: values of 2^128 and more (bytes from 247 on) are infinite,
+ *                 those below 2^-126 (bytes below 10) may count as 0. Byte 0 counts
+ *                 as 1, and 255 is NaN.
  *
  * append_paged_kv_strided and paged_chunk_attention_strided take pools that lie otherwise
  * (positions before heads, keys and values in one tensor, ...): their layout

@@ -106,10 +106,18 @@ __device__ __forceinline__ uint32_t widen2(uint32_t x, float scale) {
 }
 
 // Which values of a word are not finite, by their top bits: e4m3 with all seven bits set, bf16 and fp32 with an exponent
-// of ones. spread: all bits of those values.
+// of ones. Under a scale of 2^120 and more (bytes from 247 on) codes from 2^(255 - byte) on stand for 2^128 and more, which are
+// infinities in bf16, and under a NaN scale none is finite: odd_codes(scale) is what is added to the seven bits of each
+// code, so that it passes into the top one. spread: all bits of those values.
+constexpr uint32_t kOddCodes = 0x01010101u;
+__device__ __forceinline__ uint32_t odd_codes(float scale) {
+    const int byte = (int)(__float_as_uint(scale) >> 23);  // 255: NaN
+    const int from = max(0x80 - ((262 - byte) << 3), 1);   // (262 - byte) << 3 is the code of 2^(255 - byte)
+    return (uint32_t)(byte == 255 ? 0x80 : from) * kOddCodes;
+}
 template <int T>
-__device__ __forceinline__ uint32_t not_finite(uint32_t x) {
-    if constexpr (T == kPagedFp8) return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+__device__ __forceinline__ uint32_t not_finite(uint32_t x, uint32_t odd = kOddCodes) {
+    if constexpr (T == kPagedFp8) return ((x & 0x7f7f7f7fu) + odd) & 0x80808080u;
     else if constexpr (T == kPagedBf16) return ((x & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
     else return ((x & 0x7fffffffu) + 0x00800000u) & 0x80000000u;
 }

@@ -448,13 +448,14 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (T == kPagedF32 ? D == 64 : NQ =
         // a masked tile holds such values, they are taken out of the operands, and the queries that see their
         // keys get them one by one.
         if (masked) {
-            uint32_t bad = v_scale != v_scale ? ~0u : 0u;
+            const uint32_t odd = T == kPagedFp8 ? odd_codes(v_scale) : 0u;
+            uint32_t bad = 0u;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
                 for (int u = 0; u < kVHalves; ++u)
 #pragma unroll
-                    for (int w = 0; w < Sh::kVWords / kVHalves; ++w) bad |= not_finite<T>(value_word(j, u, w));
+                    for (int w = 0; w < Sh::kVWords / kVHalves; ++w) bad |= not_finite<T>(value_word(j, u, w), odd);
             if (__builtin_expect(__any(bad != 0), 0)) {
                 const uint8_t* base = tile_at(a.cache_v, a.layout.v, t, page);
 #pragma unroll 1
@@ -479,20 +480,16 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (T == kPagedF32 ? D == 64 : NQ =
                             __builtin_amdgcn_sched_barrier(0);  // one mask at a time
                         }
                 }
-                uint32_t none = ~0u;
-                if (v_scale != v_scale) {
-                    none = 0u;
-                    v_scale = 1.0f;
-                }
+                if (v_scale != v_scale) v_scale = 1.0f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
 #pragma unroll
                     for (int u = 0; u < kVHalves; ++u) {
                         if constexpr (Sh::kVWords == 1) {
-                            b.vr[j][0] &= none & ~spread<T>(not_finite<T>(b.vr[j][0]));
+                            b.vr[j][0] &= ~spread<T>(not_finite<T>(b.vr[j][0], odd));
                         } else {
 #pragma unroll
-                            for (int w = 0; w < Sh::kVWords / kVHalves; ++w) b.vr[j][u][w] &= none & ~spread<T>(not_finite<T>(b.vr[j][u][w]));
+                            for (int w = 0; w < Sh::kVWords / kVHalves; ++w) b.vr[j][u][w] &= ~spread<T>(not_finite<T>(b.vr[j][u][w], odd));
                         }
                     }
             }

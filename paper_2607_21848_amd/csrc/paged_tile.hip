@@ -278,7 +278,7 @@ __global__ __launch_bounds__(256, kQ == 2 ? 1 : 2) void paged_tile_kernel(PagedA
     // values (and whatever lies behind the stream's end) are left out here; the rows that see them get them one by
     // one (odd_values).
     auto leave_out = [&](int which, float& v_scale, int jv, int bv) __attribute__((always_inline)) {
-        const float f = T == kPagedFp8 ? v_scale : 1.0f;
+        const uint32_t codes = T == kPagedFp8 ? odd_codes(v_scale) : 0u;
         uint32_t odd = 0;
 #pragma unroll
         for (int p = 0; p < kPieces; ++p) {
@@ -287,14 +287,14 @@ __global__ __launch_bounds__(256, kQ == 2 ? 1 : 2) void paged_tile_kernel(PagedA
             const bool none = bv < 0 || (t0 + jv) * kTK + i / (kStored / 16) >= held;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const uint32_t bad = f != f ? ~0u : spread<T>(not_finite<T>(piece[p][w]));
+                const uint32_t bad = spread<T>(not_finite<T>(piece[p][w], codes));
                 if (none) piece[p][w] = 0;
                 else odd |= bad;
                 piece[p][w] &= ~bad;
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (f != f) v_scale = 1.0f;
+        if (v_scale != v_scale) v_scale = 1.0f;
         if (odd) lds_odd[which] = jv;
     };
     // half h of piece p, as bf16 (8-bit pages: 8 values; else the whole piece in half 0)
@@ -405,9 +405,8 @@ __global__ __launch_bounds__(256, kQ == 2 ? 1 : 2) void paged_tile_kernel(PagedA
         return lds_tab[hh][hh ? ky : p - ky * grid_w];
     };
     int cur_s = -1;  // retrieved frame whose operands are in lds_qop
-    // slot of tile j's frame (and position p in it); the wave's query operands follow it
-    auto classify = [&](int j, int& p) __attribute__((always_inline)) -> int {
-        const int2 x = lds_bias[j & 511];
+    // slot of a tile's frame (and position p in it) by what lds_bias has of it; the wave's query operands follow it
+    auto classify = [&](int2 x, int& p) __attribute__((always_inline)) -> int {
         const int sl = __builtin_amdgcn_readfirstlane(x.x);
         p = x.y;
         if (__builtin_expect(sl >= 0 && sl != cur_s, 0)) {
@@ -516,10 +515,15 @@ __global__ __launch_bounds__(256, kQ == 2 ? 1 : 2) void paged_tile_kernel(PagedA
         const bool more = j + 1 < nt;  // past the last tile its logits are computed again and not used
         const uint8_t* vt = next + kTileB;
         auto kread = [&](int kk) { kf[kk] = *reinterpret_cast<const u32x4*>(next + koff[kk]); };
+        int2 bias_at = make_int2(-1, 0);
+        if constexpr (kBias) {
+            bias_at = lds_bias[(j + 1) & 511];
+            __builtin_amdgcn_sched_barrier(0);  // the first of the step's reads: it is the one that is waited for
+        }
         const int b4_lane = block_of(j + 4);
         float k_scale = T == kPagedFp8 ? lds_scale[0][(j + 3) & 511] : 1.0f, v_scale = T == kPagedFp8 ? lds_scale[1][(j + 2) & 511] : 1.0f;
         int bias_slot = -1, bias_p = 0;
-        if constexpr (kBias) bias_slot = classify(j + 1, bias_p);
+        if constexpr (kBias) bias_slot = classify(bias_at, bias_p);
         u32x4 kop = u32x4{0, 0, 0, 0}, qop[kQ];
         // rescale where a row's maximum has grown by more than the slack
         bool grown = false;
@@ -673,7 +677,7 @@ __global__ __launch_bounds__(256, kQ == 2 ? 1 : 2) void paged_tile_kernel(PagedA
         }
         if constexpr (kBias) {
             int p = 0;
-            const int sl = classify(0, p);
+            const int sl = classify(lds_bias[0], p);
             if (sl >= 0) {
                 const u32x4 kop = key_operand(p + krow);
 #pragma unroll

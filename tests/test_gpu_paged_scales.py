@@ -104,3 +104,105 @@ def test_append_largest_values(D, held):
     pos[1::2, 0] = 1
     rv.append_paged_kv(k, k, *pool.args()[:3], _i32([0]), pairs=(2, 0, 0), theta=float(np.float32(np.pi) ** -2), pos=pos, **pool.kw())
     assert bool((pool.k[p, :, :new, 2].float().abs() == 240).all()) and _byte(pool.scales[0])[p, :, 0].tolist() == [247, 247]
+
+
+@pytest.fixture(params=[0, 1 << 19], ids=["table", "wide_table"])
+def room(request, monkeypatch):
+    """Page tables with just the entries that the streams need, and far wider ones, for which other kernels are chosen."""
+    monkeypatch.setattr(Pool, "room", request.param)
+
+
+class Stored(Pool):
+    """What the pages hold by their definition: byte 0 counts as 1, and 2^128 and more is infinite."""
+
+    def held(self, s):
+        k, v, have = super().held(s)
+        return tuple(np.where(np.abs(x) >= 2.0 ** 128, np.copysign(np.inf, x), x) for x in (k, v)) + (have,)
+
+
+def _attend(pool, q, visible=None, **kw):
+    return rv.paged_chunk_attention(q, *pool.args(), visible=None if visible is None else _i32(visible), softmax_scale=q.shape[-1] ** -0.5, **pool.kw(), **kw)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("m", [1, 17, 40, 150])
+@pytest.mark.parametrize("byte", [247, 248, 251, 254, 255])
+def test_values_past_the_largest_that_are_not_seen(room, D, m, byte):
+    """Codes whose value, with the block's scale, is infinite or NaN, at positions that only some queries see."""
+    L, H, page = 170, 2, 64
+    pool = Stored(5, FP8, [L], H, D, page)
+    q = values(gen(6), BF16, m, H, D)
+    visible = np.arange(L - m, L) + 1
+    if m == 1:
+        visible[:] = 150
+    t = pool.table[0]
+    least = 2.0 ** (255 - min(byte, 254))  # the least code value that is infinite: 256 for 247, 2 for 254
+    for blk, at in ((128 // 32, (155, 156)), (160 // 32, (168, 169))):
+        p, row = t[blk * 32 // page], blk * 32 % page
+        pool.v[p, :, row:row + 32] = 0  # a sum that holds values near the largest may pass it
+        _byte(pool.scales[1])[p, :, row // 32] = byte
+        for j, c in enumerate(at):
+            pool.v[p, j % 2, c % page, 3 * j:3 * j + 4] = torch.tensor([least, -least, min(448.0, 1.75 * least), least], device=DEV).to(FP8)
+            if byte == 247:
+                pool.v[p, :, c % page, 20:24] = torch.tensor([2.0 ** -9, -2.0 ** -9, 0.0, -0.0], device=DEV).to(FP8)
+    o, lse = _attend(pool, q, visible)
+    blind = np.flatnonzero(visible <= (128 if byte == 255 else 155))
+    if len(blind):
+        assert bool(torch.isfinite(o[blind[0]:blind[-1] + 1]).all())
+    assert bool(torch.isfinite(lse).all())
+    check_attention(pool, q, o, lse, None, visible)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("m", [1, 17, 40, 150])
+def test_nan_scales(room, D, m):
+    """Blocks of keys and values whose scale is NaN: what sees a key of one has a NaN logit, what does not is as without it."""
+    L, H, page = 200, 2, 32
+    pool = Stored(7, FP8, [L], H, D, page)
+    q = values(gen(8), BF16, m, H, D)
+    visible = np.linspace(100, L, m).astype(int)
+    if m == 1:
+        visible[:] = 159
+    _byte(pool.scales[0])[pool.table[0, 5], 1, 0] = 255  # keys 160 .. 191 of head 1
+    _byte(pool.scales[1])[pool.table[0, 6], 0, 0] = 255  # values 192 .. of head 0
+    o, lse = _attend(pool, q, visible)
+    blind = np.flatnonzero(visible <= 160)
+    seeing = np.flatnonzero(visible > 160)
+    sub = slice(int(blind[0]), int(blind[-1]) + 1)
+    assert bool(torch.isfinite(o[sub]).all())
+    check_attention(pool, q[sub], o[sub], lse[:, sub].contiguous(), None, visible[sub])
+    for p in seeing:
+        assert bool(torch.isnan(o[p, 1]).all()) and bool(torch.isnan(lse[1, p]))
+        assert bool(torch.isnan(o[p, 0]).all()) == (visible[p] > 192) and bool(torch.isfinite(lse[0, p]))
+    # head 0 has no NaN logit
+    one = Stored(7, FP8, [L], 1, D, page)
+    one.table, one.n_pages = pool.table, pool.n_pages
+    one.k, one.v = pool.k[:, :1], pool.v[:, :1]
+    one.scales = [_byte(s)[:, :1].contiguous().view(E8M0) for s in pool.scales]
+    check_attention(one, q[:, :1], o[:, :1], lse[:1], None, visible)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("m", [1, 17, 40, 150])
+def test_scales_of_any_size(room, D, m):
+    """A scale is a power of two: values under other ones give the same times their ratio, bit for bit. Byte 0 counts as 1."""
+    L, page = 300, 64
+    pool = Pool(9, FP8, [L], 2, D, page)
+    q = values(gen(10), BF16, m, 2, D)
+    got = {}
+    for byte in (0, 1, 60, 127, 180):
+        _byte(pool.scales[1])[:] = byte
+        o, lse = _attend(pool, q)
+        got[byte] = o.double()
+        if byte == 127:
+            check_attention(pool, q, o, lse)
+    for byte in (60, 180):
+        assert torch.equal(got[byte] * 2.0 ** (127 - byte), got[127])
+    assert torch.equal(got[0], got[1])
+    for byte, other in ((0, 1), (90, 127)):
+        o = []
+        for b in (byte, other):
+            _byte(pool.scales[0])[:] = b
+            _byte(pool.scales[1])[:] = 127
+            o.append(rv.paged_chunk_attention(q, *pool.args(), softmax_scale=D ** -0.5 * 2.0 ** ((127 - b) if byte else 100), **pool.kw()))
+        assert torch.equal(o[0][0], o[1][0]) and torch.equal(o[0][1], o[1][1])
