@@ -446,8 +446,9 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (T == kPagedF32 ? D == 64 : NQ =
         }
         // A query's weight of a key that it does not see is 0, and 0 times a value that is not finite would be NaN. Where
         // a masked tile holds such values, they are taken out of the operands, and the queries that see their
-        // keys get them one by one.
-        if (masked) {
+        // keys get them one by one. So they do where a probability is two numbers, whose second one may be 0 or have
+        // the other sign (8 bits are infinite under scales from 2^120 on alone).
+        if (masked || (kFine && (T == kPagedBf16 || v_scale >= 0x1p120f))) {
             const uint32_t odd = T == kPagedFp8 ? odd_codes(v_scale) : 0u;
             uint32_t bad = 0u;
 #pragma unroll

@@ -151,6 +151,9 @@ def test_values_past_the_largest_that_are_not_seen(room, D, m, byte):
         assert bool(torch.isfinite(o[blind[0]:blind[-1] + 1]).all())
     assert bool(torch.isfinite(lse).all())
     check_attention(pool, q, o, lse, None, visible)
+    if m == 1:  # every query sees them all
+        o, lse = _attend(pool, q)
+        check_attention(pool, q, o, lse)
 
 
 @pytest.mark.parametrize("D", [64, 128])
@@ -206,3 +209,23 @@ def test_scales_of_any_size(room, D, m):
             _byte(pool.scales[1])[:] = 127
             o.append(rv.paged_chunk_attention(q, *pool.args(), softmax_scale=D ** -0.5 * 2.0 ** ((127 - b) if byte else 100), **pool.kw()))
         assert torch.equal(o[0][0], o[1][0]) and torch.equal(o[0][1], o[1][1])
+
+
+@pytest.mark.parametrize("dtype", [FP8, BF16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("m", [1, 16, 17, 40, 150])
+def test_infinite_values_that_all_see(room, dtype, D, m):
+    """An infinity among the values of keys that every query of the tile sees is the output's, with its sign."""
+    L, H, page = 160, 2, 32
+    pool = Stored(11, dtype, [L], H, D, page)
+    q = values(gen(12), {FP8: BF16}.get(dtype, dtype), m, H, D)
+    p = pool.table[0, 2]
+    if dtype == FP8:
+        pool.v[p] = 0
+        pool.v[p, :, 5, 3:5] = torch.tensor([256.0, -256.0], device=DEV).to(FP8)
+        _byte(pool.scales[1])[p] = 247
+    else:
+        pool.v[p, :, 5, 3:5] = torch.tensor([INF, -INF], device=DEV).to(dtype)
+    o, lse = _attend(pool, q)
+    assert bool((o[..., 3] == INF).all()) and bool((o[..., 4] == -INF).all())
+    check_attention(pool, q, o, lse)
