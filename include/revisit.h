@@ -668,7 +668,7 @@ typedef struct rc_pool_layout {
  *   out_len       nullable [B] int32: the streams' new lengths, kv_len[s] plus its
  *                 tokens, at most max_pages page. Not kv_len itself
  *   pairs_t, pairs_y, pairs_x, theta, pos, t0, h, w  as for rotary_embed; all three 0:
- *                 keys are copied
+ *                 keys are copied (t0, h and w are then not read)
  *
  * No output (caches, scales, out_len) may overlap an input or another output
  * (REVISIT_ERR_SHAPE); but caches and scales may have their pages, heads or positions

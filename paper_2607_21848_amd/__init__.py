@@ -691,7 +691,7 @@ def append_paged_kv(k: torch.Tensor, v: torch.Tensor, cache_k: torch.Tensor, cac
     Stream s has tokens cu[s] .. cu[s+1]-1 of the n (cu [B+1] i32; None: n // B
     each); they go to its positions kv_len[s] on. Keys get the rotary position of
     rotary_embed (pairs, theta): position c stands at (t0 + c // (h*w), c // w % h,
-    c % w), or a token at pos[i] with pos [n, 3] i32. Returns the new lengths [B]
+    c % w), or a token at pos[i] with pos [n, 3] i32; pairs (0, 0, 0): keys as they are. Returns the new lengths [B]
     i32 (out_len, which must not be kv_len). No output may overlap an input; no
     autograd graph is recorded."""
     if not isinstance(k, torch.Tensor) or k.dim() != 3:

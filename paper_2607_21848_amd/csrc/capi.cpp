@@ -1138,7 +1138,8 @@ int append_paged_kv_strided(const void* k, int64_t k_row, const void* v, int64_t
     if (pairs_t < 0 || pairs_y < 0 || pairs_x < 0 || (int64_t)pairs_t + pairs_y + pairs_x > D / 2)
         return fail(REVISIT_ERR_PARAM, "%s: bands of %d + %d + %d pairs in a head of %d", fn, pairs_t, pairs_y, pairs_x, D / 2);
     if (!(finite(theta) && theta > 0.0f)) return fail(REVISIT_ERR_PARAM, "%s: theta must be finite and > 0", fn);
-    if (!pos && (h < 1 || w < 1 || (int64_t)h * w > INT32_MAX))
+    const bool grid = !pos && pairs_t + pairs_y + pairs_x > 0;  // positions come from the token grid
+    if (grid && (h < 1 || w < 1 || (int64_t)h * w > INT32_MAX))
         return fail(REVISIT_ERR_SHAPE, "%s: without positions the token grid is needed: h, w >= 1", fn);
     const int esize = dtype == REVISIT_F32 ? 4 : 2;
     const int64_t row = (int64_t)H * D, most = kMaxElems / (n_tokens > 1 ? n_tokens : 1);
@@ -1188,8 +1189,8 @@ int append_paged_kv_strided(const void* k, int64_t k_row, const void* v, int64_t
     a.D = D;
     a.pos = pos;
     a.t0 = t0;
-    a.hw = pos ? 1 : h * w;
-    a.w = pos ? 1 : w;
+    a.hw = grid ? h * w : 1;
+    a.w = grid ? w : 1;
     a.n_t = pairs_t;
     a.n_y = pairs_y;
     a.n_x = pairs_x;

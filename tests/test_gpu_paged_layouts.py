@@ -232,3 +232,19 @@ def test_in_a_graph(dtype):
         assert torch.equal(a, want[0]) and torch.equal(b, want[1])
         _same(ck, k2), _same(cv, v2)
         held.copy_(after)
+
+
+@pytest.mark.parametrize("dtype", [FP8, BF16, F32])
+def test_keys_without_a_rotation_need_no_grid(dtype):
+    pool, other = (Pool(16, dtype, [70], 2, 64, 32) for _ in range(2))
+    ck, cv, table, _ = pool.args()
+    k, v = (values(gen(17 + i), GIVEN[dtype], 60, 2, 64) for i in range(2))
+    start = torch.tensor([10], dtype=torch.int32, device=DEV)
+    rv.append_paged_kv(k, v, ck, cv, table, start, pairs=(0, 0, 0), theta=10000.0, **pool.kw())
+    rv.append_paged_kv(k, v, other.k, other.v, table, start, pairs=(0, 0, 0), theta=10000.0, h=3, w=5, t0=9, **other.kw())
+    for a, b in zip((ck, cv, *pool.scales), (other.k, other.v, *other.scales)):
+        if a is not None:
+            _same(a, b)
+    if dtype != FP8:
+        rows = torch.cat([ck[p] for p in table[0].tolist()], 1)[:, 10:70]
+        _same(rows.transpose(0, 1), k)

@@ -124,3 +124,13 @@ def test_attention(L):  # noqa: F811
                           (_layout(sk=(1 << 20, 2, 1)), dict(o=(1 << 27) + (1 << 21)), "o overlaps scale_k")]:
         st, err = _attend(L, lay, **kw)
         assert st == 2 and what in err, (what, err)
+
+
+def test_keys_that_are_copied_have_no_grid(L):  # noqa: F811
+    def append(pairs, h, w):
+        L.append_paged_kv(at(1), H * D, at(2), H * D, 2, 1, NULL, 1, at(3), at(3), at(4), at(5), NULL, NULL, at(20), PAGES, PAGE, 4, H, D, NULL, 0, h, w,
+                          *pairs, 10000.0, NULL)
+        return _lib.last_error()
+    for h, w in ((0, 0), (-1, 5), (1 << 20, 1 << 20)):
+        assert PASSED in append((0, 0, 0), h, w)
+        assert "token grid" in append((0, 0, 1), h, w)
