@@ -756,7 +756,7 @@ def paged_chunk_attention(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch
     dev = q.device
     dt, idt, n_pages, Hk, page, Dk, B, max_pages, layout = _pages(cache_k, cache_v, scale_k, scale_v, page_table, kv_len, cu, n, dev)
     Hq, q_row = _rows(q, "q", idt, n, Dk, dev.index)
-    if Hq % Hk:
+    if not Hk or Hq % Hk:
         raise ValueError(f"{Hq} query heads are not a multiple of {Hk} key heads")
     if visible is not None:
         _need(visible, "visible", torch.int32, (n,), dev)

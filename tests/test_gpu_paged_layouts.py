@@ -248,3 +248,14 @@ def test_keys_without_a_rotation_need_no_grid(dtype):
     if dtype != FP8:
         rows = torch.cat([ck[p] for p in table[0].tolist()], 1)[:, 10:70]
         _same(rows.transpose(0, 1), k)
+
+
+def test_pools_without_heads_are_refused():
+    pool = torch.zeros(2, 0, 32, 64, dtype=BF16, device=DEV)
+    table, lens = torch.zeros(1, 2, dtype=torch.int32, device=DEV), torch.ones(1, dtype=torch.int32, device=DEV)
+    q = values(gen(19), BF16, 3, 2, 64)
+    for heads in (2, 0):
+        with pytest.raises(ValueError):
+            rv.paged_chunk_attention(q[:, :heads], pool, pool, table, lens, softmax_scale=0.1)
+    with pytest.raises(rv.RevisitError):
+        rv.append_paged_kv(q[:, :0], q[:, :0], pool, pool, table, lens, pairs=(0, 0, 0), theta=10000.0)
