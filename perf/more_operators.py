@@ -148,7 +148,7 @@ def _pages(g, c, n_pages):
         return _values(g, STORED[c["cache"]], n_pages * P, H, D).view(n_pages, P, H, D).transpose(1, 2).contiguous(), None
     x = _values(g, torch.float32, n_pages * P, H, D).view(n_pages, P // BLOCK, BLOCK, H, D).permute(0, 3, 1, 2, 4)
     e = _exponent(x.abs().amax((3, 4)))
-    code = (x * torch.exp2(-e)[..., None, None]).to(E4M3).contiguous().view(n_pages, H, P, D)
+    code = (x * torch.exp2(-e)[..., None, None]).to(E4M3).reshape(n_pages, H, P, D)
     return code, (e + 127).to(torch.uint8).view(E8M0)
 
 
