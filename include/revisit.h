@@ -733,7 +733,9 @@ int append_paged_kv_strided(const void* k, int64_t k_row, const void* v, int64_t
  *
  * Hq is a multiple of Hk; n_tokens Hq / Hk <= 2^30. q must not overlap o; outputs
  * must not overlap inputs (REVISIT_ERR_SHAPE). Sums, maxima and logits are fp32,
- * probabilities are rounded to bf16 for the product with the values (fp32 pages: not at all), outputs once.
+ * probabilities are rounded to bf16 for the product with the values (fp32 pages: not at
+ * all; where streams have up to 16 queries times Hq / Hk on average: to the sum of two bf16 numbers, within
+ * 2^-16), outputs once.
  * n_tokens == 0 or B == 0 is valid (nothing to do). Results do not change between calls (no atomics).
  */
 int paged_chunk_attention(const void* q, int64_t q_row, const void* cache_k, const void* cache_v,

@@ -7,9 +7,11 @@
 //
 // That is how pools lie that come without a layout. With one, pages, heads and positions are any distances apart, and a
 // position's D elements alone lie together. Such pools have kernels of their own: in those for contiguous ones the distances are
-// numbers in the code. [pages][page][H][D] in 8 bits beside contiguous: 4680 queries on 28080 keys 910 us and 875, 10800
-// tokens of 40 heads appended 65 and 61, one query on 37440 keys 26.7 and 24.8; but 64 single tokens of up to 16384 keys 332
-// and 258: each head's workgroup then reads 128 bytes in every 1024.
+// numbers in the code. [pages][page][H][D] in 8 bits beside contiguous: 4680 queries on 28080 keys 920 us and 877, 10800
+// tokens of 40 heads appended 65 and 61, one query on 37440 keys 26.7 and 24.8; but 64 single tokens of up to 16384 keys, 8
+// heads, 332 and 258. A head's rows are 1024 bytes apart there, a power of two, and few workgroups then ask few of the
+// memory's channels: with rows of 1152 bytes 260, with key_parts = 3 instead of the one part that is chosen 261. The
+// choice does not know the layout, since the workspace's size does not. Other heads in turn on each XCD: 338.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -100,8 +100,9 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (T == kPagedF32 ? D == 64 : NQ =
     constexpr int kRows = 16 * NQ;
     constexpr int kDb = Sh::kDb;
     constexpr bool kF32 = T == kPagedF32;
-    // few rows leave the matrix cores idle: their probabilities go in as two bf16 values each, off by 2^-17 (a single
-    // one, 2^-9, made outputs of a few heavy keys 1.6 times as far off as their own rounding does)
+    // Few rows leave the matrix cores idle: their probabilities go in as two bf16 values each, off by 2^-17 (a single
+    // one, 2^-9, made outputs of a few heavy keys 1.6 times as far off as their own rounding does). Tiles of 32 rows keep
+    // one, like the tile kernel's: 30 queries on 37440 8-bit keys 26.6 us, with two 29.2.
     constexpr bool kFine = !kF32 && NQ == 1;
     // The next tile's keys leave behind this one's logits, its values behind this one's product, where the registers hold both
     // beside each other (1170 fp32 queries on 7020 keys, when it was taken: 606 us without, 567 with).
@@ -633,8 +634,8 @@ __global__ __launch_bounds__(64 * kW, kW > 4 || (T == kPagedF32 ? D == 64 : NQ =
 // O = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p over the key parts of a tile's row: a part without keys has m = -inf
 // and nothing else that counts. A workgroup takes kRowsPer rows, 256 / kRowsPer threads each: D / 4 of them hold a part's
 // head dims, and as many parts are read at once as there are such groups; their maxima and sums meet in LDS. Bound by
-// latency: four parts of a group are loaded at a time, maxima with the rest (12 rows of 8 and of 21 parts: 4.1 us; the maxima
-// first and each part when its own is there: 5.1).
+// latency: four parts of a group are loaded at a time, maxima with the rest (12 rows of 12 parts 3.4 us, of 21 4.6; the maxima
+// first and each part when its own is there took a quarter longer).
 template <int D, bool kF32, int kRowsPer>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttentionArgs a, unsigned blocks) {
     constexpr int kLanes = D / 4, kThreads = 256 / kRowsPer, kGroups = kThreads / kLanes;
